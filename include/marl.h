@@ -305,6 +305,98 @@ int32_t marl_evaluate(const marl_config* cfg, marl_env_state st, const float* pa
 int32_t marl_timing_enable(int32_t on);
 int32_t marl_timing_read(int32_t kernel_class, double* total_ms, int64_t* launches, double* work);
 
+/* ---- Sequence memories ------------------------------------------------------------------------------------------------
+ * Operators of a memory that learns from whole rollouts at once and acts from a state of constant size: linear attention
+ * with a decay for each head, rotary positions, layer norm.  (The paper's recurrent systems, Section 2, carry such a state
+ * through an episode; it names no cell.)  Arrays are time-major: T steps, B sequences (environments times agents), heads.
+ * precision 0: fp32 elements, 1: bf16; states, decays, norm parameters and statistics, tables are fp32 always. */
+
+/* An array [T][B][heads][dim] in place: element (t, b, h, d) at data + (t * step + b * seq + h * head + d) elements.  `data` need only
+ * be aligned to its elements; where it and the three strides are multiples of 16 bytes the kernels use 16-byte accesses.  Outputs
+ * overlap neither each other nor an input (marl_rotary: an output may be its input). */
+typedef struct marl_view {
+  void* data;
+  int64_t step, seq, head;
+} marl_view;
+
+typedef struct marl_attention_dims {
+  int32_t precision;
+  int32_t n_steps, n_seqs;       /* T, B; zero is allowed */
+  int32_t n_heads, n_kv_heads;   /* query head h reads key / value head h / (n_heads / n_kv_heads) */
+  int32_t dim_k, dim_v;          /* 1..128 */
+  int32_t seqs_per_flag;         /* sequences that share a done flag: the agents of an environment.  B is a multiple of it */
+  float scale;
+} marl_attention_dims;
+
+/* Linear attention with a decay for each head.  Per sequence and query head, with g = decay[h] (0 <= g <= 1), S a [dim_k][dim_v] matrix:
+ *   S_t = keep_t g S_{t-1} + k_t v_t^T,   out_t = scale * S_t^T q_t,   next_state = keep_T S_{T-1}
+ * S_{-1} = state [B][n_heads][dim_k][dim_v] (NULL: zero), keep_t = 0 where done [T][B / seqs_per_flag] (NULL: none) is nonzero at t - 1,
+ * otherwise 1: a nonzero done_t says that step t ended an episode, as in marl_traj, so packed sequences of different lengths are
+ * one sequence with flags.  next_state (nullable) is zero where the last step ended an episode.  T = 0: next_state = state.
+ * A step's output depends on the steps of its own episode up to it only, infinities and NaNs included.
+ * bf16: products have bf16 operands where these are exact or split into parts, sums and the state are fp32; outputs are rounded once.
+ * workspace: marl_linear_attention_workspace bytes.  Errors: MARL_E_NULL, MARL_E_ALIGN, MARL_E_SIZE, MARL_E_CONFIG, MARL_E_LAUNCH. */
+int32_t marl_linear_attention(const marl_attention_dims* dims, marl_view q, marl_view k, marl_view v, const float* decay,
+                              const float* state, const uint8_t* done, marl_view out, float* next_state, void* workspace,
+                              void* stream);
+
+/* Its gradient: dq, dk, dv, and dstate [B][n_heads][dim_k][dim_v] (nullable) from dout and dnext_state (NULL: zero).  dk and dv of a head that
+ * query heads share are sums over these, in a fixed order.  The decays are constants of the layer: they have no gradient. */
+int32_t marl_linear_attention_backward(const marl_attention_dims* dims, marl_view q, marl_view k, marl_view v,
+                                       const float* decay, const float* state, const uint8_t* done, marl_view dout,
+                                       const float* dnext_state, marl_view dq, marl_view dk, marl_view dv, float* dstate,
+                                       void* workspace, void* stream);
+
+/* One step, for acting: next_state = keep g state + k v^T, out = scale * next_state^T q, with n_steps = 1 (the views' step strides
+ * are not used).  fresh [B / seqs_per_flag] (NULL: none): nonzero where an episode begins with this step, keep = 0 there.
+ * next_state may be `state`. */
+int32_t marl_linear_attention_step(const marl_attention_dims* dims, marl_view q, marl_view k, marl_view v,
+                                   const float* decay, const float* state, const uint8_t* fresh, marl_view out,
+                                   float* next_state, void* stream);
+
+/* Workspace of marl_linear_attention (backward = 0) or of its gradient (1) in bytes, into *bytes.  Touches no GPU. */
+int32_t marl_linear_attention_workspace(const marl_attention_dims* dims, int32_t backward, int64_t* bytes);
+
+/* Layer norm over rows: y = (x - mean) * rstd * weight + bias, rstd = 1 / sqrt(var + eps), population variance of the row's
+ * `width` (1..16384) values.  x, y: row r at r * x_stride / r * y_stride elements, elements of `precision`, aligned to their size.  weight, bias
+ * [width] (NULL: 1, 0).  mean, rstd [n_rows] (nullable): kept for the gradient.  y may be x where the strides agree. */
+int32_t marl_layer_norm(int32_t precision, int64_t n_rows, int32_t width, const void* x, int64_t x_stride,
+                        const float* weight, const float* bias, float eps, void* y, int64_t y_stride, float* mean,
+                        float* rstd, void* stream);
+
+/* Its gradient.  With xhat = (x - mean) * rstd and u = dy * weight: dx = rstd * (u - mean(u) - xhat * mean(u * xhat)),
+ * dweight = sum over rows of dy * xhat, dbias = sum over rows of dy (fp32, both nullable, added in an order that depends on the
+ * sizes only).  dx may be dy or x where the strides agree.  workspace: marl_layer_norm_workspace bytes. */
+int32_t marl_layer_norm_backward(int32_t precision, int64_t n_rows, int32_t width, const void* dy, int64_t dy_stride,
+                                 const void* x, int64_t x_stride, const float* weight, const float* mean,
+                                 const float* rstd, void* dx, int64_t dx_stride, float* dweight, float* dbias,
+                                 void* workspace, void* stream);
+int32_t marl_layer_norm_workspace(int64_t n_rows, int32_t width, int64_t* bytes);
+
+/* Frequencies of the rotary table: pair i of rotary_dim / 2 turns by f_i radians a position, f_i = base^(-2 i / rotary_dim), changed for
+ * contexts `factor` times as long as the ones trained on:
+ *   scaling 0: not;  1: f_i / factor;  2: base * factor^(rotary_dim / (rotary_dim - 2)) in place of base (rotary_dim >= 4);
+ *   3: by its turns over the trained length, n_i = trained_length f_i / (2 pi): m f_i + (1 - m) f_i / factor, m = (n_i - slow) / (fast - slow)
+ *      held to 0..1, so pairs that turn often keep their frequency. */
+typedef struct marl_rotary_dims {
+  int32_t n_positions, rotary_dim; /* table rows; even */
+  int32_t scaling;
+  float base, factor, trained_length, slow, fast;
+  float amplitude; /* cosines and sines are multiplied by it */
+} marl_rotary_dims;
+
+/* table [n_positions][rotary_dim]: rotary_dim / 2 cosines, then the sines, of position * f_i, computed in 64 bits. */
+int32_t marl_rotary_table(const marl_rotary_dims* dims, float* table, void* stream);
+
+/* Rotation of the first rotary_dim elements of every head of q [T][B][n_heads][dim] and, with the same positions, k [T][B][n_kv_heads][dim]
+ * (k.data NULL: q alone): (x1, x2) -> (x1 c - x2 s, x1 s + x2 c), pairs (i, i + rotary_dim / 2), or (2 i, 2 i + 1) when
+ * interleaved = 1; the other elements are copied.  inverse = 1 turns back (s -> -s): the gradient of the rotation is that.
+ * positions [T][B / seqs_per_flag] int32 (NULL: first_position + t).  A position outside the table gives NaNs in the rotated
+ * elements.  dims: precision, n_steps, n_seqs, n_heads, n_kv_heads, dim_k (1 or more), seqs_per_flag are read. */
+int32_t marl_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, const float* table, int32_t n_positions,
+                    int32_t rotary_dim, const int32_t* positions, int32_t first_position, int32_t interleaved,
+                    int32_t inverse, marl_view q_out, marl_view k_out, void* stream);
+
 /* Human-readable name of a status code (static storage, host).  Part of the error convention of this boundary,
  * not of the paper's method. */
 const char* marl_status_string(int32_t status);

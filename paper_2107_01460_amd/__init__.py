@@ -8,5 +8,7 @@ from .binding import (  # noqa: F401
     Config, EnvState, Traj, MarlError, lib, make_config, query_sizes, env_reset, observe, env_step,
     policy_forward, sample_actions, rollout, rollout_static, compute_gae, ppo_update, status_string, alloc_workspace,
     timing_enable, timing_read, KERNEL_CLASSES, EvalStats, evaluate, RecState, rollout_recurrent, ppo_update_recurrent, train_step, alloc_counters,
+    linear_attention, linear_attention_backward, linear_attention_step, linear_attention_workspace, layer_norm, layer_norm_backward,
+    layer_norm_workspace, rotary, rotary_table,
 )
 from .trainer import Trainer  # noqa: F401,E402

@@ -53,8 +53,24 @@ class RecStateC(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("ha0", "hc0", "ha1", "hc1")]
 
 
+class AttentionDims(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("precision", "n_steps", "n_seqs", "n_heads", "n_kv_heads", "dim_k", "dim_v", "seqs_per_flag")] + [
+        ("scale", C.c_float)]
+
+
+class View(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("step", C.c_int64), ("seq", C.c_int64), ("head", C.c_int64)]
+
+
+class RotaryDims(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_positions", "rotary_dim", "scaling")] + [
+        (n, C.c_float) for n in ("base", "factor", "trained_length", "slow", "fast", "amplitude")]
+
+
 EXPORTS = ("marl_query_sizes", "marl_env_reset", "marl_observe", "marl_env_step", "marl_policy_forward",
            "marl_sample_actions", "marl_rollout", "marl_rollout_static", "marl_compute_gae", "marl_ppo_update", "marl_train_step", "marl_evaluate", "marl_rollout_recurrent", "marl_ppo_update_recurrent",
+           "marl_linear_attention", "marl_linear_attention_backward", "marl_linear_attention_step", "marl_linear_attention_workspace",
+           "marl_layer_norm", "marl_layer_norm_backward", "marl_layer_norm_workspace", "marl_rotary_table", "marl_rotary",
            "marl_timing_enable",
            "marl_timing_read", "marl_status_string")
 
@@ -84,6 +100,16 @@ def lib():
         L.marl_evaluate.argtypes = [cp, EnvStateC, vp, C.c_int32, EvalStatsC, vp, vp]
         L.marl_rollout_recurrent.argtypes = [cp, EnvStateC, vp, TrajC, RecStateC, C.c_uint64, vp, vp, vp, vp]
         L.marl_ppo_update_recurrent.argtypes = [cp, TrajC, RecStateC, vp, vp, vp, C.c_int64, vp, vp, vp, vp, vp]
+        ap, i32, i64 = C.POINTER(AttentionDims), C.c_int32, C.c_int64
+        L.marl_linear_attention.argtypes = [ap, View, View, View, vp, vp, vp, View, vp, vp, vp]
+        L.marl_linear_attention_backward.argtypes = [ap, View, View, View, vp, vp, vp, View, vp, View, View, View, vp, vp, vp]
+        L.marl_linear_attention_step.argtypes = [ap, View, View, View, vp, vp, vp, View, vp, vp]
+        L.marl_linear_attention_workspace.argtypes = [ap, i32, C.POINTER(i64)]
+        L.marl_layer_norm.argtypes = [i32, i64, i32, vp, i64, vp, vp, C.c_float, vp, i64, vp, vp, vp]
+        L.marl_layer_norm_backward.argtypes = [i32, i64, i32, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, vp]
+        L.marl_layer_norm_workspace.argtypes = [i64, i32, C.POINTER(i64)]
+        L.marl_rotary_table.argtypes = [C.POINTER(RotaryDims), vp, vp]
+        L.marl_rotary.argtypes = [ap, View, View, vp, i32, i32, vp, i32, i32, i32, View, View, vp]
         L.marl_timing_enable.argtypes = [C.c_int32]
         L.marl_timing_read.argtypes = [C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_int64), C.POINTER(C.c_double)]
         L.marl_status_string.argtypes = [C.c_int32]
@@ -306,6 +332,166 @@ def train_step(cfg, state, params, traj, adam_m, adam_v, counters, perm, stats, 
     _check(lib().marl_train_step(C.byref(make_config(cfg)), state.c(), _ptr(params), traj.c(), _ptr(adam_m),
                                  _ptr(adam_v), _ptr(counters), _ptr(perm), _ptr(stats), _ptr(rollout_workspace),
                                  _ptr(update_workspace), _stream(stream)))
+
+
+# ---- sequence memories ---------------------------------------------------------------------------------------------------
+# Arrays are [T][B][heads][D] tensors (fp32 or bf16), any strides with the last dimension contiguous; B = environments * agents, the agents of an
+# environment side by side, and `done` [T][environments] uint8.
+_PRECISION = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _refuse(condition, what):
+    if condition:
+        raise MarlError(f"marl error -3: {what}")
+
+
+def _floats(t, shape, name):
+    """Pointer of an optional contiguous fp32 tensor of this shape."""
+    if t is None:
+        return None
+    _refuse(t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous(), f"{name}: contiguous float32 {list(shape)}")
+    return t.data_ptr()
+
+
+def _view(t, shape, dtype, name):
+    _refuse(t.dtype != dtype or tuple(t.shape) != tuple(shape), f"{name}: {dtype} {list(shape)}")
+    s = t.stride()
+    _refuse(s[3] != 1 and shape[3] > 1, f"{name}: the last dimension is contiguous")
+    return View(t.data_ptr(), s[0], s[1], s[2])
+
+
+def _flags(t, T, B, name):
+    """(pointer, sequences that share a flag) of flags [T][environments]."""
+    if t is None:
+        return None, 1
+    _refuse(t.dtype not in (torch.uint8, torch.bool) or t.dim() != 2 or not t.is_contiguous() or t.shape[0] != T, f"{name}: contiguous uint8 [{T}][environments]")
+    n = t.shape[1]
+    _refuse(n == 0 and B > 0 or n > 0 and B % n != 0, f"{name}: {B} sequences do not share {n} flags")
+    return t.data_ptr(), max(B // n, 1) if n else 1
+
+
+def _attention(q, k, v, flags, scale, name="done"):
+    """(dims, shapes of q / k / v / out, dtype, flags' pointer)"""
+    _refuse(q.dtype not in _PRECISION, "q: float32 or bfloat16")
+    _refuse(q.dim() != 4 or k.dim() != 4 or v.dim() != 4, "q, k, v: [T][B][heads][D]")
+    (T, B, H, Dk), (Hk, Dv) = q.shape, v.shape[2:]
+    ptr, per = _flags(flags, T, B, name)
+    dims = AttentionDims(_PRECISION[q.dtype], T, B, H, Hk, Dk, Dv, per, scale)
+    return dims, ((T, B, H, Dk), (T, B, Hk, Dk), (T, B, Hk, Dv), (T, B, H, Dv)), q.dtype, ptr
+
+
+def linear_attention_workspace(q, k, v, backward=False):
+    n = C.c_int64()
+    dims = _attention(q, k, v, None, 1.0)[0]
+    _check(lib().marl_linear_attention_workspace(C.byref(dims), int(backward), C.byref(n)))
+    return n.value
+
+
+def _workspace(t, need):
+    _refuse(t is not None and t.numel() * t.element_size() < need or t is None and need > 0, f"workspace: {need} bytes")
+    return _ptr(t)
+
+
+def linear_attention(q, k, v, decay, out, workspace=None, state=None, next_state=None, done=None, scale=1.0, stream=None):
+    """out [T][B][Hq][Dv] and next_state [B][Hq][Dk][Dv] of linear attention with decay[h] per head, episodes ending where done is nonzero."""
+    dims, (qs, ks, vs, os), dt, flags = _attention(q, k, v, done, scale)
+    state_shape = (qs[1], qs[2], qs[3], vs[3])
+    need = C.c_int64()
+    _check(lib().marl_linear_attention_workspace(C.byref(dims), 0, C.byref(need)))
+    _check(lib().marl_linear_attention(C.byref(dims), _view(q, qs, dt, "q"), _view(k, ks, dt, "k"), _view(v, vs, dt, "v"),
+                                       _floats(decay, qs[2:3], "decay"), _floats(state, state_shape, "state"), flags,
+                                       _view(out, os, dt, "out"), _floats(next_state, state_shape, "next_state"),
+                                       _workspace(workspace, need.value), _stream(stream)))
+
+
+def linear_attention_backward(q, k, v, decay, dout, dq, dk, dv, workspace=None, state=None, dnext_state=None, dstate=None, done=None, scale=1.0,
+                              stream=None):
+    """Gradients dq, dk, dv and dstate of linear_attention from dout and dnext_state."""
+    dims, (qs, ks, vs, os), dt, flags = _attention(q, k, v, done, scale)
+    state_shape = (qs[1], qs[2], qs[3], vs[3])
+    need = C.c_int64()
+    _check(lib().marl_linear_attention_workspace(C.byref(dims), 1, C.byref(need)))
+    _check(lib().marl_linear_attention_backward(
+        C.byref(dims), _view(q, qs, dt, "q"), _view(k, ks, dt, "k"), _view(v, vs, dt, "v"), _floats(decay, qs[2:3], "decay"),
+        _floats(state, state_shape, "state"), flags, _view(dout, os, dt, "dout"), _floats(dnext_state, state_shape, "dnext_state"),
+        _view(dq, qs, dt, "dq"), _view(dk, ks, dt, "dk"), _view(dv, vs, dt, "dv"), _floats(dstate, state_shape, "dstate"),
+        _workspace(workspace, need.value), _stream(stream)))
+
+
+def linear_attention_step(q, k, v, decay, state, out, next_state=None, done=None, scale=1.0, stream=None):
+    """One step: q [B][Hq][Dk], k, v [B][Hk][D], out [B][Hq][Dv]; done [environments]: of the step before (the state is cleared).  The state is
+    updated in place unless next_state is given."""
+    one = lambda t: t.unsqueeze(0)
+    _refuse(q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or out.dim() != 3, "q, k, v, out: [B][heads][D]")
+    dims, (qs, ks, vs, os), dt, flags = _attention(one(q), one(k), one(v), None if done is None else one(done), scale)
+    state_shape = (qs[1], qs[2], qs[3], vs[3])
+    _check(lib().marl_linear_attention_step(
+        C.byref(dims), _view(one(q), qs, dt, "q"), _view(one(k), ks, dt, "k"), _view(one(v), vs, dt, "v"), _floats(decay, qs[2:3], "decay"),
+        _floats(state, state_shape, "state"), flags, _view(one(out), os, dt, "out"),
+        _floats(state if next_state is None else next_state, state_shape, "next_state"), _stream(stream)))
+
+
+def _rows(t, n, width, dtype, name):
+    _refuse(t.dtype != dtype or tuple(t.shape) != (n, width) or (width > 1 and t.stride(1) != 1), f"{name}: {dtype} [{n}][{width}], rows contiguous")
+    return t.data_ptr(), t.stride(0)
+
+
+def layer_norm(x, weight, bias, out, mean=None, rstd=None, eps=1e-5, stream=None):
+    """out = (x - mean) * rstd * weight + bias over the rows of x [rows][width]; weight, bias, mean, rstd may be None."""
+    _refuse(x.dtype not in _PRECISION or x.dim() != 2, "x: float32 or bfloat16 [rows][width]")
+    n, width = x.shape
+    _check(lib().marl_layer_norm(_PRECISION[x.dtype], n, width, *_rows(x, n, width, x.dtype, "x"), _floats(weight, (width,), "weight"),
+                                 _floats(bias, (width,), "bias"), eps, *_rows(out, n, width, x.dtype, "out"), _floats(mean, (n,), "mean"),
+                                 _floats(rstd, (n,), "rstd"), _stream(stream)))
+
+
+def layer_norm_workspace(rows, width):
+    n = C.c_int64()
+    _check(lib().marl_layer_norm_workspace(int(rows), int(width), C.byref(n)))
+    return n.value
+
+
+def layer_norm_backward(dout, x, weight, mean, rstd, dx, dweight=None, dbias=None, workspace=None, stream=None):
+    """dx, and the column sums dweight, dbias (may be None), from dout and what layer_norm kept."""
+    _refuse(x.dtype not in _PRECISION or x.dim() != 2, "x: float32 or bfloat16 [rows][width]")
+    n, width = x.shape
+    need = layer_norm_workspace(n, width) if dweight is not None or dbias is not None else 0
+    _check(lib().marl_layer_norm_backward(
+        _PRECISION[x.dtype], n, width, *_rows(dout, n, width, x.dtype, "dout"), *_rows(x, n, width, x.dtype, "x"),
+        _floats(weight, (width,), "weight"), _floats(mean, (n,), "mean"), _floats(rstd, (n,), "rstd"), *_rows(dx, n, width, x.dtype, "dx"),
+        _floats(dweight, (width,), "dweight"), _floats(dbias, (width,), "dbias"), _workspace(workspace, need), _stream(stream)))
+
+
+ROTARY_SCALING = {None: 0, "linear": 1, "base": 2, "by_turns": 3}
+
+
+def rotary_table(n_positions, rotary_dim, base=10000.0, scaling=None, factor=1.0, trained_length=0.0, slow=1.0, fast=32.0, amplitude=1.0, stream=None):
+    """[n_positions][rotary_dim] float32: cosines, then sines, of position times frequency, for contexts `factor` times the trained length."""
+    table = torch.empty((n_positions, rotary_dim), dtype=torch.float32, device="cuda")
+    dims = RotaryDims(n_positions, rotary_dim, ROTARY_SCALING[scaling], base, factor, trained_length, slow, fast, amplitude)
+    _check(lib().marl_rotary_table(C.byref(dims), _ptr(table), _stream(stream)))
+    return table
+
+
+def rotary(q, k, table, q_out, k_out, positions=None, first_position=0, interleaved=False, inverse=False, stream=None):
+    """Rotates the first table.shape[1] elements of every head of q and k (k, k_out may be None) by positions [T][environments] int32, or by
+    first_position + t.  The outputs may be the inputs.  inverse: the gradient."""
+    _refuse(q.dtype not in _PRECISION or q.dim() != 4, "q: float32 or bfloat16 [T][B][heads][D]")
+    T, B, H, D = q.shape
+    Hk = 1 if k is None else k.shape[2]
+    _refuse(table.dim() != 2, "table: [positions][rotary_dim]")
+    per = 1
+    if positions is not None:
+        _refuse(positions.dtype != torch.int32 or positions.dim() != 2 or not positions.is_contiguous() or positions.shape[0] != T or
+                (positions.shape[1] == 0 if B else False) or (B % positions.shape[1] if B else 0), f"positions: contiguous int32 [{T}][environments]")
+        per = max(B // positions.shape[1], 1) if B else 1
+    dims = AttentionDims(_PRECISION[q.dtype], T, B, H, Hk, D, D, per, 1.0)
+    none = View(None, 0, 0, 0)
+    _check(lib().marl_rotary(
+        C.byref(dims), _view(q, (T, B, H, D), q.dtype, "q"), none if k is None else _view(k, (T, B, Hk, D), q.dtype, "k"),
+        _floats(table, table.shape, "table"), table.shape[0], table.shape[1], None if positions is None else positions.data_ptr(),
+        int(first_position), int(interleaved), int(inverse), _view(q_out, (T, B, H, D), q.dtype, "q_out"),
+        none if k is None else _view(k_out, (T, B, Hk, D), q.dtype, "k_out"), _stream(stream)))
 
 
 KERNEL_CLASSES = {"gemm_nn": 0, "gemm_nt": 1, "gemm_tn": 2, "env_step": 3, "gae": 4, "fused_train": 5, "rollout": 6}

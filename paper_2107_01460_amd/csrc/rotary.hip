@@ -1,0 +1,230 @@
+// Rotary positions: the table of cosines and sines, and the rotation of queries and keys in one launch.  Bound by memory: every element in and
+// out once; a step's table row is shared by its heads and comes from a cache.
+#include "common.h"
+
+namespace marl {
+namespace {
+
+// ---- table -----------------------------------------------------------------------------------------------------------------------
+// In 64 bits: an angle of p radians has an error of p * 2^-24 in 32.
+__global__ void __launch_bounds__(256) rotary_table_kernel(marl_rotary_dims d, float* __restrict__ table) {
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int half = d.rotary_dim / 2;
+  if (at >= (int64_t)d.n_positions * half) return;
+  const int64_t position = at / half;
+  const int i = (int)(at % half);
+  const double R = d.rotary_dim;
+  double base = d.base;
+  if (d.scaling == 2) base *= pow((double)d.factor, R / (R - 2.0));
+  double f = pow(base, -2.0 * i / R);
+  if (d.scaling == 1) f /= d.factor;
+  if (d.scaling == 3) {
+    const double turns = d.trained_length * f / 6.283185307179586476925;
+    double m = (turns - d.slow) / ((double)d.fast - d.slow);
+    m = m < 0.0 ? 0.0 : m > 1.0 ? 1.0 : m;
+    f = m * f + (1.0 - m) * f / d.factor;
+  }
+  double sine, cosine;
+  sincos((double)position * f, &sine, &cosine);
+  table[position * d.rotary_dim + i] = (float)(cosine * d.amplitude);
+  table[position * d.rotary_dim + half + i] = (float)(sine * d.amplitude);
+}
+
+// ---- rotation ----------------------------------------------------------------------------------------------------------------------
+struct RotaryArray {
+  const char* in;
+  char* out;
+  int64_t in_step, in_seq, in_head, out_step, out_seq, out_head;  // elements
+};
+struct RotaryArgs {
+  RotaryArray a[2];     // q, k
+  const float* table;
+  const int32_t* positions;
+  int32_t n_positions, rotary, first, inverse;
+  uint32_t B, heads[2], seqs_per_flag, n_flags;
+  uint32_t dim, items;  // items of a head: pairs of vectors, then vectors that are copied
+  uint32_t pair_items;
+  int64_t tokens;
+};
+
+// One item: E elements and their partners E (half layout), or E consecutive ones that hold E / 2 pairs (interleaved, E > 1); E = 1: one pair, or one
+// element that is copied.
+template <class T, int E>
+struct Piece {
+  T v[E];
+};
+template <class T, int E>
+__device__ __forceinline__ Piece<T, E> get(const T* p) {
+  Piece<T, E> r;
+  if constexpr (E == 1) {
+    r.v[0] = *p;
+  } else {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    __builtin_memcpy(&r, &u, 16);
+  }
+  return r;
+}
+template <class T, int E>
+__device__ __forceinline__ void put(T* p, const Piece<T, E>& r) {
+  if constexpr (E == 1) {
+    *p = r.v[0];
+  } else {
+    uint4 u;
+    __builtin_memcpy(&u, &r, 16);
+    *reinterpret_cast<uint4*>(p) = u;
+  }
+}
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(bf16_t v) { return from_bf16(v); }
+template <class T>
+__device__ __forceinline__ T narrow(float v) {
+  if constexpr (sizeof(T) == 4) return v;
+  else return to_bf16(v);
+}
+
+template <class T, int E, bool INTERLEAVED>
+__global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs args) {
+  // items in order: token, head (of q, then of k), item of the head; a workgroup's first token and the rest by 32-bit division
+  const uint32_t per_token = (args.heads[0] + args.heads[1]) * args.items;
+  const int64_t first = (int64_t)blockIdx.x * 256;
+  const int64_t token0 = first / per_token;
+  const uint32_t at = (uint32_t)(first - token0 * per_token) + threadIdx.x;
+  const uint32_t more = at / per_token, in_token = at - more * per_token;
+  if (token0 + more >= args.tokens) return;
+  const int64_t t0 = token0 / args.B;
+  uint32_t b = (uint32_t)(token0 - t0 * args.B) + more;
+  const uint32_t over = b / args.B;
+  b -= over * args.B;
+  const int64_t t = t0 + over;
+  uint32_t head = in_token / args.items;
+  const uint32_t item = in_token - head * args.items;
+  const bool second = head >= args.heads[0];
+  if (second) head -= args.heads[0];
+  const RotaryArray& a = args.a[second];
+  const T* in = reinterpret_cast<const T*>(a.in) + t * a.in_step + b * a.in_seq + head * a.in_head;
+  T* out = reinterpret_cast<T*>(a.out) + t * a.out_step + b * a.out_seq + head * a.out_head;
+  const int R = args.rotary, half = R / 2;
+  if (item >= args.pair_items) {  // behind the rotated part
+    const uint32_t c = INTERLEAVED && E > 1 ? item * E : R + (item - args.pair_items) * E;
+    put<T, E>(out + c, get<T, E>(in + c));
+    return;
+  }
+  const int64_t position = args.positions != nullptr ? args.positions[t * args.n_flags + b / args.seqs_per_flag] : args.first + t;
+  const bool known = position >= 0 && position < args.n_positions;
+  const float* row = args.table + (known ? position : 0) * R;
+  auto turn = [&](float x1, float x2, int i, float& y1, float& y2) {
+    float c = row[i], s = row[half + i];
+    if (args.inverse) s = -s;
+    if (!known) c = s = __builtin_nanf("");
+    y1 = x1 * c - x2 * s;
+    y2 = x1 * s + x2 * c;
+  };
+  if constexpr (INTERLEAVED && E > 1) {
+    const uint32_t c = item * E;
+    Piece<T, E> p = get<T, E>(in + c);
+#pragma unroll
+    for (int k = 0; k < E; k += 2) {
+      if ((int)c + k >= R) break;
+      float y1, y2;
+      turn(widen(p.v[k]), widen(p.v[k + 1]), ((int)c + k) / 2, y1, y2);
+      p.v[k] = narrow<T>(y1);
+      p.v[k + 1] = narrow<T>(y2);
+    }
+    put<T, E>(out + c, p);
+  } else {
+    const uint32_t c1 = INTERLEAVED ? 2 * item : item * E, c2 = INTERLEAVED ? c1 + 1 : c1 + half;
+    Piece<T, E> p1 = get<T, E>(in + c1), p2 = get<T, E>(in + c2);
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      float y1, y2;
+      turn(widen(p1.v[k]), widen(p2.v[k]), (int)item * E + k, y1, y2);
+      p1.v[k] = narrow<T>(y1);
+      p2.v[k] = narrow<T>(y2);
+    }
+    put<T, E>(out + c1, p1);
+    put<T, E>(out + c2, p2);
+  }
+}
+
+template <class T, int E>
+int32_t rotate(RotaryArgs a, bool interleaved, hipStream_t s) {
+  a.pair_items = interleaved && E > 1 ? ((uint32_t)a.rotary + E - 1) / E : (uint32_t)a.rotary / 2 / E;
+  a.items = interleaved && E > 1 ? a.dim / E : a.pair_items + (a.dim - a.rotary) / E;
+  const int64_t total = a.tokens * (a.heads[0] + a.heads[1]) * a.items, blocks = (total + 255) / 256;
+  if (blocks >= ((int64_t)1 << 31)) return MARL_E_SIZE;
+  if (interleaved) hipLaunchKernelGGL((rotary_kernel<T, E, true>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((rotary_kernel<T, E, false>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+  return launch_status();
+}
+
+}  // namespace
+}  // namespace marl
+
+using namespace marl;
+
+extern "C" {
+
+int32_t marl_rotary_table(const marl_rotary_dims* dims, float* table, void* stream) {
+  if (dims == nullptr) return MARL_E_NULL;
+  const marl_rotary_dims& d = *dims;
+  if (d.n_positions < 1 || d.rotary_dim < 2) return MARL_E_SIZE;
+  if (d.rotary_dim % 2 != 0 || d.scaling < 0 || d.scaling > 3) return MARL_E_CONFIG;
+  if (!(d.base > 0.f) || (d.scaling != 0 && !(d.factor > 0.f)) || (d.scaling == 2 && d.rotary_dim < 4)) return MARL_E_CONFIG;
+  if (d.scaling == 3 && (!(d.trained_length > 0.f) || !(d.fast > d.slow))) return MARL_E_CONFIG;
+  MARL_REQUIRE_PTR(table);
+  const int64_t blocks = ((int64_t)d.n_positions * (d.rotary_dim / 2) + 255) / 256;
+  if (blocks >= ((int64_t)1 << 31)) return MARL_E_SIZE;
+  hipLaunchKernelGGL(rotary_table_kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, d, table);
+  return launch_status();
+}
+
+int32_t marl_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, const float* table, int32_t n_positions,
+                    int32_t rotary_dim, const int32_t* positions, int32_t first_position, int32_t interleaved,
+                    int32_t inverse, marl_view q_out, marl_view k_out, void* stream) {
+  if (dims == nullptr) return MARL_E_NULL;
+  const marl_attention_dims& d = *dims;
+  if (d.precision != 0 && d.precision != 1) return MARL_E_CONFIG;
+  if (d.n_steps < 0 || d.n_seqs < 0 || n_positions < 1) return MARL_E_SIZE;
+  if (d.dim_k < 1 || d.dim_k > 1024 || rotary_dim < 2 || rotary_dim > d.dim_k) return MARL_E_SIZE;
+  if (rotary_dim % 2 != 0 || interleaved < 0 || interleaved > 1 || inverse < 0 || inverse > 1) return MARL_E_CONFIG;
+  if (d.n_heads < 1 || d.n_heads > (1 << 15) || (k.data != nullptr && (d.n_kv_heads < 1 || d.n_kv_heads > (1 << 15)))) return MARL_E_CONFIG;
+  if (d.seqs_per_flag < 1 || d.n_seqs % d.seqs_per_flag != 0) return MARL_E_CONFIG;
+  RotaryArgs a{};
+  a.tokens = (int64_t)d.n_steps * d.n_seqs;
+  if (a.tokens == 0) return MARL_OK;
+  const uintptr_t odd = d.precision == 0 ? 3u : 1u;
+  const int elem = d.precision == 0 ? 4 : 2;
+  const int n = k.data != nullptr ? 2 : 1;
+  const marl_view in[2] = {q, k}, out[2] = {q_out, k_out};
+  uintptr_t low = 0;
+  for (int u = 0; u < n; ++u) {
+    if (in[u].data == nullptr || out[u].data == nullptr) return MARL_E_NULL;
+    const uintptr_t pi = reinterpret_cast<uintptr_t>(in[u].data), po = reinterpret_cast<uintptr_t>(out[u].data);
+    if (((pi | po) & odd) != 0) return MARL_E_ALIGN;
+    a.a[u] = {static_cast<const char*>(in[u].data), static_cast<char*>(out[u].data), in[u].step, in[u].seq, in[u].head, out[u].step, out[u].seq,
+              out[u].head};
+    for (int64_t x : {in[u].step, in[u].seq, in[u].head, out[u].step, out[u].seq, out[u].head}) low |= (uintptr_t)(x * elem);
+    low |= pi | po;
+  }
+  MARL_REQUIRE_PTR(table);
+  if ((reinterpret_cast<uintptr_t>(positions) & 3u) != 0) return MARL_E_ALIGN;
+  a.table = table;
+  a.positions = positions;
+  a.n_positions = n_positions;
+  a.rotary = rotary_dim;
+  a.first = first_position;
+  a.inverse = inverse;
+  a.B = (uint32_t)d.n_seqs;
+  a.heads[0] = (uint32_t)d.n_heads;
+  a.heads[1] = n == 2 ? (uint32_t)d.n_kv_heads : 0;
+  a.seqs_per_flag = (uint32_t)d.seqs_per_flag;
+  a.n_flags = (uint32_t)(d.n_seqs / d.seqs_per_flag);
+  a.dim = (uint32_t)d.dim_k;
+  const int E = 16 / elem;
+  const bool wide = (low & 15u) == 0 && d.dim_k % E == 0 && (interleaved ? true : rotary_dim / 2 % E == 0);
+  hipStream_t s = (hipStream_t)stream;
+  if (d.precision == 0) return wide ? rotate<float, 4>(a, interleaved != 0, s) : rotate<float, 1>(a, interleaved != 0, s);
+  return wide ? rotate<bf16_t, 8>(a, interleaved != 0, s) : rotate<bf16_t, 1>(a, interleaved != 0, s);
+}
+
+}  // extern "C"
