@@ -6,17 +6,18 @@
 //     out: (x, y, z) = (q, k, v);   dq: (dout, v, k), the state transposed;   dv: (k, q, dout) and dk: (v, dout, q) in reverse,
 // because dq_i = scale S_i dout_i with the same S, and R_j = scale q_j dout_j^T + g R_{j+1} gives dv_j = R_j^T k_j, dk_j = R_j v_j.
 //
-// One wavefront takes one head of one sequence (or a slice of its z columns) through time, sixteen steps at once, on the matrix cores, with S
-// in accumulator registers: per 16 steps four small products, scores y x^T, x S, scores z and y^T z.  Transposed throughout (out^T = z^T
-// scores^T), the accumulator layout of a product -- lane = column, four rows in registers -- is the operand layout of the next, so that neither
-// scores nor S go through LDS; y and z do, because the last two products contract over time.
+// A wavefront takes up to 32 z columns of one head of one sequence through time, a tile of 16 (fp32) or 32 steps (bf16) at once, on the matrix
+// cores, with its columns of S in accumulator registers: four small products a tile, scores y x^T, x S, scores z and y^T z.  Transposed
+// throughout (out^T = z^T scores^T), the accumulator layout of a product -- lane = column, four rows in registers -- is the operand layout of
+// the next, so that neither scores nor S go through LDS.
+// A workgroup of up to four wavefronts takes neighbouring heads (and all slices of their columns): a step's rows of neighbouring heads are one run of
+// memory, and steps are far apart in it (megabytes, when there are many sequences), so its wavefronts fetch and store whole runs together and hand
+// them to each other through LDS; the next tile is on its way in registers meanwhile.
 #pragma once
 #include "split_bf16.h"
 
 namespace marl {
 
-constexpr int kTile = 16;          // steps that a wavefront takes at once
-constexpr int kMaxWaves = 4;       // of a workgroup; they share nothing
 constexpr int kMaxRoles = 3;
 
 struct ScanArray {
@@ -47,11 +48,9 @@ struct ScanArgs {
   const uint8_t* done;
   float* carry;          // states only: [sequence, head][stretch] factor from a stretch's first state to its last
   int32_t T, B;
-  uint32_t n_roles, H, seqs_per_flag;
-  uint32_t slices;       // of the z columns, one wavefront each
-  uint32_t n_stretches;
-  int32_t stretch;       // steps of a stretch, a multiple of kTile
-  uint32_t units;        // B * H * slices
+  uint32_t n_roles, H, seqs_per_flag, n_stretches;
+  int32_t stretch;       // steps of a stretch, whole tiles
+  uint32_t pairs;        // B * H
 };
 
 template <class T>
@@ -59,27 +58,24 @@ struct ScanTraits;
 template <>
 struct ScanTraits<float> {
   typedef floatx4 Frag;                     // four elements along a contraction
-  static constexpr int kPad = 4;            // of an LDS row, elements
+  static constexpr int kSub = 1;            // blocks of sixteen steps in a tile: the fewest products
 };
 template <>
 struct ScanTraits<bf16_t> {
   typedef shortx4 Frag;
-  static constexpr int kPad = 8;
+  static constexpr int kSub = 2;            // products contract over 32 steps, and S is split into parts once for 32
 };
-// Feature of element e of lane group g in tile a of N tiles of sixteen features.  bf16: two tiles deal a lane eight consecutive ones, 16 bytes.
+// Feature of element e of lane group g in tile a of N tiles of sixteen x and y features.  bf16: two tiles deal a lane eight consecutive ones, 16 bytes.
 template <class T, int N>
 __device__ __forceinline__ int feat(int a, int g, int e) {
   return sizeof(T) == 2 && N % 2 == 0 ? 32 * (a / 2) + 8 * g + 4 * (a & 1) + e : 16 * a + 4 * g + e;
 }
 
-__device__ __forceinline__ float ipow(float g, int m) {  // g^m, 0^0 = 1
-  float r = 1.f;
-  while (m != 0) {
+__device__ __forceinline__ float ipow(float base, int m) {  // base^m rounded once, 0^0 = 1
+  double r = 1.0, g = base;
+  for (; m != 0; m >>= 1, g *= g)
     if (m & 1) r *= g;
-    g *= g;
-    m >>= 1;
-  }
-  return r;
+  return (float)r;
 }
 
 // ---- products of 16 x 16 outputs; the contraction index of element e of lane group g is the same on both sides -----------------------
@@ -89,6 +85,12 @@ __device__ __forceinline__ floatx4 mma(floatx4 a, floatx4 b, floatx4 c) {
   return c;
 }
 __device__ __forceinline__ floatx4 mma(shortx4 a, shortx4 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ shortx8 both(shortx4 a, shortx4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+// over two tiles' contraction: one instruction of twice the length in bf16
+__device__ __forceinline__ floatx4 mma2(floatx4 a0, floatx4 a1, floatx4 b0, floatx4 b1, floatx4 c) { return mma(a1, b1, mma(a0, b0, c)); }
+__device__ __forceinline__ floatx4 mma2(shortx4 a0, shortx4 a1, shortx4 b0, shortx4 b1, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, both(a0, a1)), __builtin_bit_cast(bf16x8, both(b0, b1)), c, 0, 0, 0);
+}
 
 __device__ __forceinline__ shortx4 pack4(floatx4 v) {
   const uint2 u = make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]));
@@ -98,163 +100,44 @@ __device__ __forceinline__ floatx4 unpack4(shortx4 s) {
   const uint2 u = __builtin_bit_cast(uint2, s);
   return floatx4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u)};
 }
-// fp32 values times exact operands.  bf16: the values in two parts (relative error 2^-16: what the scores and the state are rounded to where
-// the result is an output of eight bits) or in three (2^-24: where it is a state that goes on).
-__device__ __forceinline__ floatx4 mma_two(floatx4 v, floatx4 b, floatx4 c) { return mma(v, b, c); }
-__device__ __forceinline__ floatx4 mma_two(floatx4 v, shortx4 b, floatx4 c) {
-  const shortx4 h = pack4(v);
-  c = mma(pack4(v - unpack4(h)), b, c);
-  return mma(h, b, c);
-}
-struct Weighed {
-  shortx4 h, m, l;
+// fp32 values as operands beside exact ones.  bf16: as a sum of two parts (relative error 2^-16: scores and S, where the result is an output of
+// eight bits) or of three (2^-24: what enters a state that goes on).
+template <class T, int P>
+struct Parts {
+  typename ScanTraits<T>::Frag p[sizeof(T) == 4 ? 1 : P];
 };
-__device__ __forceinline__ floatx4 weigh_parts(floatx4 y, floatx4 w) { return y * w; }
-__device__ __forceinline__ Weighed weigh_parts(shortx4 y, floatx4 w) {
-  floatx4 v = unpack4(y) * w;
-  Weighed p;
-  p.h = pack4(v);
-  v -= unpack4(p.h);
-  p.m = pack4(v);
-  v -= unpack4(p.m);
-  p.l = pack4(v);
-  return p;
-}
-__device__ __forceinline__ floatx4 mma(const Weighed& a, shortx4 b, floatx4 c) {
-  c = mma(a.l, b, c);
-  c = mma(a.m, b, c);
-  return mma(a.h, b, c);
-}
-
-// ---- rows of sixteen steps: lane (i = lane % 16, g = lane / 16) holds features feat(a, g, 0..3) of step i --------------------------------
-template <class T, int N>
-struct Rows {
-  typename ScanTraits<T>::Frag f[N];
-};
-__device__ __forceinline__ float load_one(const float* p) { return *p; }
-__device__ __forceinline__ short load_one(const bf16_t* p) { return (short)*p; }
-
-// row: of the lane's step (clamped to a valid one), n: valid steps; column 0 of the slice at `first`
-template <class T, int N>
-__device__ __forceinline__ void load_rows(Rows<T, N>& r, const ScanArray& a, const char* row, int first, bool valid, int g) {
-  constexpr int kRun = (sizeof(T) == 2 && N % 2 == 0) ? 2 : 1;  // tiles a 16-byte access covers
-  if (a.wide) {
-#pragma unroll
-    for (int t = 0; t < N; t += kRun) {
-      const int col = first + feat<T, N>(t, g, 0);
-      const bool in = valid && col < a.dim;
-      const char* p = row + (in ? col * (int)sizeof(T) : 0);
-      if constexpr (sizeof(T) == 4) {
-        const floatx4 v = *reinterpret_cast<const floatx4*>(p);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r.f[t][e] = in ? v[e] : 0.f;
-      } else if constexpr (kRun == 2) {
-        uint4 v = *reinterpret_cast<const uint4*>(p);
-        v.x = in ? v.x : 0u; v.y = in ? v.y : 0u; v.z = in ? v.z : 0u; v.w = in ? v.w : 0u;
-        r.f[t] = __builtin_bit_cast(shortx4, make_uint2(v.x, v.y));
-        r.f[t + 1] = __builtin_bit_cast(shortx4, make_uint2(v.z, v.w));
-      } else {
-        const uint2 v = *reinterpret_cast<const uint2*>(p);
-        r.f[t] = __builtin_bit_cast(shortx4, make_uint2(in ? v.x : 0u, in ? v.y : 0u));
-      }
-    }
+template <class T, int P>
+__device__ __forceinline__ Parts<T, P> parts_of(floatx4 v) {
+  Parts<T, P> r;
+  if constexpr (sizeof(T) == 4) {
+    r.p[0] = v;
   } else {
 #pragma unroll
-    for (int t = 0; t < N; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int col = first + feat<T, N>(t, g, e);
-        const bool in = valid && col < a.dim;
-        const auto v = load_one(reinterpret_cast<const T*>(row) + (in ? col : 0));
-        r.f[t][e] = in ? v : 0;
-      }
+    for (int k = 0; k < P; ++k) {
+      r.p[k] = pack4(v);
+      if (k + 1 < P) v -= unpack4(r.p[k]);
+    }
   }
-}
-// Is there an infinity or a NaN among them?  (exponents of ones; bit 31 or 15 of the result)
-__device__ __forceinline__ uint32_t not_finite(floatx4 v) {
-  uint32_t r = 0;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) r |= (__float_as_uint(v[e]) & 0x7f800000u) + 0x00800000u;
   return r;
 }
-__device__ __forceinline__ uint32_t not_finite(shortx4 v) {
-  const uint2 u = __builtin_bit_cast(uint2, v);
-  return ((u.x & 0x7f807f80u) + 0x00800080u) | ((u.y & 0x7f807f80u) + 0x00800080u);
-}
+__device__ __forceinline__ floatx4 widen4(floatx4 v) { return v; }
+__device__ __forceinline__ floatx4 widen4(shortx4 v) { return unpack4(v); }
 
-template <class T, int N>
-__device__ __forceinline__ void rows_to_lds(T* lds, const Rows<T, N>& r, int i, int g) {
-  constexpr int kPitch = 16 * N + ScanTraits<T>::kPad;
-  if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int t = 0; t < N; ++t) *reinterpret_cast<floatx4*>(lds + i * kPitch + feat<T, N>(t, g, 0)) = r.f[t];
-  } else if constexpr (N % 2 == 0) {
-#pragma unroll
-    for (int t = 0; t < N; t += 2) {
-      const shortx8 v = __builtin_shufflevector(r.f[t], r.f[t + 1], 0, 1, 2, 3, 4, 5, 6, 7);
-      *reinterpret_cast<shortx8*>(lds + i * kPitch + feat<T, N>(t, g, 0)) = v;
-    }
-  } else {
-#pragma unroll
-    for (int t = 0; t < N; ++t) *reinterpret_cast<shortx4*>(lds + i * kPitch + feat<T, N>(t, g, 0)) = r.f[t];
-  }
-}
-// Columns: lane m = lane % 16 of tile t gets feature feat(t, m / 4, m % 4) at steps 4 g .. 4 g + 3
-template <int N>
-__device__ __forceinline__ floatx4 column(const float* lds, int t, int i, int g) {
-  constexpr int kPitch = 16 * N + ScanTraits<float>::kPad;
-  floatx4 v;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = lds[(4 * g + e) * kPitch + 16 * t + i];
-  return v;
-}
-template <int N>
-__device__ __forceinline__ shortx4 column(const bf16_t* lds, int t, int i, int g) {
-  constexpr int kPitch = 16 * N + ScanTraits<bf16_t>::kPad;
-  typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
-  const int at = feat<bf16_t, N>(t, i & 3, 0);
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(lds + (4 * g + (i >> 2)) * kPitch + at));
-}
-
-// Between LDS writes and reads of one wavefront's own part: its LDS accesses take effect in order, the compiler has to keep it.
-__device__ __forceinline__ void wave_lds_order() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
-// Powers of the decay that a tile of n steps needs, as lane (i, g) uses them: row i on the x side, rows 4 g + e on the y side
-struct TilePowers {
-  float to_i;        // from the tile's first state to step i: g^(i+1); reverse: from its last, g^(n-1-i)
-  float whole;       // g^n
-  floatx4 from_j;    // from step j to the tile's other end: g^(n-1-j), reverse g^(j+1)
-};
-__device__ __forceinline__ TilePowers tile_powers(float decay, int n, bool reverse, int i, int g) {
-  TilePowers p;
-  p.to_i = reverse ? (i < n ? ipow(decay, n - 1 - i) : 0.f) : ipow(decay, i + 1);
-  p.whole = ipow(decay, n);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int j = 4 * g + e;
-    p.from_j[e] = j >= n ? 0.f : reverse ? ipow(decay, j + 1) : ipow(decay, n - 1 - j);
-  }
-  return p;
-}
-
-// One tile the slow way, step by step from memory, where it holds infinities or NaNs: a matrix product multiplies masked places by zero, which
-// makes a NaN of them, and would carry them into other steps' and other episodes' outputs.  (noinline would put S into memory.)
+// One step after another from memory, where there are infinities or NaNs: a matrix product multiplies masked places by zero, which makes a NaN of
+// them, and would carry them into other steps' and other episodes' outputs.  n steps from t0 on, S before them (reverse: behind them) on entry.
 template <class T, int NK, int NV, bool STATE_ONLY>
-__device__ void scan_tile_slow(floatx4 (&S)[NK][NV], const ScanRole& r, const char* xb, const char* yb, const char* zb, char* ob, int t0, int n,
-                               int slice0, float decay, uint32_t ends, int i, int g) {
+__device__ void scan_slow(floatx4 (&S)[NK][NV], const ScanRole& r, const char* xb, const char* yb, const char* zb, char* ob, int t0, int n, int slice0,
+                          float decay, const uint8_t* done, int64_t n_flags, int i, int g) {
   for (int s = 0; s < n; ++s) {
-    const int at = r.reverse ? n - 1 - s : s, t = t0 + at;
-    const bool end = (ends >> at) & 1u;
-    const T* y = reinterpret_cast<const T*>(yb + (int64_t)t * r.y.step);
-    const T* z = reinterpret_cast<const T*>(zb + (int64_t)t * r.z.step);
-    const T* x = STATE_ONLY ? nullptr : reinterpret_cast<const T*>(xb + (int64_t)t * r.x.step);
+    const int64_t t = t0 + (r.reverse ? n - 1 - s : s);
+    const bool end = done != nullptr && done[t * n_flags] != 0;
+    const T* y = reinterpret_cast<const T*>(yb + t * r.y.step);
+    const T* z = reinterpret_cast<const T*>(zb + t * r.z.step);
+    const T* x = STATE_ONLY ? nullptr : reinterpret_cast<const T*>(xb + t * r.x.step);
     float zv[NV], o[NV];
 #pragma unroll
     for (int b = 0; b < NV; ++b) {
-      const int c = slice0 + feat<T, NV>(b, i >> 2, i & 3);
+      const int c = slice0 + 16 * b + i;
       zv[b] = c < r.z.dim ? r.update * load_act(z, c) : 0.f;
       o[b] = 0.f;
     }
@@ -282,9 +165,9 @@ __device__ void scan_tile_slow(floatx4 (&S)[NK][NV], const ScanRole& r, const ch
         float v = o[b];
         v += __shfl_xor(v, 16);
         v += __shfl_xor(v, 32);
-        const int c = slice0 + feat<T, NV>(b, i >> 2, i & 3);
+        const int c = slice0 + 16 * b + i;
         if (g == 0 && c < r.z.dim) {
-          char* p = ob + (int64_t)t * r.out.step;
+          char* p = ob + t * r.out.step;
           v *= r.inter;
           if (r.out_f32 || sizeof(T) == 4)
             reinterpret_cast<float*>(p)[c] = v;
@@ -296,42 +179,163 @@ __device__ void scan_tile_slow(floatx4 (&S)[NK][NV], const ScanRole& r, const ch
   }
 }
 
-template <class T, int NK, int NV, bool STATE_ONLY>
-__global__ void __launch_bounds__(64 * kMaxWaves, 2) scan_kernel(const ScanArgs args) {
+// A copy that the compiler takes for a new value: what a rare branch works out from it is worked out there, not kept in registers across the loop
+// (a hundred of them in all, and spilled).
+__device__ __forceinline__ int fresh(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// ---- tiles in LDS: [sequence, head][step][pieces of 16 bytes], a row's pieces exchanged so that sixteen rows' equal pieces lie in different banks --------
+template <int PIECES>
+__device__ __forceinline__ int swizzle(int row) {
+  return PIECES % 16 == 0 ? row & 15 : PIECES % 8 == 0 ? row >> 1 & 7 : PIECES % 4 == 0 ? row >> 2 & 3 : row >> 3 & 1;
+}
+// Rows: lane (i, g) gets features feat(a, g, 0..3) of step `row`
+template <class T, int N>
+struct Rows {
+  typename ScanTraits<T>::Frag f[N];
+};
+template <class T, int N>
+__device__ __forceinline__ void rows_of(Rows<T, N>& r, const char* tile, int row, int g) {
+  constexpr int kPieces = N * (int)sizeof(T);
+  const char* p = tile + row * kPieces * 16;
+  const int swz = swizzle<kPieces>(row);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int t = 0; t < N; ++t) r.f[t] = *reinterpret_cast<const floatx4*>(p + ((4 * t + g) ^ swz) * 16);
+  } else if constexpr (N % 2 == 0) {
+#pragma unroll
+    for (int t = 0; t < N; t += 2) {
+      const shortx8 v = *reinterpret_cast<const shortx8*>(p + ((2 * t + g) ^ swz) * 16);
+      r.f[t] = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+      r.f[t + 1] = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < N; ++t) r.f[t] = *reinterpret_cast<const shortx4*>(p + ((2 * t + (g >> 1)) ^ swz) * 16 + 8 * (g & 1));
+  }
+}
+// Columns: lane (i, g) gets one feature at steps 4 g .. 4 g + 3 of the block of sixteen steps that begins at `row`.  first: of the sixteen features,
+// run: how far apart fours of them lie (lanes i = 4 c .. 4 c + 3 take first + run c .. + 3)
+template <class T, int PIECES>
+__device__ __forceinline__ floatx4 column(const float* tile, int row, int first, int run, int i, int g) {
+  const int f = first + run * (i >> 2) + (i & 3);
+  floatx4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int at = row + 4 * g + e;
+    v[e] = tile[at * PIECES * 4 + (((f >> 2) ^ swizzle<PIECES>(at)) << 2) + (f & 3)];
+  }
+  return v;
+}
+template <class T, int PIECES>
+__device__ __forceinline__ shortx4 column(const bf16_t* tile, int row, int first, int run, int i, int g) {
+  typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
+  const int at = row + 4 * g + (i >> 2), f = first + run * (i & 3);  // (the transposing read: a lane names four features of one step)
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(tile + at * PIECES * 8 + (((f >> 3) ^ swizzle<PIECES>(at)) << 3) + (f & 7)));
+}
+
+// ---- a workgroup's share of an array's tile: SLOTS pieces a thread, piece fastest, then head, then step ------------------------------------
+template <class T, int PIECES, int P, int TILE, int THREADS, bool WIDE>
+struct Stage {
+  static constexpr int kAll = PIECES * P * TILE, kSlots = (kAll + THREADS - 1) / THREADS;
+  const char* from[kSlots];  // of the piece in the tile that is fetched next
+  uint4 v[kSlots];
+  static __device__ __forceinline__ int index(int s, int tid) { return min(s * THREADS + tid, kAll - 1); }
+  static __device__ __forceinline__ int piece(int q) { return q % PIECES; }
+  static __device__ __forceinline__ int pair(int q) { return q / PIECES % P; }
+  static __device__ __forceinline__ int row(int q) { return q / (PIECES * P); }
+  // A piece past the array's columns: its loads go to column 0, zeros go to LDS
+  template <class Base>
+  __device__ __forceinline__ void begin(const ScanArray& a, int t0, int tid, Base base) {
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+      const int q = index(s, tid);
+      from[s] = base(a, pair(q)) + (int64_t)(t0 + row(q)) * a.step + (piece(q) * (int)(16 / sizeof(T)) < a.dim ? piece(q) * 16 : 0);
+    }
+  }
+  __device__ __forceinline__ void request(const ScanArray& a, int n, int64_t next, int tid) {  // n: steps in the tile; next: bytes to the tile after
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+      const char* p = from[s];
+      if (n < TILE) {
+        const int at = row(index(s, fresh(tid)));
+        p -= at < n ? 0 : (at - n + 1) * a.step;
+      }
+      if constexpr (WIDE) {
+        v[s] = *reinterpret_cast<const uint4*>(p);
+      } else {
+        constexpr int E = 16 / sizeof(T);
+        const int in = a.dim - piece(index(s, fresh(tid))) * E;  // elements of the piece that there are
+        T e[E];
+#pragma unroll
+        for (int k = 0; k < E; ++k) e[k] = reinterpret_cast<const T*>(p)[k < in ? k : 0];
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+          if (k >= in) e[k] = 0;
+        __builtin_memcpy(&v[s], e, 16);
+      }
+      from[s] += next;
+    }
+  }
+  __device__ __forceinline__ void to_lds(char* tile, const ScanArray& a, int n, int tid) {
+    const bool some = n < TILE || PIECES * (int)(16 / sizeof(T)) > a.dim;
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+      const int q = index(s, tid), at = row(q);
+      if (some) {
+        const int p = index(s, fresh(tid));
+        if (row(p) >= n || piece(p) * (int)(16 / sizeof(T)) >= a.dim) v[s] = make_uint4(0, 0, 0, 0);
+      }
+      if (kAll % THREADS == 0 || s * THREADS + tid < kAll)
+        *reinterpret_cast<uint4*>(tile + ((pair(q) * TILE + at) * PIECES + (piece(q) ^ swizzle<PIECES>(at))) * 16) = v[s];
+    }
+  }
+};
+
+template <int SL>
+constexpr int scan_pairs() { return SL == 1 ? 4 : SL == 2 ? 2 : 1; }  // (sequence, head) pairs of a workgroup
+
+template <class T, int NK, int NV, int SL, bool STATE_ONLY, bool WIDE>
+__global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 ? 2 : 3) scan_kernel(const ScanArgs args) {
   typedef ScanTraits<T> Tr;
   typedef typename Tr::Frag Frag;
-  constexpr int kPitchY = 16 * NK + Tr::kPad, kPitchZ = 16 * NV + Tr::kPad;
-  constexpr int kWaveLds = kTile * (kPitchY + kPitchZ);
-  __shared__ __align__(16) T lds_all[kMaxWaves * kWaveLds];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
-  // neighbours in a contiguous run on one XCD: first the roles, which read the same arrays, then the stretches, then the units
+  constexpr int U = Tr::kSub, kTile = 16 * U, P = scan_pairs<SL>(), kThreads = 64 * SL * P, E = 16 / sizeof(T);
+  constexpr int kPiecesX = NK * (int)sizeof(T), kPiecesZ = SL * NV * (int)sizeof(T);
+  typedef Stage<T, kPiecesX, P, kTile, kThreads, WIDE> StageX;
+  typedef Stage<T, kPiecesZ, P, kTile, kThreads, WIDE> StageZ;
+  constexpr int kBytesX = StageX::kAll * 16, kBytesZ = StageZ::kAll * 16;
+  __shared__ __align__(16) char lds_x[STATE_ONLY ? 16 : kBytesX];
+  __shared__ __align__(16) char lds_y[kBytesX];
+  __shared__ __align__(16) char lds_z[kBytesZ];
+  __shared__ __align__(16) char lds_o[STATE_ONLY ? 16 : kBytesZ];
+  __shared__ uint32_t lds_left[SL * P];  // wavefronts that have left the common way
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
+  // neighbours in a contiguous run on one XCD: first the roles, which read the same arrays, then the stretches, then the pairs
   uint32_t at = xcd_remap(blockIdx.x, gridDim.x);
   const uint32_t role_index = at % args.n_roles;
   at /= args.n_roles;
   const int stretch = (int)(at % args.n_stretches);
-  const uint32_t unit = at / args.n_stretches * (blockDim.x >> 6) + wave;
-  if (unit >= args.units) return;
+  const uint32_t pair0 = at / args.n_stretches * P;
   const ScanRole& r = args.role[role_index];
-  const int slice0 = (int)(unit % args.slices) * 16 * NV;
-  const int64_t pair = unit / args.slices;  // (sequence, query head)
+  const int local = wave / SL, slice0 = wave % SL * 16 * NV;
+  const bool active = pair0 + local < args.pairs;
+  const int64_t pair = min(pair0 + local, args.pairs - 1);  // (sequence, query head)
   const int64_t b = (uint32_t)pair / args.H;
   const int h = (int)((uint32_t)pair % args.H);
-  T* lds_y = lds_all + wave * kWaveLds;
-  T* lds_z = lds_y + kTile * kPitchY;
   const int t_begin = stretch * args.stretch, t_end = min(args.T, t_begin + args.stretch);
   const bool reverse = r.reverse != 0;
-  auto base = [&](const ScanArray& a) { return const_cast<char*>(a.data) + b * a.seq + (int64_t)((uint32_t)h / a.share) * a.head; };
-  const char *xb = STATE_ONLY ? nullptr : base(r.x), *yb = base(r.y), *zb = base(r.z);
-  char* ob = STATE_ONLY ? nullptr : base(r.out);
+  auto base = [&](const ScanArray& a, int which) {
+    const uint32_t p = min(pair0 + which, args.pairs - 1);
+    return a.data + (int64_t)(p / args.H) * a.seq + (int64_t)(p % args.H / a.share) * a.head;
+  };
   const float decay = args.decay[h];
   const uint8_t* done = args.done == nullptr ? nullptr : args.done + (uint32_t)b / args.seqs_per_flag;
   const int64_t n_flags = (uint32_t)args.B / args.seqs_per_flag;
-
-  // features of the state's elements: rows feat_x(a, g, e), columns feat_z(c, i / 4, i % 4)
-  auto feat_x = [&](int a, int e) { return feat<T, NK>(a, g, e); };
-  auto feat_z = [&](int c) { return slice0 + feat<T, NV>(c, i >> 2, i & 3); };
   const int Dx = r.y.dim, Dz = r.z.dim;
-  floatx4 S[NK][NV];
+
+  floatx4 S[NK][NV];  // rows feat(a, g, e), columns slice0 + 16 c + i
   {
     const float* s = nullptr;
     if (!STATE_ONLY && r.from.data != nullptr) s = r.from.data + (pair * r.from.stretches + (r.from.stretches > 1 ? stretch : 0)) * Dx * Dz;
@@ -341,148 +345,303 @@ __global__ void __launch_bounds__(64 * kMaxWaves, 2) scan_kernel(const ScanArgs 
       for (int c = 0; c < NV; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int f = feat_x(a, e), z = feat_z(c);
+          const int f = feat<T, NK>(a, g, e), z = slice0 + 16 * c + i;
           S[a][c][e] = s != nullptr && f < Dx && z < Dz ? s[f * r.from.row + z * r.from.col] : 0.f;
         }
   }
 
-  floatx4 near;  // g^|i-j|
+  // Blocks of a tile are numbered in the order of the scan: block u of a reverse scan is the tile's block U - 1 - u in time.
+  // Powers of the decay between a row of x (lane i) and rows of y (4 g + e): in one block, and from the block before; from the state that
+  // came in to a row; from a row of y of the last block to the state that goes on.  Times the scan's factors.
+  floatx4 near, far, from_j;
+  float to_i;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) near[e] = ipow(decay, abs(i - (4 * g + e)));
-  const TilePowers full = tile_powers(decay, kTile, reverse, i, g);
-  float carried = 1.f;
+  for (int e = 0; e < 4; ++e) {
+    const int j = 4 * g + e, d = reverse ? j - i : i - j;
+    near[e] = d < 0 ? 0.f : r.inner * ipow(decay, d);
+    far[e] = r.inner * ipow(decay, 16 + d);
+    from_j[e] = r.update * ipow(decay, reverse ? j + 1 : 15 - j);
+  }
+  to_i = r.inter * ipow(decay, reverse ? 15 - i : i + 1);
+  const float block = ipow(decay, 16);
+  const float whole = ipow(decay, kTile);
+  const float lost = (float)(1.0 - (double)whole);   // whole > 0.5: S -= lost S, so that no tile adds whole's own rounding to a long memory
+  auto block_at = [&](int u) { return 16 * (reverse ? U - 1 - u : u); };
 
   const int n_tiles = (t_end - t_begin + kTile - 1) / kTile;
-  Rows<T, NK> x, y, x_next, y_next;
-  Rows<T, NV> z, z_next;
-  uint8_t flag = 0, flag_next = 0;
-  auto tile_start = [&](int k) { return t_begin + kTile * (reverse ? n_tiles - 1 - k : k); };
-  auto request = [&](int k) {
-    const int t0 = tile_start(k), n = min(kTile, t_end - t0);
-    const int64_t t = t0 + min(i, n - 1);
-    const bool valid = i < n;
-    if constexpr (!STATE_ONLY) load_rows<T, NK>(x_next, r.x, xb + t * r.x.step, 0, valid, g);
-    load_rows<T, NK>(y_next, r.y, yb + t * r.y.step, 0, valid, g);
-    load_rows<T, NV>(z_next, r.z, zb + t * r.z.step, slice0, valid, g);
-    if (done != nullptr) flag_next = valid ? done[t * n_flags] : (uint8_t)0;
+  int t0 = reverse ? t_begin + kTile * (n_tiles - 1) : t_begin;
+  StageX sx, sy;
+  StageZ sz;
+  const int tile_way = reverse ? -kTile : kTile;
+  if constexpr (!STATE_ONLY) sx.begin(r.x, t0, tid, base);
+  sy.begin(r.y, t0, tid, base);
+  sz.begin(r.z, t0, tid, base);
+  uint8_t flag = 0;
+  auto request = [&](int t) {
+    const int n = min(kTile, t_end - t);
+    if constexpr (!STATE_ONLY) sx.request(r.x, n, tile_way * r.x.step, tid);
+    sy.request(r.y, n, tile_way * r.y.step, tid);
+    sz.request(r.z, n, tile_way * r.z.step, tid);
+    if (done != nullptr) flag = done[(int64_t)(t + min(lane, n - 1)) * n_flags];
   };
-  request(0);
-  for (int k = 0; k < n_tiles; ++k) {
-    x = x_next; y = y_next; z = z_next; flag = flag_next;
-    const int t0 = tile_start(k), n = min(kTile, t_end - t0);
-    if (k + 1 < n_tiles) request(k + 1);
-    const uint32_t ends = (uint32_t)__builtin_amdgcn_ballot_w64(flag != 0) & 0xffffu;  // episodes that end in the tile, by step
-    TilePowers p = full;
-    if (n < kTile) p = tile_powers(decay, n, reverse, i, g);
+  request(t0);
+  if (lane == 0) lds_left[wave] = active ? 0 : 1;
+  const char* x_tile = lds_x + local * kTile * kPiecesX * 16;
+  const char* y_tile = lds_y + local * kTile * kPiecesX * 16;
+  const char* z_tile = lds_z + local * kTile * kPiecesZ * 16;
+  auto y_column = [&](int u, int a) {
+    constexpr bool kRuns = sizeof(T) == 2 && NK % 2 == 0;
+    return column<T, kPiecesX>(reinterpret_cast<const T*>(y_tile), block_at(u), kRuns ? 32 * (a / 2) + 4 * (a & 1) : 16 * a, kRuns ? 8 : 4, i, g);
+  };
+  auto z_column = [&](int u, int c) {
+    return column<T, kPiecesZ>(reinterpret_cast<const T*>(z_tile), block_at(u), slice0 + 16 * c, 4, i, g);
+  };
+  constexpr int kParts = sizeof(T) == 4 ? 1 : 2;
+  bool any_end = false;
+  int left_at = -1;  // the tile's first step from which on this wavefront does its work the slow way
 
-    rows_to_lds<T, NK>(lds_y, y, i, g);
-    rows_to_lds<T, NV>(lds_z, z, i, g);
-    wave_lds_order();
-    uint32_t bad = 0;
-#pragma unroll
-    for (int a = 0; a < NK; ++a) bad |= not_finite(y.f[a]);
-#pragma unroll
-    for (int c = 0; c < NV; ++c) bad |= not_finite(z.f[c]);
-    bad &= sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+  for (int k = 0; k < n_tiles; ++k, t0 += tile_way) {
+    const int n = min(kTile, t_end - t0);
+    const uint32_t ends = (uint32_t)__builtin_amdgcn_ballot_w64(flag != 0 && lane < n);  // episodes that end in the tile, by step
+    if constexpr (!STATE_ONLY) sx.to_lds(lds_x, r.x, n, tid);
+    sy.to_lds(lds_y, r.y, n, tid);
+    sz.to_lds(lds_z, r.z, n, tid);
+    lds_barrier();
+    if (k + 1 < n_tiles) request(t0 + tile_way);
 
-    Frag zt[NV];
+    if (left_at < 0) {
+      Frag zt[U][NV];
 #pragma unroll
-    for (int c = 0; c < NV; ++c) zt[c] = column<NV>(lds_z, c, i, g);
-
-    floatx4 o[NV];
-    if constexpr (!STATE_ONLY) {
-      const uint32_t to_here = reverse ? ends >> i : ends & ((1u << i) - 1u);  // ends between the state that came in and step i
-      const float w_in = to_here == 0 ? p.to_i * r.inter : 0.f;
-      floatx4 score = {0.f, 0.f, 0.f, 0.f};
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int a = 0; a < NK; ++a) score = mma(y.f[a], x.f[a], score);
+        for (int c = 0; c < NV; ++c) zt[u][c] = z_column(u, c);
+      if constexpr (!STATE_ONLY) {
+        // scores: block u of x with the blocks v <= u of y; lane i of x, rows 4 g + e of y
+        floatx4 score[U][U];
+        Rows<T, NK> x[U];
 #pragma unroll
-      for (int c = 0; c < NV; ++c) {
-        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int u = 0; u < U; ++u) rows_of<T, NK>(x[u], x_tile, block_at(u) + i, g);
 #pragma unroll
-        for (int a = 0; a < NK; ++a) acc = mma_two(S[a][c], x.f[a], acc);
+        for (int v = 0; v < U; ++v) {
+          Rows<T, NK> y;
+          rows_of<T, NK>(y, y_tile, block_at(v) + i, g);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[c][e] = to_here == 0 ? acc[e] * w_in : 0.f;
-      }
+          for (int u = v; u < U; ++u) {
+            floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (NK % 2 == 0) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = 4 * g + e, lo = min(i, j), hi = max(i, j);
-        const bool seen = (reverse ? j >= i : j <= i) && ((ends & ((1u << hi) - 1u)) >> lo) == 0;
-        score[e] = seen ? score[e] * near[e] * r.inner : 0.f;
-      }
-      // (scores as the second operand: the two parts of a bf16 score are formed once)
-      if constexpr (sizeof(T) == 4) {
+              for (int a = 0; a < NK; a += 2) acc = mma2(y.f[a], y.f[a + 1], x[u].f[a], x[u].f[a + 1], acc);
+            } else {
 #pragma unroll
-        for (int c = 0; c < NV; ++c) o[c] = mma(zt[c], score, o[c]);
-      } else {
-        const shortx4 hi = pack4(score), lo = pack4(score - unpack4(hi));
-#pragma unroll
-        for (int c = 0; c < NV; ++c) o[c] = mma(zt[c], hi, mma(zt[c], lo, o[c]));
-      }
-      float sum = 0.f;
-#pragma unroll
-      for (int c = 0; c < NV; ++c) sum += (o[c][0] + o[c][1]) + (o[c][2] + o[c][3]);
-      if (!(fabsf(sum) < __builtin_inff())) bad = 1;
-    }
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(bad != 0) != 0, 0)) {
-      scan_tile_slow<T, NK, NV, STATE_ONLY>(S, r, xb, yb, zb, ob, t0, n, slice0, decay, ends, i, g);
-      carried = ends == 0 ? carried * p.whole : 0.f;
-      continue;
-    }
-    if constexpr (!STATE_ONLY) {
-      if (i < n) {
-        char* row = ob + (int64_t)(t0 + i) * r.out.step;
-        if (r.out_f32 || sizeof(T) == 4) {
-#pragma unroll
-          for (int c = 0; c < NV; ++c) {
-            const int f0 = slice0 + feat<T, NV>(c, g, 0);
-            if (r.out.wide && f0 < Dz)
-              *reinterpret_cast<floatx4*>(reinterpret_cast<float*>(row) + f0) = o[c];
-            else if (!r.out.wide)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (f0 + e < Dz) reinterpret_cast<float*>(row)[f0 + e] = o[c][e];
+              for (int a = 0; a < NK; ++a) acc = mma(y.f[a], x[u].f[a], acc);
+            }
+            score[u][v] = acc;
           }
-        } else if (NV % 2 == 0 && r.out.wide) {
+        }
+        floatx4 o[U][NV];
 #pragma unroll
-          for (int c = 0; c + 1 < NV; c += 2) {
-            const int f0 = slice0 + feat<T, NV>(c, g, 0);
-            if (f0 < Dz) {
-              const shortx8 v = __builtin_shufflevector(pack4(o[c]), pack4(o[c + 1]), 0, 1, 2, 3, 4, 5, 6, 7);
-              *reinterpret_cast<shortx8*>(reinterpret_cast<bf16_t*>(row) + f0) = v;
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int c = 0; c < NV; ++c) o[u][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+          if constexpr (NK % 2 == 0) {
+#pragma unroll
+            for (int a = 0; a < NK; a += 2) {
+              const Parts<T, 2> s0 = parts_of<T, 2>(S[a][c]), s1 = parts_of<T, 2>(S[a + 1][c]);
+#pragma unroll
+              for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int p = kParts - 1; p >= 0; --p) o[u][c] = mma2(s0.p[p], s1.p[p], x[u].f[a], x[u].f[a + 1], o[u][c]);
+            }
+          } else {
+#pragma unroll
+            for (int a = 0; a < NK; ++a) {
+              const Parts<T, 2> s0 = parts_of<T, 2>(S[a][c]);
+#pragma unroll
+              for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int p = kParts - 1; p >= 0; --p) o[u][c] = mma(s0.p[p], x[u].f[a], o[u][c]);
             }
           }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float to = to_i;
+          if (u > 0) to *= block;
+          if (reverse && n < kTile) {  // the tile's last step is n - 1
+            const int ti = block_at(u) + fresh(i);
+            to = ti < n ? r.inter * ipow(decay, n - 1 - ti) : 0.f;
+          }
+          if (ends == 0) {
+#pragma unroll
+            for (int c = 0; c < NV; ++c) o[u][c] *= to;
+#pragma unroll
+            for (int v = 0; v <= u; ++v) score[u][v] *= u == v ? near : far;
+          } else {
+            const int ti = block_at(u) + fresh(i), g4 = 4 * fresh(g);
+            const uint32_t between = reverse ? ends >> ti : ends & ((1u << ti) - 1u);
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[u][c][e] = between == 0 ? o[u][c][e] * to : 0.f;
+#pragma unroll
+            for (int v = 0; v <= u; ++v)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int tj = block_at(v) + g4 + e, lo = min(ti, tj), hi = max(ti, tj);
+                const bool seen = ((ends & ((1u << hi) - 1u)) >> lo) == 0;
+                score[u][v][e] = seen ? score[u][v][e] * (u == v ? near[e] : far[e]) : 0.f;
+              }
+          }
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          Parts<T, 2> w[U];
+#pragma unroll
+          for (int v = 0; v <= u; ++v) w[v] = parts_of<T, 2>(score[u][v]);
+#pragma unroll
+          for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int p = kParts - 1; p >= 0; --p) {
+              if (u == 0) o[u][c] = mma(zt[0][c], w[0].p[p], o[u][c]);
+              else if constexpr (U > 1) o[u][c] = mma2(zt[0][c], zt[1][c], w[0].p[p], w[1].p[p], o[u][c]);
+            }
+#pragma unroll
+          for (int c = 0; c < NV; ++c) sum += (o[u][c][0] + o[u][c][1]) + (o[u][c][2] + o[u][c][3]);
+        }
+        // an infinity or a NaN in a row of y or z shows in that step's own output: the rest of the sequence is done the slow way then
+        if (__builtin_amdgcn_ballot_w64(!(fabsf(sum) < __builtin_inff())) != 0) {
+          left_at = t0;
+          if (lane == 0) lds_left[wave] = 1;
+        } else if (WIDE && !(sizeof(T) == 2 && r.out_f32)) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int row = block_at(u) + i, swz = swizzle<kPiecesZ>(row);
+            char* p = lds_o + (local * kTile + row) * kPiecesZ * 16;
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+              const int f = slice0 + 16 * c + 4 * g;
+              if constexpr (sizeof(T) == 4) *reinterpret_cast<floatx4*>(p + ((f / 4) ^ swz) * 16) = o[u][c];
+              else *reinterpret_cast<shortx4*>(p + ((f / 8) ^ swz) * 16 + (f & 4) * 2) = pack4(o[u][c]);
+            }
+          }
+        } else if (active) {
+          char* ob = const_cast<char*>(base(r.out, local));
+          const int i0 = fresh(i), f0 = slice0 + 4 * fresh(g);
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (block_at(u) + i0 < n) {
+              char* row = ob + (int64_t)(t0 + block_at(u) + i0) * r.out.step;
+#pragma unroll
+              for (int c = 0; c < NV; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int f = f0 + 16 * c + e;
+                  if (f >= Dz) continue;
+                  if (sizeof(T) == 4 || r.out_f32) reinterpret_cast<float*>(row)[f] = o[u][c][e];
+                  else reinterpret_cast<bf16_t*>(row)[f] = to_bf16(o[u][c][e]);
+                }
+            }
+        }
+      }
+      if (left_at < 0) {
+        floatx4 w[U];  // what a row of y adds to the state that goes on
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          w[u] = from_j;
+          if (u + 1 < U) w[u] *= block;
+        }
+        if (n < kTile || ends != 0) {
+          const int g4 = 4 * fresh(g);
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int tj = block_at(u) + g4 + e;
+              if (!reverse && n < kTile) w[u][e] = tj < n ? r.update * ipow(decay, n - 1 - tj) : 0.f;
+              const uint32_t between = reverse ? ends & ((1u << tj) - 1u) : ends >> tj;
+              if (between != 0) w[u][e] = 0.f;
+            }
+        }
+        if (ends != 0) {
+          any_end = true;
+#pragma unroll
+          for (int a = 0; a < NK; ++a)
+#pragma unroll
+            for (int c = 0; c < NV; ++c) S[a][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+        } else if (whole > 0.5f && n == kTile) {
+#pragma unroll
+          for (int a = 0; a < NK; ++a)
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) S[a][c][e] = fmaf(-lost, S[a][c][e], S[a][c][e]);
         } else {
+          const float f = n == kTile ? whole : ipow(decay, n);
 #pragma unroll
-          for (int c = 0; c < NV; ++c) {
-            const int f0 = slice0 + feat<T, NV>(c, g, 0);
+          for (int a = 0; a < NK; ++a)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (f0 + e < Dz) reinterpret_cast<bf16_t*>(row)[f0 + e] = to_bf16(o[c][e]);
+            for (int c = 0; c < NV; ++c) S[a][c] *= f;
+        }
+        // the weights go to the side with fewer fragments
+        constexpr int Q = sizeof(T) == 4 ? 1 : 3;
+        Parts<T, 3> zw[U][NV];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int c = 0; c < NV; ++c) zw[u][c] = parts_of<T, 3>(widen4(zt[u][c]) * w[u]);
+#pragma unroll
+        for (int a = 0; a < NK; ++a) {
+          Frag yt[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) yt[u] = y_column(u, a);
+#pragma unroll
+          for (int p = Q - 1; p >= 0; --p)
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+              if constexpr (U == 2) S[a][c] = mma2(yt[0], yt[1], zw[0][c].p[p], zw[1][c].p[p], S[a][c]);
+              else S[a][c] = mma(yt[0], zw[0][c].p[p], S[a][c]);
+            }
+        }
+      }
+    }
+    lds_barrier();
+    if constexpr (!STATE_ONLY) {
+      if (WIDE && !(sizeof(T) == 2 && r.out_f32)) {
+#pragma unroll
+        for (int s = 0; s < StageZ::kSlots; ++s) {
+          const int q = StageZ::index(s, tid), row = StageZ::row(q), piece = StageZ::piece(q), which = StageZ::pair(q);
+          const bool on = (StageZ::kAll % kThreads == 0 || s * kThreads + tid < StageZ::kAll) && row < n && piece * E < Dz &&
+                          lds_left[which * SL + piece * E / (16 * NV)] == 0;
+          if (on) {
+            const uint4 v = *reinterpret_cast<const uint4*>(lds_o + ((which * kTile + row) * kPiecesZ + (piece ^ swizzle<kPiecesZ>(row))) * 16);
+            *reinterpret_cast<uint4*>(const_cast<char*>(base(r.out, which)) + (int64_t)(t0 + row) * r.out.step + piece * 16) = v;
           }
         }
       }
     }
-    floatx4 w;  // what step j adds to the state that goes on
+  }
+
+  if (!active) return;
+  auto own = [&](const ScanArray& a) { return const_cast<char*>(base(a, local)); };
+  if constexpr (STATE_ONLY) {  // nothing shows on the way: look at the end, and start again the slow way
+    float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = 4 * g + e;
-      const uint32_t after = reverse ? ends & ((1u << j) - 1u) : ends >> j;
-      w[e] = after == 0 ? p.from_j[e] * r.update : 0.f;
+    for (int a = 0; a < NK; ++a)
+#pragma unroll
+      for (int c = 0; c < NV; ++c) sum += (S[a][c][0] + S[a][c][1]) + (S[a][c][2] + S[a][c][3]);
+    if (__builtin_amdgcn_ballot_w64(!(fabsf(sum) < __builtin_inff())) != 0) {
+#pragma unroll
+      for (int a = 0; a < NK; ++a)
+#pragma unroll
+        for (int c = 0; c < NV; ++c) S[a][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+      scan_slow<T, NK, NV, STATE_ONLY>(S, r, nullptr, own(r.y), own(r.z), nullptr, t_begin, t_end - t_begin, slice0, decay, done, n_flags, i, g);
     }
-#pragma unroll
-    for (int a = 0; a < NK; ++a) {
-      const auto yw = weigh_parts(column<NK>(lds_y, a, i, g), w);
-#pragma unroll
-      for (int c = 0; c < NV; ++c) {
-        floatx4 s = S[a][c];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] = ends == 0 ? s[e] * p.whole : 0.f;
-        S[a][c] = mma(yw, zt[c], s);
-      }
-    }
-    carried = ends == 0 ? carried * p.whole : 0.f;
-    wave_lds_order();
+  } else if (left_at >= 0) {
+    const int from = reverse ? t_begin : left_at, to = reverse ? min(left_at + kTile, t_end) : t_end;
+    scan_slow<T, NK, NV, STATE_ONLY>(S, r, own(r.x), own(r.y), own(r.z), own(r.out), from, to - from, slice0, decay, done, n_flags, i, g);
   }
 
   if (r.to.data != nullptr) {
@@ -493,38 +652,38 @@ __global__ void __launch_bounds__(64 * kMaxWaves, 2) scan_kernel(const ScanArgs 
       for (int c = 0; c < NV; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int f = feat_x(a, e), zc = feat_z(c);
+          const int f = feat<T, NK>(a, g, e), zc = slice0 + 16 * c + i;
           if (f < Dx && zc < Dz) s[f * r.to.row + zc * r.to.col] = S[a][c][e];
         }
   }
-  if (STATE_ONLY && role_index == 0 && slice0 == 0 && lane == 0) args.carry[pair * args.n_stretches + stretch] = carried;
+  if (STATE_ONLY && role_index == 0 && slice0 == 0 && lane == 0) args.carry[pair * args.n_stretches + stretch] = any_end ? 0.f : ipow(decay, t_end - t_begin);
 }
 
 // ---- launch: the instance by (padded) widths -------------------------------------------------------------------------------------------
-// Columns of the state that one wavefront holds: at most 64 accumulator registers a lane
-inline int scan_nk(int dim) { return dim <= 16 ? 1 : dim <= 32 ? 2 : dim <= 64 ? 4 : 8; }
-inline int scan_nv(int nk, int dim) { return dim <= 16 ? 1 : dim <= 32 || nk == 8 ? 2 : 4; }
-inline int scan_slices(int nk, int dim) {
-  const int w = 16 * scan_nv(nk, dim);
-  return (dim + w - 1) / w;
-}
+inline int scan_nk(int dim) { return dim <= 16 ? 1 : dim <= 32 ? 2 : dim <= 64 ? 4 : dim <= 96 ? 6 : 8; }
+inline int scan_nv(int dim) { return dim <= 16 ? 1 : 2; }
+inline int scan_slices(int dim) { return dim <= 32 ? 1 : (dim + 31) / 32; }
 
-// A stretch of no steps has no valid row to point at: the caller never launches one.
-void launch_scan_f32(const ScanArgs& a, int nk, int nv, bool state_only, dim3 grid, dim3 block, hipStream_t s);
-void launch_scan_bf16(const ScanArgs& a, int nk, int nv, bool state_only, dim3 grid, dim3 block, hipStream_t s);
+// A scan of no steps has no valid row to point at: the caller never launches one.
+void launch_scan_f32(const ScanArgs& a, int dx, int dz, bool state_only, bool wide, hipStream_t s);
+void launch_scan_bf16(const ScanArgs& a, int dx, int dz, bool state_only, bool wide, hipStream_t s);
 
 template <class T>
-inline void launch_scan(const ScanArgs& a, int nk, int nv, bool state_only, dim3 grid, dim3 block, hipStream_t s) {
-#define MARL_SCAN(K, V)                                                                                 \
-  if (nk == K && nv == V) {                                                                             \
-    if (state_only) hipLaunchKernelGGL((scan_kernel<T, K, V, true>), grid, block, 0, s, a);            \
-    else hipLaunchKernelGGL((scan_kernel<T, K, V, false>), grid, block, 0, s, a);                      \
-    return;                                                                                             \
+inline void launch_scan(const ScanArgs& a, int dx, int dz, bool state_only, bool wide, hipStream_t s) {
+  const int nk = scan_nk(dx), nv = scan_nv(dz), slices = scan_slices(dz);
+#define MARL_SCAN(K, V, SL)                                                                                               \
+  if (nk == K && nv == V && slices == SL) {                                                                               \
+    constexpr uint32_t P = scan_pairs<SL>();                                                                              \
+    const dim3 grid((a.pairs + P - 1) / P * a.n_stretches * a.n_roles), block(64 * SL * P);                               \
+    if (state_only && wide) hipLaunchKernelGGL((scan_kernel<T, K, V, SL, true, true>), grid, block, 0, s, a);            \
+    else if (state_only) hipLaunchKernelGGL((scan_kernel<T, K, V, SL, true, false>), grid, block, 0, s, a);              \
+    else if (wide) hipLaunchKernelGGL((scan_kernel<T, K, V, SL, false, true>), grid, block, 0, s, a);                    \
+    else hipLaunchKernelGGL((scan_kernel<T, K, V, SL, false, false>), grid, block, 0, s, a);                             \
+    return;                                                                                                               \
   }
-  MARL_SCAN(1, 1) MARL_SCAN(1, 2) MARL_SCAN(1, 4)
-  MARL_SCAN(2, 1) MARL_SCAN(2, 2) MARL_SCAN(2, 4)
-  MARL_SCAN(4, 1) MARL_SCAN(4, 2) MARL_SCAN(4, 4)
-  MARL_SCAN(8, 1) MARL_SCAN(8, 2)
+#define MARL_SCAN_ALL(K) MARL_SCAN(K, 1, 1) MARL_SCAN(K, 2, 1) MARL_SCAN(K, 2, 2) MARL_SCAN(K, 2, 3) MARL_SCAN(K, 2, 4)
+  MARL_SCAN_ALL(1) MARL_SCAN_ALL(2) MARL_SCAN_ALL(4) MARL_SCAN_ALL(6) MARL_SCAN_ALL(8)
+#undef MARL_SCAN_ALL
 #undef MARL_SCAN
 }
 

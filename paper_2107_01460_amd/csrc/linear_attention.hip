@@ -23,16 +23,16 @@ Plan plan_of(const marl_attention_dims& d, bool backward) {
   Plan p{};
   p.pairs = (int64_t)d.n_seqs * d.n_heads;
   p.group = d.n_heads / d.n_kv_heads;
-  const int nk = scan_nk(d.dim_k);
-  const int64_t units = p.pairs * scan_slices(nk, d.dim_v) * (backward ? 3 : 1);
-  const int64_t tiles = ((int64_t)d.n_steps + kTile - 1) / kTile;
+  const int64_t units = p.pairs * scan_slices(d.dim_v) * (backward ? 3 : 1);
+  const int tile = 16 * (d.precision == 0 ? ScanTraits<float>::kSub : ScanTraits<bf16_t>::kSub), least = 64 / tile;
+  const int64_t tiles = ((int64_t)d.n_steps + tile - 1) / tile;
   int64_t n = units > 0 ? kWaves / units : 1;
-  n = n < tiles / 4 ? n : tiles / 4;
+  n = n < tiles / least ? n : tiles / least;
   if (n < 2) n = 1;
   const int64_t per = tiles > 0 ? (tiles + n - 1) / n : 1;
-  p.stretch = (int32_t)(per * kTile);
+  p.stretch = (int32_t)(per * tile);
   p.n_stretches = (uint32_t)(tiles > 0 ? (tiles + per - 1) / per : 1);
-  if (p.n_stretches == 1) p.stretch = d.n_steps > 0 ? (int32_t)(tiles > (INT32_MAX / kTile) ? INT32_MAX : tiles * kTile) : kTile;
+  if (p.n_stretches == 1) p.stretch = tiles > 0 ? (int32_t)(tiles * tile) : tile;
   int64_t at = 0;
   auto take = [&](int64_t floats) {
     const int64_t here = at;
@@ -212,20 +212,20 @@ ScanState state_of(const float* p, uint32_t stretches, int row, int col) { retur
 
 // Launch over roles of one shape: widths dx (x, y) and dz (z, out)
 int32_t scan(ScanArgs a, const marl_attention_dims& d, const Plan& p, int dx, int dz, bool state_only, hipStream_t s) {
-  const int nk = scan_nk(dx), nv = scan_nv(nk, dz);
   a.T = d.n_steps;
   a.B = d.n_seqs;
   a.H = (uint32_t)d.n_heads;
   a.seqs_per_flag = (uint32_t)d.seqs_per_flag;
-  a.slices = (uint32_t)scan_slices(nk, dz);
   a.n_stretches = p.n_stretches;
   a.stretch = p.stretch;
-  a.units = (uint32_t)(p.pairs * a.slices);
-  const int64_t waves = (int64_t)a.units * a.n_roles * a.n_stretches;
-  const uint32_t per = waves >= 4 * 256 ? 4 : 1;  // few wavefronts: one to a compute unit
-  const int64_t blocks = ((int64_t)a.units + per - 1) / per * a.n_roles * a.n_stretches;
-  if (blocks >= ((int64_t)1 << 31)) return MARL_E_SIZE;
-  (d.precision == 0 ? launch_scan_f32 : launch_scan_bf16)(a, nk, nv, state_only, dim3((unsigned)blocks), dim3(64 * per), s);
+  a.pairs = (uint32_t)p.pairs;
+  if (p.pairs * a.n_roles * a.n_stretches >= ((int64_t)1 << 31)) return MARL_E_SIZE;
+  bool wide = true;
+  for (uint32_t u = 0; u < a.n_roles; ++u) {
+    const ScanRole& r = a.role[u];
+    wide = wide && r.y.wide && r.z.wide && (state_only || (r.x.wide && r.out.wide));
+  }
+  (d.precision == 0 ? launch_scan_f32 : launch_scan_bf16)(a, dx, dz, state_only, wide, s);
   return launch_status();
 }
 
@@ -396,7 +396,7 @@ int32_t marl_linear_attention_backward(const marl_attention_dims* dims, marl_vie
   rv.from = state_of(r0, p.n_stretches, d.dim_v, 1);
   if (!joined) rv.to = state_of(dstate, 1, d.dim_v, 1);
   a.carry = nullptr;
-  const bool one = scan_nk(d.dim_k) == scan_nk(d.dim_v) && d.dim_k == d.dim_v;  // one launch for all three
+  const bool one = d.dim_k == d.dim_v;  // one launch for all three
   a.n_roles = one ? 3 : 2;
   a.role[0] = rq;
   a.role[1] = rk;

@@ -2,7 +2,5 @@
 #include "linear_attention.h"
 
 namespace marl {
-void launch_scan_f32(const ScanArgs& a, int nk, int nv, bool state_only, dim3 grid, dim3 block, hipStream_t s) {
-  launch_scan<float>(a, nk, nv, state_only, grid, block, s);
-}
+void launch_scan_f32(const ScanArgs& a, int dx, int dz, bool state_only, bool wide, hipStream_t s) { launch_scan<float>(a, dx, dz, state_only, wide, s); }
 }  // namespace marl
