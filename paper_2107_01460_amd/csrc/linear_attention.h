@@ -71,11 +71,11 @@ __device__ __forceinline__ int feat(int a, int g, int e) {
   return sizeof(T) == 2 && N % 2 == 0 ? 32 * (a / 2) + 8 * g + 4 * (a & 1) + e : 16 * a + 4 * g + e;
 }
 
-__device__ __forceinline__ float ipow(float base, int m) {  // base^m rounded once, 0^0 = 1
+__device__ __forceinline__ double ipow(float base, int m) {  // base^m, 0^0 = 1
   double r = 1.0, g = base;
   for (; m != 0; m >>= 1, g *= g)
     if (m & 1) r *= g;
-  return (float)r;
+  return r;
 }
 
 // ---- products of 16 x 16 outputs; the contraction index of element e of lane group g is the same on both sides -----------------------
@@ -177,6 +177,12 @@ __device__ void scan_slow(floatx4 (&S)[NK][NV], const ScanRole& r, const char* x
       }
     }
   }
+}
+
+// Between LDS writes and reads of one wavefront's own part: its LDS accesses take effect in order, the compiler has to keep it.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
 // A copy that the compiler takes for a new value: what a rare branch works out from it is worked out there, not kept in registers across the loop
@@ -294,6 +300,25 @@ struct Stage {
   }
 };
 
+// The state's element (feat(a, g, e), first + 16 c + i) for every a, c, e of a lane: f(element's place in the lane's registers, its address or nullptr).
+// Addresses are a uniform part and one offset a lane.
+template <class T, int NK, int NV, class F>
+__device__ __forceinline__ void each_state_element(float* s, int row, int col, int Dx, int Dz, int first, int i, int g, F f) {
+  const int f0 = feat<T, NK>(0, g, 0);
+  const uint32_t lane = (uint32_t)(f0 * row + (first + i) * col);
+  const bool whole = Dx == 16 * NK && first + 16 * NV <= Dz;
+#pragma unroll
+  for (int a = 0; a < NK; ++a)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int c = 0; c < NV; ++c) {
+        float* p = s + (feat<T, NK>(a, 0, e) * row + 16 * c * col);
+        if (whole) f(a, c, e, p + lane);
+        else f(a, c, e, f0 + feat<T, NK>(a, 0, e) < Dx && first + 16 * c + i < Dz ? p + lane : nullptr);
+      }
+}
+
 template <int SL>
 constexpr int scan_pairs() { return SL == 1 ? 4 : SL == 2 ? 2 : 1; }  // (sequence, head) pairs of a workgroup
 
@@ -311,6 +336,7 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 ? 2 : 3) s
   __shared__ __align__(16) char lds_z[kBytesZ];
   __shared__ __align__(16) char lds_o[STATE_ONLY ? 16 : kBytesZ];
   __shared__ uint32_t lds_left[SL * P];  // wavefronts that have left the common way
+  __shared__ float powers[SL * P][kTile + 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
   // neighbours in a contiguous run on one XCD: first the roles, which read the same arrays, then the stretches, then the pairs
   uint32_t at = xcd_remap(blockIdx.x, gridDim.x);
@@ -336,36 +362,33 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 ? 2 : 3) s
   const int Dx = r.y.dim, Dz = r.z.dim;
 
   floatx4 S[NK][NV];  // rows feat(a, g, e), columns slice0 + 16 c + i
-  {
-    const float* s = nullptr;
-    if (!STATE_ONLY && r.from.data != nullptr) s = r.from.data + (pair * r.from.stretches + (r.from.stretches > 1 ? stretch : 0)) * Dx * Dz;
+  if (!STATE_ONLY && r.from.data != nullptr) {
+    float* s = r.from.data + (pair * r.from.stretches + (r.from.stretches > 1 ? stretch : 0)) * Dx * Dz;
+    each_state_element<T, NK, NV>(s, r.from.row, r.from.col, Dx, Dz, slice0, i, g,
+                                  [&](int a, int c, int e, const float* p) { S[a][c][e] = p != nullptr ? *p : 0.f; });
+  } else {
 #pragma unroll
     for (int a = 0; a < NK; ++a)
 #pragma unroll
-      for (int c = 0; c < NV; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int f = feat<T, NK>(a, g, e), z = slice0 + 16 * c + i;
-          S[a][c][e] = s != nullptr && f < Dx && z < Dz ? s[f * r.from.row + z * r.from.col] : 0.f;
-        }
+      for (int c = 0; c < NV; ++c) S[a][c] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
 
   // Blocks of a tile are numbered in the order of the scan: block u of a reverse scan is the tile's block U - 1 - u in time.
   // Powers of the decay between a row of x (lane i) and rows of y (4 g + e): in one block, and from the block before; from the state that
   // came in to a row; from a row of y of the last block to the state that goes on.  Times the scan's factors.
+  if (lane <= kTile) powers[wave][lane] = (float)ipow(decay, lane);
+  const float* power = powers[wave];
+  wave_lds_order();
   floatx4 near, far, from_j;
-  float to_i;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const int j = 4 * g + e, d = reverse ? j - i : i - j;
-    near[e] = d < 0 ? 0.f : r.inner * ipow(decay, d);
-    far[e] = r.inner * ipow(decay, 16 + d);
-    from_j[e] = r.update * ipow(decay, reverse ? j + 1 : 15 - j);
+    near[e] = d < 0 ? 0.f : r.inner * power[abs(d)];
+    far[e] = U > 1 ? r.inner * power[16 + d] : 0.f;
+    from_j[e] = r.update * power[reverse ? j + 1 : 15 - j];
   }
-  to_i = r.inter * ipow(decay, reverse ? 15 - i : i + 1);
-  const float block = ipow(decay, 16);
-  const float whole = ipow(decay, kTile);
-  const float lost = (float)(1.0 - (double)whole);   // whole > 0.5: S -= lost S, so that no tile adds whole's own rounding to a long memory
+  const float to_i = r.inter * power[reverse ? 15 - i : i + 1], block = power[16], whole = power[kTile];
+  const float lost = (float)(1.0 - ipow(decay, kTile));   // whole > 0.5: S -= lost S, so that no tile adds whole's own rounding to a long memory
   auto block_at = [&](int u) { return 16 * (reverse ? U - 1 - u : u); };
 
   const int n_tiles = (t_end - t_begin + kTile - 1) / kTile;
@@ -471,7 +494,7 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 ? 2 : 3) s
           if (u > 0) to *= block;
           if (reverse && n < kTile) {  // the tile's last step is n - 1
             const int ti = block_at(u) + fresh(i);
-            to = ti < n ? r.inter * ipow(decay, n - 1 - ti) : 0.f;
+            to = ti < n ? r.inter * power[n - 1 - ti] : 0.f;
           }
           if (ends == 0) {
 #pragma unroll
@@ -560,7 +583,7 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 ? 2 : 3) s
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int tj = block_at(u) + g4 + e;
-              if (!reverse && n < kTile) w[u][e] = tj < n ? r.update * ipow(decay, n - 1 - tj) : 0.f;
+              if (!reverse && n < kTile) w[u][e] = tj < n ? r.update * power[n - 1 - tj] : 0.f;
               const uint32_t between = reverse ? ends & ((1u << tj) - 1u) : ends >> tj;
               if (between != 0) w[u][e] = 0.f;
             }
@@ -579,7 +602,7 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 ? 2 : 3) s
 #pragma unroll
               for (int e = 0; e < 4; ++e) S[a][c][e] = fmaf(-lost, S[a][c][e], S[a][c][e]);
         } else {
-          const float f = n == kTile ? whole : ipow(decay, n);
+          const float f = n == kTile ? whole : power[n];
 #pragma unroll
           for (int a = 0; a < NK; ++a)
 #pragma unroll
@@ -646,17 +669,11 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 ? 2 : 3) s
 
   if (r.to.data != nullptr) {
     float* s = r.to.data + (pair * r.to.stretches + (r.to.stretches > 1 ? stretch : 0)) * Dx * Dz;
-#pragma unroll
-    for (int a = 0; a < NK; ++a)
-#pragma unroll
-      for (int c = 0; c < NV; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int f = feat<T, NK>(a, g, e), zc = slice0 + 16 * c + i;
-          if (f < Dx && zc < Dz) s[f * r.to.row + zc * r.to.col] = S[a][c][e];
-        }
+    each_state_element<T, NK, NV>(s, r.to.row, r.to.col, Dx, Dz, slice0, i, g, [&](int a, int c, int e, float* p) {
+      if (p != nullptr) *p = S[a][c][e];
+    });
   }
-  if (STATE_ONLY && role_index == 0 && slice0 == 0 && lane == 0) args.carry[pair * args.n_stretches + stretch] = any_end ? 0.f : ipow(decay, t_end - t_begin);
+  if (STATE_ONLY && role_index == 0 && slice0 == 0 && lane == 0) args.carry[pair * args.n_stretches + stretch] = any_end ? 0.f : (float)ipow(decay, t_end - t_begin);
 }
 
 // ---- launch: the instance by (padded) widths -------------------------------------------------------------------------------------------

@@ -30,6 +30,23 @@ __global__ void __launch_bounds__(256) rotary_table_kernel(marl_rotary_dims d, f
   table[position * d.rotary_dim + half + i] = (float)(sine * d.amplitude);
 }
 
+// Division of n < 2^31 by a number fixed at launch: a product and a shift.  (magic d = 2^shift + e with 0 < e <= 2^(shift - 31), so n magic / 2^shift
+// is less than n / d + 1 / d.)
+struct Divisor {
+  uint32_t d = 1, magic = 0;
+  int shift = 0;
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return __umulhi(2 * n, magic) >> (shift - 31); }
+};
+Divisor divisor(uint32_t d) {
+  Divisor r;
+  r.d = d;
+  int lg = 0;
+  while ((1u << lg) < d) ++lg;
+  r.shift = 31 + lg;
+  r.magic = (uint32_t)(((uint64_t)1 << r.shift) / d + 1);
+  return r;
+}
+
 // ---- rotation ----------------------------------------------------------------------------------------------------------------------
 struct RotaryArray {
   const char* in;
@@ -41,9 +58,10 @@ struct RotaryArgs {
   const float* table;
   const int32_t* positions;
   int32_t n_positions, rotary, first, inverse;
-  uint32_t B, heads[2], seqs_per_flag, n_flags;
-  uint32_t dim, items;  // items of a head: pairs of vectors, then vectors that are copied
-  uint32_t pair_items;
+  uint32_t heads[2], n_flags, dim;
+  uint32_t pair_items;  // items of a head: rotated ones, then ones that are copied
+  Divisor B, seqs_per_flag, items, per_token;
+  int32_t table_wide;   // 16-byte accesses to table rows
   int64_t tokens;
 };
 
@@ -82,75 +100,110 @@ __device__ __forceinline__ T narrow(float v) {
   else return to_bf16(v);
 }
 
+// N consecutive values of a table row's half from `first` on, those that there are
+template <int N>
+__device__ __forceinline__ void load_row(float (&v)[N], const float* half_row, int first, int half, int wide) {
+  if (N % 4 == 0 && wide) {  // (half is a multiple of four, and so of a run of four)
+#pragma unroll
+    for (int k = 0; k + 3 < N; k += 4) {
+      const float4 f = *reinterpret_cast<const float4*>(half_row + (first + k < half ? first + k : 0));
+      v[k] = f.x; v[k + 1] = f.y; v[k + 2] = f.z; v[k + 3] = f.w;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = half_row[min(first + k, half - 1)];
+  }
+}
+
+// A thread takes kItems items, each 256 after the last, so that the chains of loads (position, table row) of several are on their way together.
+constexpr int kItems = 4;
+
 template <class T, int E, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs args) {
+  constexpr bool kPairsInside = INTERLEAVED && E > 1;
+  constexpr int kPairs = kPairsInside ? E / 2 : E;  // pairs of an item
   // items in order: token, head (of q, then of k), item of the head; a workgroup's first token and the rest by 32-bit division
-  const uint32_t per_token = (args.heads[0] + args.heads[1]) * args.items;
-  const int64_t first = (int64_t)blockIdx.x * 256;
-  const int64_t token0 = first / per_token;
-  const uint32_t at = (uint32_t)(first - token0 * per_token) + threadIdx.x;
-  const uint32_t more = at / per_token, in_token = at - more * per_token;
-  if (token0 + more >= args.tokens) return;
-  const int64_t t0 = token0 / args.B;
-  uint32_t b = (uint32_t)(token0 - t0 * args.B) + more;
-  const uint32_t over = b / args.B;
-  b -= over * args.B;
-  const int64_t t = t0 + over;
-  uint32_t head = in_token / args.items;
-  const uint32_t item = in_token - head * args.items;
-  const bool second = head >= args.heads[0];
-  if (second) head -= args.heads[0];
-  const RotaryArray& a = args.a[second];
-  const T* in = reinterpret_cast<const T*>(a.in) + t * a.in_step + b * a.in_seq + head * a.in_head;
-  T* out = reinterpret_cast<T*>(a.out) + t * a.out_step + b * a.out_seq + head * a.out_head;
+  const int64_t first = (int64_t)blockIdx.x * (256 * kItems);
+  const int64_t token0 = first / args.per_token.d;
+  const uint32_t in0 = (uint32_t)(first - token0 * args.per_token.d) + threadIdx.x;
+  const int64_t t00 = token0 / args.B.d;
+  const uint32_t b0 = (uint32_t)(token0 - t00 * args.B.d);
   const int R = args.rotary, half = R / 2;
-  if (item >= args.pair_items) {  // behind the rotated part
-    const uint32_t c = INTERLEAVED && E > 1 ? item * E : R + (item - args.pair_items) * E;
-    put<T, E>(out + c, get<T, E>(in + c));
-    return;
+  struct Item {
+    T* out;
+    Piece<T, E> p1, p2;
+    int first_pair;  // -1: copied
+    uint32_t c1, c2;
+    const float* row;
+    bool on, known;
+  } it[kItems];
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    Item& x = it[u];
+    const uint32_t at = in0 + 256 * u, more = args.per_token(at), in_token = at - more * args.per_token.d;
+    x.on = token0 + more < args.tokens;
+    if (!x.on) continue;
+    uint32_t b = b0 + more;
+    const uint32_t over = args.B(b);
+    b -= over * args.B.d;
+    const int64_t t = t00 + over;
+    uint32_t head = args.items(in_token);
+    const uint32_t item = in_token - head * args.items.d;
+    const bool second = head >= args.heads[0];
+    if (second) head -= args.heads[0];
+    const RotaryArray& a = args.a[second];
+    const T* in = reinterpret_cast<const T*>(a.in) + t * a.in_step + b * a.in_seq + head * a.in_head;
+    x.out = reinterpret_cast<T*>(a.out) + t * a.out_step + b * a.out_seq + head * a.out_head;
+    if (item >= args.pair_items) {  // behind the rotated part
+      x.first_pair = -1;
+      x.c1 = kPairsInside ? item * E : R + (item - args.pair_items) * E;
+    } else {
+      x.first_pair = (int)item * kPairs;
+      x.c1 = kPairsInside ? item * E : INTERLEAVED ? 2 * item : item * E;
+      x.c2 = INTERLEAVED ? x.c1 + 1 : x.c1 + half;
+    }
+    x.p1 = get<T, E>(in + x.c1);
+    if (!kPairsInside && x.first_pair >= 0) x.p2 = get<T, E>(in + x.c2);
+    if (x.first_pair >= 0) {
+      const int64_t position = args.positions != nullptr ? args.positions[t * args.n_flags + args.seqs_per_flag(b)] : args.first + t;
+      x.known = position >= 0 && position < args.n_positions;
+      x.row = args.table + (x.known ? position : 0) * R;
+    }
   }
-  const int64_t position = args.positions != nullptr ? args.positions[t * args.n_flags + b / args.seqs_per_flag] : args.first + t;
-  const bool known = position >= 0 && position < args.n_positions;
-  const float* row = args.table + (known ? position : 0) * R;
-  auto turn = [&](float x1, float x2, int i, float& y1, float& y2) {
-    float c = row[i], s = row[half + i];
-    if (args.inverse) s = -s;
-    if (!known) c = s = __builtin_nanf("");
-    y1 = x1 * c - x2 * s;
-    y2 = x1 * s + x2 * c;
-  };
-  if constexpr (INTERLEAVED && E > 1) {
-    const uint32_t c = item * E;
-    Piece<T, E> p = get<T, E>(in + c);
 #pragma unroll
-    for (int k = 0; k < E; k += 2) {
-      if ((int)c + k >= R) break;
-      float y1, y2;
-      turn(widen(p.v[k]), widen(p.v[k + 1]), ((int)c + k) / 2, y1, y2);
-      p.v[k] = narrow<T>(y1);
-      p.v[k + 1] = narrow<T>(y2);
-    }
-    put<T, E>(out + c, p);
-  } else {
-    const uint32_t c1 = INTERLEAVED ? 2 * item : item * E, c2 = INTERLEAVED ? c1 + 1 : c1 + half;
-    Piece<T, E> p1 = get<T, E>(in + c1), p2 = get<T, E>(in + c2);
+  for (int u = 0; u < kItems; ++u) {
+    Item& x = it[u];
+    if (!x.on) continue;
+    if (x.first_pair >= 0) {
+      float cosine[kPairs], sine[kPairs];
+      load_row<kPairs>(cosine, x.row, x.first_pair, half, args.table_wide);
+      load_row<kPairs>(sine, x.row + half, x.first_pair, half, args.table_wide);
 #pragma unroll
-    for (int k = 0; k < E; ++k) {
-      float y1, y2;
-      turn(widen(p1.v[k]), widen(p2.v[k]), (int)item * E + k, y1, y2);
-      p1.v[k] = narrow<T>(y1);
-      p2.v[k] = narrow<T>(y2);
+      for (int k = 0; k < kPairs; ++k) {
+        if (kPairsInside && x.first_pair + k >= half) break;
+        float c = cosine[k], s = sine[k];
+        if (args.inverse) s = -s;
+        if (!x.known) c = s = __builtin_nanf("");
+        T& v1 = kPairsInside ? x.p1.v[2 * k] : x.p1.v[k];
+        T& v2 = kPairsInside ? x.p1.v[2 * k + 1] : x.p2.v[k];
+        const float x1 = widen(v1), x2 = widen(v2);
+        v1 = narrow<T>(x1 * c - x2 * s);
+        v2 = narrow<T>(x1 * s + x2 * c);
+      }
+      if (!kPairsInside) put<T, E>(x.out + x.c2, x.p2);
     }
-    put<T, E>(out + c1, p1);
-    put<T, E>(out + c2, p2);
+    put<T, E>(x.out + x.c1, x.p1);
   }
 }
 
 template <class T, int E>
 int32_t rotate(RotaryArgs a, bool interleaved, hipStream_t s) {
-  a.pair_items = interleaved && E > 1 ? ((uint32_t)a.rotary + E - 1) / E : (uint32_t)a.rotary / 2 / E;
-  a.items = interleaved && E > 1 ? a.dim / E : a.pair_items + (a.dim - a.rotary) / E;
-  const int64_t total = a.tokens * (a.heads[0] + a.heads[1]) * a.items, blocks = (total + 255) / 256;
+  const bool inside = interleaved && E > 1;
+  a.pair_items = inside ? ((uint32_t)a.rotary + E - 1) / E : (uint32_t)a.rotary / 2 / E;
+  const uint32_t items = inside ? a.dim / E : a.pair_items + (a.dim - a.rotary) / E, per_token = (a.heads[0] + a.heads[1]) * items;
+  a.items = divisor(items);
+  a.per_token = divisor(per_token);
+  const int64_t blocks = (a.tokens * per_token + 256 * kItems - 1) / (256 * kItems);
   if (blocks >= ((int64_t)1 << 31)) return MARL_E_SIZE;
   if (interleaved) hipLaunchKernelGGL((rotary_kernel<T, E, true>), dim3((unsigned)blocks), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((rotary_kernel<T, E, false>), dim3((unsigned)blocks), dim3(256), 0, s, a);
@@ -184,10 +237,10 @@ int32_t marl_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, c
   if (dims == nullptr) return MARL_E_NULL;
   const marl_attention_dims& d = *dims;
   if (d.precision != 0 && d.precision != 1) return MARL_E_CONFIG;
-  if (d.n_steps < 0 || d.n_seqs < 0 || n_positions < 1) return MARL_E_SIZE;
+  if (d.n_steps < 0 || d.n_seqs < 0 || d.n_seqs > (1 << 30) || n_positions < 1) return MARL_E_SIZE;
   if (d.dim_k < 1 || d.dim_k > 1024 || rotary_dim < 2 || rotary_dim > d.dim_k) return MARL_E_SIZE;
   if (rotary_dim % 2 != 0 || interleaved < 0 || interleaved > 1 || inverse < 0 || inverse > 1) return MARL_E_CONFIG;
-  if (d.n_heads < 1 || d.n_heads > (1 << 15) || (k.data != nullptr && (d.n_kv_heads < 1 || d.n_kv_heads > (1 << 15)))) return MARL_E_CONFIG;
+  if (d.n_heads < 1 || d.n_heads > (1 << 14) || (k.data != nullptr && (d.n_kv_heads < 1 || d.n_kv_heads > (1 << 14)))) return MARL_E_CONFIG;
   if (d.seqs_per_flag < 1 || d.n_seqs % d.seqs_per_flag != 0) return MARL_E_CONFIG;
   RotaryArgs a{};
   a.tokens = (int64_t)d.n_steps * d.n_seqs;
@@ -214,12 +267,13 @@ int32_t marl_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, c
   a.rotary = rotary_dim;
   a.first = first_position;
   a.inverse = inverse;
-  a.B = (uint32_t)d.n_seqs;
+  a.B = divisor((uint32_t)d.n_seqs);
   a.heads[0] = (uint32_t)d.n_heads;
   a.heads[1] = n == 2 ? (uint32_t)d.n_kv_heads : 0;
-  a.seqs_per_flag = (uint32_t)d.seqs_per_flag;
+  a.seqs_per_flag = divisor((uint32_t)d.seqs_per_flag);
   a.n_flags = (uint32_t)(d.n_seqs / d.seqs_per_flag);
   a.dim = (uint32_t)d.dim_k;
+  a.table_wide = rotary_dim % 8 == 0;
   const int E = 16 / elem;
   const bool wide = (low & 15u) == 0 && d.dim_k % E == 0 && (interleaved ? true : rotary_dim / 2 % E == 0);
   hipStream_t s = (hipStream_t)stream;
