@@ -338,128 +338,161 @@ def train_step(cfg, state, params, traj, adam_m, adam_v, counters, perm, stats, 
 # Arrays are [T][B][heads][D] tensors (fp32 or bf16), any strides with the last dimension contiguous; B = environments * agents, the agents of an
 # environment side by side, and `done` [T][environments] uint8.
 _PRECISION = {torch.float32: 0, torch.bfloat16: 1}
+_VIEW, _DIMS = struct.Struct("=Q3q"), struct.Struct("=8if")
+assert _VIEW.size == C.sizeof(View) and _DIMS.size == C.sizeof(AttentionDims)
 
 
-def _refuse(condition, what):
-    if condition:
-        raise MarlError(f"marl error -3: {what}")
+def _refused(what):
+    return MarlError(f"marl error -3: {what}")
 
 
+# (What follows runs in front of every call, which for a single step takes as long as the kernel: comparisons first, words only for a refusal.)
 def _floats(t, shape, name):
     """Pointer of an optional contiguous fp32 tensor of this shape."""
     if t is None:
         return None
-    _refuse(t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous(), f"{name}: contiguous float32 {list(shape)}")
+    if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+        raise _refused(f"{name}: contiguous float32 {list(shape)} on the GPU")
     return t.data_ptr()
 
 
 def _view(t, shape, dtype, name):
-    _refuse(t.dtype != dtype or tuple(t.shape) != tuple(shape), f"{name}: {dtype} {list(shape)}")
-    s = t.stride()
-    _refuse(s[3] != 1 and shape[3] > 1, f"{name}: the last dimension is contiguous")
-    return View(t.data_ptr(), s[0], s[1], s[2])
+    if t.dtype != dtype or t.shape != shape or not t.is_cuda:
+        raise _refused(f"{name}: {dtype} {list(shape)} on the GPU")
+    step, seq, head, last = t.stride()
+    if last != 1 and shape[3] > 1:
+        raise _refused(f"{name}: the last dimension is contiguous")
+    return View.from_buffer_copy(_VIEW.pack(t.data_ptr(), step, seq, head))
 
 
-def _flags(t, T, B, name):
-    """(pointer, sequences that share a flag) of flags [T][environments]."""
+def _step_view(t, shape, dtype, name):
+    """Of one step, [B][heads][D]"""
+    if t.dtype != dtype or t.shape != shape or not t.is_cuda:
+        raise _refused(f"{name}: {dtype} {list(shape)} on the GPU")
+    seq, head, last = t.stride()
+    if last != 1 and shape[2] > 1:
+        raise _refused(f"{name}: the last dimension is contiguous")
+    return View.from_buffer_copy(_VIEW.pack(t.data_ptr(), 0, seq, head))
+
+
+def _flags(t, lead, B, name):
+    """(pointer, sequences that share a flag) of flags [environments], behind the dimensions `lead`."""
     if t is None:
         return None, 1
-    _refuse(t.dtype not in (torch.uint8, torch.bool) or t.dim() != 2 or not t.is_contiguous() or t.shape[0] != T, f"{name}: contiguous uint8 [{T}][environments]")
-    n = t.shape[1]
-    _refuse(n == 0 and B > 0 or n > 0 and B % n != 0, f"{name}: {B} sequences do not share {n} flags")
-    return t.data_ptr(), max(B // n, 1) if n else 1
+    n = t.shape[-1]
+    if t.dtype not in (torch.uint8, torch.bool) or t.shape[:-1] != lead or not t.is_contiguous() or not t.is_cuda:
+        raise _refused(f"{name}: contiguous uint8 {list(lead)}[environments] on the GPU")
+    if B == 0:
+        return t.data_ptr(), 1
+    if n == 0 or B % n:
+        raise _refused(f"{name}: {B} sequences do not share {n} flags")
+    return t.data_ptr(), B // n
 
 
-def _attention(q, k, v, flags, scale, name="done"):
-    """(dims, shapes of q / k / v / out, dtype, flags' pointer)"""
-    _refuse(q.dtype not in _PRECISION, "q: float32 or bfloat16")
-    _refuse(q.dim() != 4 or k.dim() != 4 or v.dim() != 4, "q, k, v: [T][B][heads][D]")
-    (T, B, H, Dk), (Hk, Dv) = q.shape, v.shape[2:]
-    ptr, per = _flags(flags, T, B, name)
-    dims = AttentionDims(_PRECISION[q.dtype], T, B, H, Hk, Dk, Dv, per, scale)
-    return dims, ((T, B, H, Dk), (T, B, Hk, Dk), (T, B, Hk, Dv), (T, B, H, Dv)), q.dtype, ptr
+def _attention_dims(q, k, v, flags, scale):
+    """(dims, T, B, H, Hk, Dk, Dv, flags' pointer) of arrays [T][B][heads][D]"""
+    precision = _PRECISION.get(q.dtype)
+    if precision is None or q.dim() != 4 or v.dim() != 4 or k.dim() != 4:
+        raise _refused("q, k, v: float32 or bfloat16 [T][B][heads][D]")
+    T, B, H, Dk = q.shape
+    _, _, Hk, Dv = v.shape
+    ptr, per = _flags(flags, (T,), B, "done")
+    return AttentionDims.from_buffer_copy(_DIMS.pack(precision, T, B, H, Hk, Dk, Dv, per, scale)), T, B, H, Hk, Dk, Dv, ptr
 
 
 def linear_attention_workspace(q, k, v, backward=False):
+    """Bytes of workspace that linear_attention, or its gradient, needs for arrays of these shapes."""
     n = C.c_int64()
-    dims = _attention(q, k, v, None, 1.0)[0]
-    _check(lib().marl_linear_attention_workspace(C.byref(dims), int(backward), C.byref(n)))
+    _check(lib().marl_linear_attention_workspace(C.byref(_attention_dims(q, k, v, None, 1.0)[0]), int(backward), C.byref(n)))
     return n.value
 
 
 def _workspace(t, need):
-    _refuse(t is not None and t.numel() * t.element_size() < need or t is None and need > 0, f"workspace: {need} bytes")
+    if t is None:
+        if need > 0:
+            raise _refused(f"workspace: {need} bytes")
+        return None
+    if t.nbytes < need:
+        raise _refused(f"workspace: {need} bytes")
     return _ptr(t)
 
 
 def linear_attention(q, k, v, decay, out, workspace=None, state=None, next_state=None, done=None, scale=1.0, stream=None):
     """out [T][B][Hq][Dv] and next_state [B][Hq][Dk][Dv] of linear attention with decay[h] per head, episodes ending where done is nonzero."""
-    dims, (qs, ks, vs, os), dt, flags = _attention(q, k, v, done, scale)
-    state_shape = (qs[1], qs[2], qs[3], vs[3])
-    need = C.c_int64()
-    _check(lib().marl_linear_attention_workspace(C.byref(dims), 0, C.byref(need)))
-    _check(lib().marl_linear_attention(C.byref(dims), _view(q, qs, dt, "q"), _view(k, ks, dt, "k"), _view(v, vs, dt, "v"),
-                                       _floats(decay, qs[2:3], "decay"), _floats(state, state_shape, "state"), flags,
-                                       _view(out, os, dt, "out"), _floats(next_state, state_shape, "next_state"),
-                                       _workspace(workspace, need.value), _stream(stream)))
+    dims, T, B, H, Hk, Dk, Dv, flags = _attention_dims(q, k, v, done, scale)
+    dt, states, need, L = q.dtype, (B, H, Dk, Dv), C.c_int64(), lib()
+    _check(L.marl_linear_attention_workspace(C.byref(dims), 0, C.byref(need)))
+    _check(L.marl_linear_attention(C.byref(dims), _view(q, (T, B, H, Dk), dt, "q"), _view(k, (T, B, Hk, Dk), dt, "k"),
+                                   _view(v, (T, B, Hk, Dv), dt, "v"), _floats(decay, (H,), "decay"), _floats(state, states, "state"), flags,
+                                   _view(out, (T, B, H, Dv), dt, "out"), _floats(next_state, states, "next_state"),
+                                   _workspace(workspace, need.value), _stream(stream)))
 
 
 def linear_attention_backward(q, k, v, decay, dout, dq, dk, dv, workspace=None, state=None, dnext_state=None, dstate=None, done=None, scale=1.0,
                               stream=None):
     """Gradients dq, dk, dv and dstate of linear_attention from dout and dnext_state."""
-    dims, (qs, ks, vs, os), dt, flags = _attention(q, k, v, done, scale)
-    state_shape = (qs[1], qs[2], qs[3], vs[3])
-    need = C.c_int64()
-    _check(lib().marl_linear_attention_workspace(C.byref(dims), 1, C.byref(need)))
-    _check(lib().marl_linear_attention_backward(
-        C.byref(dims), _view(q, qs, dt, "q"), _view(k, ks, dt, "k"), _view(v, vs, dt, "v"), _floats(decay, qs[2:3], "decay"),
-        _floats(state, state_shape, "state"), flags, _view(dout, os, dt, "dout"), _floats(dnext_state, state_shape, "dnext_state"),
-        _view(dq, qs, dt, "dq"), _view(dk, ks, dt, "dk"), _view(dv, vs, dt, "dv"), _floats(dstate, state_shape, "dstate"),
-        _workspace(workspace, need.value), _stream(stream)))
+    dims, T, B, H, Hk, Dk, Dv, flags = _attention_dims(q, k, v, done, scale)
+    dt, states, need, L = q.dtype, (B, H, Dk, Dv), C.c_int64(), lib()
+    qs, ks, vs, os = (T, B, H, Dk), (T, B, Hk, Dk), (T, B, Hk, Dv), (T, B, H, Dv)
+    _check(L.marl_linear_attention_workspace(C.byref(dims), 1, C.byref(need)))
+    _check(L.marl_linear_attention_backward(
+        C.byref(dims), _view(q, qs, dt, "q"), _view(k, ks, dt, "k"), _view(v, vs, dt, "v"), _floats(decay, (H,), "decay"),
+        _floats(state, states, "state"), flags, _view(dout, os, dt, "dout"), _floats(dnext_state, states, "dnext_state"), _view(dq, qs, dt, "dq"),
+        _view(dk, ks, dt, "dk"), _view(dv, vs, dt, "dv"), _floats(dstate, states, "dstate"), _workspace(workspace, need.value), _stream(stream)))
 
 
 def linear_attention_step(q, k, v, decay, state, out, next_state=None, done=None, scale=1.0, stream=None):
     """One step: q [B][Hq][Dk], k, v [B][Hk][D], out [B][Hq][Dv]; done [environments]: of the step before (the state is cleared).  The state is
     updated in place unless next_state is given."""
-    one = lambda t: t.unsqueeze(0)
-    _refuse(q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or out.dim() != 3, "q, k, v, out: [B][heads][D]")
-    dims, (qs, ks, vs, os), dt, flags = _attention(one(q), one(k), one(v), None if done is None else one(done), scale)
-    state_shape = (qs[1], qs[2], qs[3], vs[3])
+    precision, dt = _PRECISION.get(q.dtype), q.dtype
+    if precision is None or q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        raise _refused("q, k, v: float32 or bfloat16 [B][heads][D]")
+    B, H, Dk = q.shape
+    _, Hk, Dv = v.shape
+    flags, per = _flags(done, (), B, "done")
+    dims, states = AttentionDims.from_buffer_copy(_DIMS.pack(precision, 1, B, H, Hk, Dk, Dv, per, scale)), (B, H, Dk, Dv)
+    before = _floats(state, states, "state")
     _check(lib().marl_linear_attention_step(
-        C.byref(dims), _view(one(q), qs, dt, "q"), _view(one(k), ks, dt, "k"), _view(one(v), vs, dt, "v"), _floats(decay, qs[2:3], "decay"),
-        _floats(state, state_shape, "state"), flags, _view(one(out), os, dt, "out"),
-        _floats(state if next_state is None else next_state, state_shape, "next_state"), _stream(stream)))
+        C.byref(dims), _step_view(q, (B, H, Dk), dt, "q"), _step_view(k, (B, Hk, Dk), dt, "k"), _step_view(v, (B, Hk, Dv), dt, "v"),
+        _floats(decay, (H,), "decay"), before, flags, _step_view(out, (B, H, Dv), dt, "out"),
+        before if next_state is None else _floats(next_state, states, "next_state"), _stream(stream)))
 
 
-def _rows(t, n, width, dtype, name):
-    _refuse(t.dtype != dtype or tuple(t.shape) != (n, width) or (width > 1 and t.stride(1) != 1), f"{name}: {dtype} [{n}][{width}], rows contiguous")
+def _rows(t, shape, dtype, name):
+    if t.dtype != dtype or t.shape != shape or shape[1] > 1 and t.stride(1) != 1 or not t.is_cuda:
+        raise _refused(f"{name}: {dtype} {list(shape)} on the GPU, rows contiguous")
     return t.data_ptr(), t.stride(0)
 
 
 def layer_norm(x, weight, bias, out, mean=None, rstd=None, eps=1e-5, stream=None):
     """out = (x - mean) * rstd * weight + bias over the rows of x [rows][width]; weight, bias, mean, rstd may be None."""
-    _refuse(x.dtype not in _PRECISION or x.dim() != 2, "x: float32 or bfloat16 [rows][width]")
-    n, width = x.shape
-    _check(lib().marl_layer_norm(_PRECISION[x.dtype], n, width, *_rows(x, n, width, x.dtype, "x"), _floats(weight, (width,), "weight"),
-                                 _floats(bias, (width,), "bias"), eps, *_rows(out, n, width, x.dtype, "out"), _floats(mean, (n,), "mean"),
+    precision, dt = _PRECISION.get(x.dtype), x.dtype
+    if precision is None or x.dim() != 2:
+        raise _refused("x: float32 or bfloat16 [rows][width]")
+    shape = n, width = x.shape
+    _check(lib().marl_layer_norm(precision, n, width, *_rows(x, shape, dt, "x"), _floats(weight, (width,), "weight"),
+                                 _floats(bias, (width,), "bias"), eps, *_rows(out, shape, dt, "out"), _floats(mean, (n,), "mean"),
                                  _floats(rstd, (n,), "rstd"), _stream(stream)))
 
 
 def layer_norm_workspace(rows, width):
+    """Bytes of workspace that the gradient of layer_norm needs."""
     n = C.c_int64()
-    _check(lib().marl_layer_norm_workspace(int(rows), int(width), C.byref(n)))
+    _check(lib().marl_layer_norm_workspace(rows, width, C.byref(n)))
     return n.value
 
 
 def layer_norm_backward(dout, x, weight, mean, rstd, dx, dweight=None, dbias=None, workspace=None, stream=None):
     """dx, and the column sums dweight, dbias (may be None), from dout and what layer_norm kept."""
-    _refuse(x.dtype not in _PRECISION or x.dim() != 2, "x: float32 or bfloat16 [rows][width]")
-    n, width = x.shape
-    need = layer_norm_workspace(n, width) if dweight is not None or dbias is not None else 0
+    precision, dt = _PRECISION.get(x.dtype), x.dtype
+    if precision is None or x.dim() != 2:
+        raise _refused("x: float32 or bfloat16 [rows][width]")
+    shape = n, width = x.shape
+    need = 0 if dweight is None and dbias is None else layer_norm_workspace(n, width)
     _check(lib().marl_layer_norm_backward(
-        _PRECISION[x.dtype], n, width, *_rows(dout, n, width, x.dtype, "dout"), *_rows(x, n, width, x.dtype, "x"),
-        _floats(weight, (width,), "weight"), _floats(mean, (n,), "mean"), _floats(rstd, (n,), "rstd"), *_rows(dx, n, width, x.dtype, "dx"),
-        _floats(dweight, (width,), "dweight"), _floats(dbias, (width,), "dbias"), _workspace(workspace, need), _stream(stream)))
+        precision, n, width, *_rows(dout, shape, dt, "dout"), *_rows(x, shape, dt, "x"), _floats(weight, (width,), "weight"),
+        _floats(mean, (n,), "mean"), _floats(rstd, (n,), "rstd"), *_rows(dx, shape, dt, "dx"), _floats(dweight, (width,), "dweight"),
+        _floats(dbias, (width,), "dbias"), _workspace(workspace, need), _stream(stream)))
 
 
 ROTARY_SCALING = {None: 0, "linear": 1, "base": 2, "by_turns": 3}
@@ -476,22 +509,26 @@ def rotary_table(n_positions, rotary_dim, base=10000.0, scaling=None, factor=1.0
 def rotary(q, k, table, q_out, k_out, positions=None, first_position=0, interleaved=False, inverse=False, stream=None):
     """Rotates the first table.shape[1] elements of every head of q and k (k, k_out may be None) by positions [T][environments] int32, or by
     first_position + t.  The outputs may be the inputs.  inverse: the gradient."""
-    _refuse(q.dtype not in _PRECISION or q.dim() != 4, "q: float32 or bfloat16 [T][B][heads][D]")
-    T, B, H, D = q.shape
+    precision, dt = _PRECISION.get(q.dtype), q.dtype
+    if precision is None or q.dim() != 4 or k is not None and k.dim() != 4:
+        raise _refused("q, k: float32 or bfloat16 [T][B][heads][D]")
+    qs = T, B, H, D = q.shape
     Hk = 1 if k is None else k.shape[2]
-    _refuse(table.dim() != 2, "table: [positions][rotary_dim]")
-    per = 1
+    ks = T, B, Hk, D
+    if table.dim() != 2:
+        raise _refused("table: [positions][rotary_dim]")
+    P, R = table.shape
+    at, per = None, 1
     if positions is not None:
-        _refuse(positions.dtype != torch.int32 or positions.dim() != 2 or not positions.is_contiguous() or positions.shape[0] != T or
-                (positions.shape[1] == 0 if B else False) or (B % positions.shape[1] if B else 0), f"positions: contiguous int32 [{T}][environments]")
-        per = max(B // positions.shape[1], 1) if B else 1
-    dims = AttentionDims(_PRECISION[q.dtype], T, B, H, Hk, D, D, per, 1.0)
-    none = View(None, 0, 0, 0)
+        n = positions.shape[-1]
+        if positions.dtype != torch.int32 or positions.shape[:-1] != (T,) or not positions.is_contiguous() or not positions.is_cuda or B and (n == 0 or B % n):
+            raise _refused(f"positions: contiguous int32 [{T}][environments] of {B} sequences, on the GPU")
+        at, per = positions.data_ptr(), B // n if B else 1
+    none = View()
     _check(lib().marl_rotary(
-        C.byref(dims), _view(q, (T, B, H, D), q.dtype, "q"), none if k is None else _view(k, (T, B, Hk, D), q.dtype, "k"),
-        _floats(table, table.shape, "table"), table.shape[0], table.shape[1], None if positions is None else positions.data_ptr(),
-        int(first_position), int(interleaved), int(inverse), _view(q_out, (T, B, H, D), q.dtype, "q_out"),
-        none if k is None else _view(k_out, (T, B, Hk, D), q.dtype, "k_out"), _stream(stream)))
+        C.byref(AttentionDims.from_buffer_copy(_DIMS.pack(precision, T, B, H, Hk, D, D, per, 1.0))), _view(q, qs, dt, "q"),
+        none if k is None else _view(k, ks, dt, "k"), _floats(table, (P, R), "table"), P, R, at, first_position, interleaved, inverse,
+        _view(q_out, qs, dt, "q_out"), none if k is None else _view(k_out, ks, dt, "k_out"), _stream(stream)))
 
 
 KERNEL_CLASSES = {"gemm_nn": 0, "gemm_nt": 1, "gemm_tn": 2, "env_step": 3, "gae": 4, "fused_train": 5, "rollout": 6}

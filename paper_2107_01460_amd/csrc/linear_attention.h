@@ -399,6 +399,17 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 ? 2 : 3) s
   if constexpr (!STATE_ONLY) sx.begin(r.x, t0, tid, base);
   sy.begin(r.y, t0, tid, base);
   sz.begin(r.z, t0, tid, base);
+  char* to_out[StageZ::kSlots];  // of a thread's pieces of the output's tile
+  uint32_t out_on = 0;
+  if constexpr (!STATE_ONLY) {
+#pragma unroll
+    for (int s = 0; s < StageZ::kSlots; ++s) {
+      const int q = StageZ::index(s, tid);
+      to_out[s] = const_cast<char*>(base(r.out, StageZ::pair(q))) + (int64_t)(t0 + StageZ::row(q)) * r.out.step + StageZ::piece(q) * 16;
+      if ((StageZ::kAll % kThreads == 0 || s * kThreads + tid < StageZ::kAll) && StageZ::piece(q) * E < Dz) out_on |= 1u << s;
+    }
+  }
+  const int64_t out_way = tile_way * r.out.step;
   uint8_t flag = 0;
   auto request = [&](int t) {
     const int n = min(kTile, t_end - t);
@@ -502,18 +513,20 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 ? 2 : 3) s
 #pragma unroll
             for (int v = 0; v <= u; ++v) score[u][v] *= u == v ? near : far;
           } else {
-            const int ti = block_at(u) + fresh(i), g4 = 4 * fresh(g);
+            // step ti sees the steps from the last end before it on; in a reverse scan up to the first end from it on
+            const int ti = block_at(u) + fresh(i);
             const uint32_t between = reverse ? ends >> ti : ends & ((1u << ti) - 1u);
+            const int edge = (reverse ? ti + __builtin_ctz(between | 0x80000000u) : 32 - __clz(between)) - 4 * g;
+            const bool clear = between == 0;
 #pragma unroll
             for (int c = 0; c < NV; ++c)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[u][c][e] = between == 0 ? o[u][c][e] * to : 0.f;
+              for (int e = 0; e < 4; ++e) o[u][c][e] = clear ? o[u][c][e] * to : 0.f;
 #pragma unroll
             for (int v = 0; v <= u; ++v)
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const int tj = block_at(v) + g4 + e, lo = min(ti, tj), hi = max(ti, tj);
-                const bool seen = ((ends & ((1u << hi) - 1u)) >> lo) == 0;
+                const bool seen = reverse ? clear || block_at(v) + e <= edge : block_at(v) + e >= edge;
                 score[u][v][e] = seen ? score[u][v][e] * (u == v ? near[e] : far[e]) : 0.f;
               }
           }
@@ -578,14 +591,15 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 ? 2 : 3) s
         }
         if (n < kTile || ends != 0) {
           const int g4 = 4 * fresh(g);
+          // steps that reach the state that goes on: those behind the last end; in a reverse scan those up to the first
+          const int from = reverse || ends == 0 ? 0 : 32 - __builtin_clz(ends), to = reverse && ends != 0 ? __builtin_ctz(ends) : kTile;
 #pragma unroll
           for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int tj = block_at(u) + g4 + e;
               if (!reverse && n < kTile) w[u][e] = tj < n ? r.update * power[n - 1 - tj] : 0.f;
-              const uint32_t between = reverse ? ends & ((1u << tj) - 1u) : ends >> tj;
-              if (between != 0) w[u][e] = 0.f;
+              if (tj < from || tj > to) w[u][e] = 0.f;
             }
         }
         if (ends != 0) {
@@ -636,12 +650,10 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 ? 2 : 3) s
 #pragma unroll
         for (int s = 0; s < StageZ::kSlots; ++s) {
           const int q = StageZ::index(s, tid), row = StageZ::row(q), piece = StageZ::piece(q), which = StageZ::pair(q);
-          const bool on = (StageZ::kAll % kThreads == 0 || s * kThreads + tid < StageZ::kAll) && row < n && piece * E < Dz &&
-                          lds_left[which * SL + piece * E / (16 * NV)] == 0;
-          if (on) {
-            const uint4 v = *reinterpret_cast<const uint4*>(lds_o + ((which * kTile + row) * kPiecesZ + (piece ^ swizzle<kPiecesZ>(row))) * 16);
-            *reinterpret_cast<uint4*>(const_cast<char*>(base(r.out, which)) + (int64_t)(t0 + row) * r.out.step + piece * 16) = v;
-          }
+          if ((out_on >> s & 1u) && row < n && lds_left[which * SL + piece * E / (16 * NV)] == 0)
+            *reinterpret_cast<uint4*>(to_out[s]) =
+                *reinterpret_cast<const uint4*>(lds_o + ((which * kTile + row) * kPiecesZ + (piece ^ swizzle<kPiecesZ>(row))) * 16);
+          to_out[s] += out_way;
         }
       }
     }

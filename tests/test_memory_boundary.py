@@ -120,28 +120,43 @@ def test_rotary_arguments(M):
     assert L.marl_rotary_table(None, GOOD, None) == NULL
 
 
-def test_tensors_that_do_not_fit_are_refused(M):
-    """Shapes, types and workspaces are compared before the library is called."""
-    q, k = torch.zeros(4, 6, 4, 16), torch.zeros(4, 6, 2, 16)
-    decay, out = torch.ones(4), torch.zeros(4, 6, 4, 16)
-    good = dict(q=q, k=k, v=k, decay=decay, out=out)
+def refusals(M, device):
+    """Calls whose tensors do not fit: shapes, types, strides, workspaces, compared before the library is called."""
+    new = lambda *s, **kw: torch.zeros(*s, device=device, **kw)
+    q, k = new(4, 6, 4, 16), new(4, 6, 2, 16)
+    decay, out = new(4), new(4, 6, 4, 16)
+    u8 = lambda *s: new(*s, dtype=torch.uint8)
     for change in (dict(q=q.half()), dict(q=q[0]), dict(k=k[:3]), dict(v=k.bfloat16()), dict(decay=decay[:3]), dict(decay=decay.double()), dict(out=out[..., :8]),
-                   dict(q=q.transpose(2, 3)), dict(state=torch.zeros(6, 4, 16, 15)), dict(done=torch.zeros(4, 4, dtype=torch.uint8)),
-                   dict(done=torch.zeros(3, 6, dtype=torch.uint8)), dict(done=torch.zeros(4, 6)), dict(next_state=torch.zeros(6, 4, 16, 16).transpose(0, 1))):
-        with pytest.raises(M.MarlError):
-            M.linear_attention(**{**good, **change})
-    with pytest.raises(M.MarlError):   # long: needs a workspace
-        M.linear_attention(torch.zeros(4096, 1, 1, 16), *[torch.zeros(4096, 1, 1, 16)] * 2, decay[:1], torch.zeros(4096, 1, 1, 16))
-    x = torch.zeros(5, 8)
-    for args in ((x.half(), None, None, x), (x, torch.ones(7), None, x), (x, None, None, x[:4]), (x.t(), None, None, x.t())):
-        with pytest.raises(M.MarlError):
-            M.layer_norm(*args)
-    with pytest.raises(M.MarlError):
-        M.layer_norm_backward(x, x, None, torch.zeros(5), torch.zeros(5), x.clone(), torch.zeros(8), None, torch.zeros(4, dtype=torch.uint8))
-    table = torch.zeros(9, 8)
-    for change in (dict(table=table[0]), dict(positions=torch.zeros(4, 6)), dict(positions=torch.zeros(4, 5, dtype=torch.int32)), dict(q_out=out.bfloat16())):
-        with pytest.raises(M.MarlError):
-            M.rotary(**{**dict(q=q, k=k, table=table, q_out=out, k_out=torch.zeros_like(k)), **change})
+                   dict(q=q.transpose(2, 3)), dict(state=new(6, 4, 16, 15)), dict(done=u8(4, 4)), dict(done=u8(3, 6)), dict(done=new(4, 6)),
+                   dict(next_state=new(4, 6, 16, 16).transpose(0, 1))):
+        yield lambda c=change: M.linear_attention(**{**dict(q=q, k=k, v=k, decay=decay, out=out), **c})
+    yield lambda: M.linear_attention(new(4096, 1, 1, 16), *[new(4096, 1, 1, 16)] * 2, decay[:1], new(4096, 1, 1, 16))   # long: needs a workspace
+    yield lambda: M.linear_attention_backward(q, k, k, decay, out, q.clone(), k.clone(), k.clone(), u8(64))                # shared heads: too small a one
+    for change in (dict(q=q), dict(state=new(6, 4, 16, 8)), dict(done=u8(4)), dict(done=u8(1, 6)), dict(out=out[0, :, :3]), dict(k=k[0].half())):
+        yield lambda c=change: M.linear_attention_step(**{**dict(q=q[0], k=k[0], v=k[0], decay=decay, state=new(6, 4, 16, 16), out=out[0]), **c})
+    x = new(5, 8)
+    for args in ((x.half(), None, None, x), (x, new(7), None, x), (x, None, None, x[:4]), (x.t(), None, None, x.t()), (x, None, new(8).double(), x)):
+        yield lambda a=args: M.layer_norm(*a)
+    yield lambda: M.layer_norm_backward(x, x, None, new(5), new(5), x.clone(), new(8), None, u8(4))
+    yield lambda: M.layer_norm_backward(x, x, None, new(4), new(5), x.clone())
+    table = new(9, 8)
+    for change in (dict(table=table[0]), dict(positions=new(4, 6)), dict(positions=new(4, 5, dtype=torch.int32)), dict(q_out=out.bfloat16()), dict(k=k[0])):
+        yield lambda c=change: M.rotary(**{**dict(q=q, k=k, table=table, q_out=out, k_out=k.clone()), **c})
+
+
+@pytest.mark.gpu
+def test_tensors_that_do_not_fit_are_refused(M):
+    for call in refusals(M, "cuda"):
+        with pytest.raises(M.MarlError, match="marl error -3"):
+            call()
+
+
+def test_tensors_in_host_memory_are_refused(M):
+    q, x = torch.zeros(4, 6, 4, 16), torch.zeros(5, 8)
+    for call in (lambda: M.linear_attention(q, q, q, torch.ones(4), q.clone()), lambda: M.layer_norm(x, None, None, x), lambda: M.rotary(q, None, x, q, None),
+                 lambda: M.linear_attention_step(q[0], q[0], q[0], torch.ones(4), torch.zeros(6, 4, 16, 16), q[0].clone())):
+        with pytest.raises(M.MarlError, match="on the GPU"):
+            call()
 
 
 @pytest.fixture(scope="module")
