@@ -248,17 +248,19 @@ struct Stage {
   static constexpr int kAll = PIECES * P * TILE, kSlots = (kAll + THREADS - 1) / THREADS;
   const char* from[kSlots];  // of the piece in the tile that is fetched next
   uint4 v[kSlots];
+  uint32_t past = 0;         // pieces past the array's columns: their loads go to column 0, zeros go to LDS
   static __device__ __forceinline__ int index(int s, int tid) { return min(s * THREADS + tid, kAll - 1); }
   static __device__ __forceinline__ int piece(int q) { return q % PIECES; }
   static __device__ __forceinline__ int pair(int q) { return q / PIECES % P; }
   static __device__ __forceinline__ int row(int q) { return q / (PIECES * P); }
-  // A piece past the array's columns: its loads go to column 0, zeros go to LDS
   template <class Base>
   __device__ __forceinline__ void begin(const ScanArray& a, int t0, int tid, Base base) {
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
       const int q = index(s, tid);
-      from[s] = base(a, pair(q)) + (int64_t)(t0 + row(q)) * a.step + (piece(q) * (int)(16 / sizeof(T)) < a.dim ? piece(q) * 16 : 0);
+      const bool in = piece(q) * (int)(16 / sizeof(T)) < a.dim;
+      from[s] = base(a, pair(q)) + (int64_t)(t0 + row(q)) * a.step + (in ? piece(q) * 16 : 0);
+      if (!in) past |= 1u << s;
     }
   }
   __device__ __forceinline__ void request(const ScanArray& a, int n, int64_t next, int tid) {  // n: steps in the tile; next: bytes to the tile after
@@ -286,14 +288,12 @@ struct Stage {
     }
   }
   __device__ __forceinline__ void to_lds(char* tile, const ScanArray& a, int n, int tid) {
-    const bool some = n < TILE || PIECES * (int)(16 / sizeof(T)) > a.dim;
+    const bool padded = PIECES * (int)(16 / sizeof(T)) > a.dim;
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
       const int q = index(s, tid), at = row(q);
-      if (some) {
-        const int p = index(s, fresh(tid));
-        if (row(p) >= n || piece(p) * (int)(16 / sizeof(T)) >= a.dim) v[s] = make_uint4(0, 0, 0, 0);
-      }
+      if (padded && (past >> s & 1u)) v[s] = make_uint4(0, 0, 0, 0);
+      if (n < TILE && row(index(s, fresh(tid))) >= n) v[s] = make_uint4(0, 0, 0, 0);
       if (kAll % THREADS == 0 || s * THREADS + tid < kAll)
         *reinterpret_cast<uint4*>(tile + ((pair(q) * TILE + at) * PIECES + (piece(q) ^ swizzle<PIECES>(at))) * 16) = v[s];
     }
@@ -323,7 +323,7 @@ template <int SL>
 constexpr int scan_pairs() { return SL == 1 ? 4 : SL == 2 ? 2 : 1; }  // (sequence, head) pairs of a workgroup
 
 template <class T, int NK, int NV, int SL, bool STATE_ONLY, bool WIDE>
-__global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 ? 2 : 3) scan_kernel(const ScanArgs args) {
+__global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 || (NK == 4 && SL == 1) ? 2 : 3) scan_kernel(const ScanArgs args) {
   typedef ScanTraits<T> Tr;
   typedef typename Tr::Frag Frag;
   constexpr int U = Tr::kSub, kTile = 16 * U, P = scan_pairs<SL>(), kThreads = 64 * SL * P, E = 16 / sizeof(T);

@@ -1,4 +1,6 @@
 // Linear attention: the calls, the join of the stretches of a long sequence, the sum over shared heads, the single step.
+#include <type_traits>
+
 #include "linear_attention.h"
 
 namespace marl {
@@ -68,7 +70,7 @@ __global__ void __launch_bounds__(256) join_kernel(JoinArgs a0, JoinArgs a1, uin
   if (at >= total) return;
   const int64_t pair = at / size, e = at % size;
   float run = a.first == nullptr ? 0.f : a.first[at];
-  constexpr int kBatch = 8;
+  constexpr int kBatch = 32;  // loads on their way together
   for (int p0 = 0; p0 < a.n; p0 += kBatch) {
     float v[kBatch], c[kBatch];
 #pragma unroll
@@ -89,20 +91,31 @@ __global__ void __launch_bounds__(256) join_kernel(JoinArgs a0, JoinArgs a1, uin
 }
 
 // ---- the gradient of a shared head: the sum over its query heads -------------------------------------------------------------------
-template <class T>
+template <class T, int V>
 __global__ void __launch_bounds__(256) sum_heads_kernel(const float* __restrict__ part, T* __restrict__ out, int64_t step, int64_t seq, int64_t head,
-                                                        uint32_t B, uint32_t heads, uint32_t group, uint32_t dim, int64_t total) {
-  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (int64_t)gridDim.x * 256) {
-    const uint32_t d = at % dim;
-    const int64_t row = at / dim;   // (t, b, kv head)
-    const uint32_t h = row % heads;
-    const int64_t tb = row / heads;
-    const float* p = part + row * group * dim + d;
-    float s = 0.f;
-    for (uint32_t u = 0; u < group; ++u) s += p[(int64_t)u * dim];
-    T* o = out + tb / B * step + tb % B * seq + h * head + d;
-    if constexpr (sizeof(T) == 4) *o = s;
-    else *o = to_bf16(s);
+                                                        uint32_t B, uint32_t heads, uint32_t group, uint32_t dim) {
+  const uint32_t t = blockIdx.y, per_step = B * heads * (dim / V);
+  for (uint32_t at = blockIdx.x * 256 + threadIdx.x; at < per_step; at += gridDim.x * 256) {
+    const uint32_t row = at / (dim / V), d = (at - row * (dim / V)) * V;  // row: (sequence, kv head)
+    const uint32_t b = row / heads, h = row - b * heads;
+    const float* p = part + ((int64_t)t * B * heads + row) * group * dim + d;
+    float s[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) s[k] = 0.f;
+    for (uint32_t u = 0; u < group; ++u, p += dim) {
+      if constexpr (V == 4) {
+        const float4 f = *reinterpret_cast<const float4*>(p);
+        s[0] += f.x; s[1] += f.y; s[2] += f.z; s[3] += f.w;
+      } else {
+        s[0] += *p;
+      }
+    }
+    T* o = out + (int64_t)t * step + b * seq + h * head + d;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      if constexpr (sizeof(T) == 4) o[k] = s[k];
+      else o[k] = to_bf16(s[k]);
+    }
   }
 }
 
@@ -237,15 +250,21 @@ int32_t join(JoinArgs a0, JoinArgs a1, int n_args, const marl_attention_dims& d,
 }
 
 int32_t sum_heads(const marl_attention_dims& d, const Plan& p, const float* part, const marl_view& out, int dim, hipStream_t s) {
-  const int64_t total = (int64_t)d.n_steps * d.n_seqs * d.n_kv_heads * dim;
-  const int64_t want = (total + 255) / 256;
-  const dim3 grid((unsigned)(want < 16384 ? want : 16384));
-  if (d.precision == 0)
-    hipLaunchKernelGGL(sum_heads_kernel<float>, grid, dim3(256), 0, s, part, (float*)out.data, out.step, out.seq, out.head, (uint32_t)d.n_seqs,
-                       (uint32_t)d.n_kv_heads, (uint32_t)p.group, (uint32_t)dim, total);
-  else
-    hipLaunchKernelGGL(sum_heads_kernel<bf16_t>, grid, dim3(256), 0, s, part, (bf16_t*)out.data, out.step, out.seq, out.head, (uint32_t)d.n_seqs,
-                       (uint32_t)d.n_kv_heads, (uint32_t)p.group, (uint32_t)dim, total);
+  const int64_t per_step = (int64_t)d.n_seqs * d.n_kv_heads * dim;
+  if (per_step >= ((int64_t)1 << 31)) return MARL_E_SIZE;
+  auto launch = [&](auto zero, auto v) {
+    typedef decltype(zero) T;
+    constexpr int V = decltype(v)::value;
+    const int64_t want = (per_step / V + 255) / 256;
+    for (int32_t t = 0; t < d.n_steps; t += 65535) {  // (grid y)
+      const int32_t n = d.n_steps - t < 65535 ? d.n_steps - t : 65535;
+      hipLaunchKernelGGL((sum_heads_kernel<T, V>), dim3((unsigned)(want < 4096 ? want : 4096), (unsigned)n), dim3(256), 0, s,
+                         part + (int64_t)t * p.pairs * dim, (T*)out.data + t * out.step, out.step, out.seq, out.head, (uint32_t)d.n_seqs,
+                         (uint32_t)d.n_kv_heads, (uint32_t)p.group, (uint32_t)dim);
+    }
+  };
+  if (dim % 4 == 0) d.precision == 0 ? launch(0.f, std::integral_constant<int, 4>()) : launch((bf16_t)0, std::integral_constant<int, 4>());
+  else d.precision == 0 ? launch(0.f, std::integral_constant<int, 1>()) : launch((bf16_t)0, std::integral_constant<int, 1>());
   return launch_status();
 }
 
