@@ -12,3 +12,4 @@ from .binding import (  # noqa: F401
     layer_norm_workspace, rotary, rotary_table,
 )
 from .trainer import Trainer  # noqa: F401,E402
+from .memory import MemoryCritic, episode_positions  # noqa: F401,E402
