@@ -25,7 +25,6 @@ struct ScanArray {
   int64_t step, seq, head;  // bytes
   uint32_t share;           // query heads per head of this array
   int32_t dim;
-  int32_t wide;             // 16-byte accesses
 };
 
 // A state [rows][columns] fp32 of (sequence, query head) u and stretch of time p at data + (u * stretches + p) * size, element (r, c) at r * row + c * col
@@ -243,12 +242,36 @@ __device__ __forceinline__ shortx4 column(const bf16_t* tile, int row, int first
 }
 
 // ---- a workgroup's share of an array's tile: SLOTS pieces a thread, piece fastest, then head, then step ------------------------------------
-template <class T, int PIECES, int P, int TILE, int THREADS, bool WIDE>
+// Sixteen bytes at any element's address (the accesses of this target need no alignment)
+template <class P>
+__device__ __forceinline__ uint4 load16(const P* p) {
+  uint4 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+template <class P>
+__device__ __forceinline__ void store16(P* p, uint4 v) { __builtin_memcpy(p, &v, 16); }
+__device__ __forceinline__ uint4 shift_right(uint4 v, int bytes) {  // 1 .. 15
+  uint64_t lo = v.x | (uint64_t)v.y << 32, hi = v.z | (uint64_t)v.w << 32;
+  if (bytes < 8) {
+    lo = lo >> 8 * bytes | hi << (64 - 8 * bytes);
+    hi >>= 8 * bytes;
+  } else {
+    lo = hi >> (8 * bytes - 64);
+    hi = 0;
+  }
+  return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+}
+
+// WHOLE: the arrays' rows are whole pieces.
+template <class T, int PIECES, int P, int TILE, int THREADS, bool WHOLE>
 struct Stage {
-  static constexpr int kAll = PIECES * P * TILE, kSlots = (kAll + THREADS - 1) / THREADS;
+  static constexpr int E = 16 / sizeof(T), kAll = PIECES * P * TILE, kSlots = (kAll + THREADS - 1) / THREADS;
+  static constexpr bool kShort = !WHOLE && PIECES * E <= 16;  // rows may be shorter than sixteen bytes
   const char* from[kSlots];  // of the piece in the tile that is fetched next
   uint4 v[kSlots];
-  uint32_t past = 0;         // pieces past the array's columns: their loads go to column 0, zeros go to LDS
+  uint32_t past = 0;         // slots whose pieces lie past the array's columns: their loads go to column 0, zeros go to LDS
+  uint32_t last = 0;         // slots whose pieces are a row's last columns and fewer than sixteen bytes: the sixteen bytes that end with the row are loaded
   static __device__ __forceinline__ int index(int s, int tid) { return min(s * THREADS + tid, kAll - 1); }
   static __device__ __forceinline__ int piece(int q) { return q % PIECES; }
   static __device__ __forceinline__ int pair(int q) { return q / PIECES % P; }
@@ -257,10 +280,16 @@ struct Stage {
   __device__ __forceinline__ void begin(const ScanArray& a, int t0, int tid, Base base) {
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
-      const int q = index(s, tid);
-      const bool in = piece(q) * (int)(16 / sizeof(T)) < a.dim;
-      from[s] = base(a, pair(q)) + (int64_t)(t0 + row(q)) * a.step + (in ? piece(q) * 16 : 0);
-      if (!in) past |= 1u << s;
+      const int q = index(s, tid), in = a.dim - piece(q) * E;  // elements of the piece that there are
+      int first = piece(q) * E;
+      if (in <= 0) {
+        past |= 1u << s;
+        first = 0;
+      } else if (in < E) {
+        last |= 1u << s;
+        first = max(a.dim - E, 0);
+      }
+      from[s] = base(a, pair(q)) + (int64_t)(t0 + row(q)) * a.step + first * (int)sizeof(T);
     }
   }
   __device__ __forceinline__ void request(const ScanArray& a, int n, int64_t next, int tid) {  // n: steps in the tile; next: bytes to the tile after
@@ -271,27 +300,34 @@ struct Stage {
         const int at = row(index(s, fresh(tid)));
         p -= at < n ? 0 : (at - n + 1) * a.step;
       }
-      if constexpr (WIDE) {
-        v[s] = *reinterpret_cast<const uint4*>(p);
-      } else {
-        constexpr int E = 16 / sizeof(T);
-        const int in = a.dim - piece(index(s, fresh(tid))) * E;  // elements of the piece that there are
-        T e[E];
-#pragma unroll
-        for (int k = 0; k < E; ++k) e[k] = reinterpret_cast<const T*>(p)[k < in ? k : 0];
-#pragma unroll
-        for (int k = 0; k < E; ++k)
-          if (k >= in) e[k] = 0;
-        __builtin_memcpy(&v[s], e, 16);
+      if (!kShort || a.dim >= E) {
+        v[s] = load16(p);
+      } else {  // a row shorter than sixteen bytes, element by element
+        uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+        for (int k = 0; k < a.dim; ++k) {
+          const T e = reinterpret_cast<const T*>(p)[k];
+          uint64_t bits = 0;
+          __builtin_memcpy(&bits, &e, sizeof(T));
+          const int at = 8 * (int)sizeof(T) * k;
+          if (at < 64) lo |= bits << at;
+          else hi |= bits << (at - 64);
+        }
+        v[s] = make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
       }
       from[s] += next;
     }
   }
   __device__ __forceinline__ void to_lds(char* tile, const ScanArray& a, int n, int tid) {
-    const bool padded = PIECES * (int)(16 / sizeof(T)) > a.dim;
+    const bool padded = PIECES * E > a.dim;
+    const int over = a.dim > E && a.dim % E != 0 ? (E - a.dim % E) * (int)sizeof(T) : 0;
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
       const int q = index(s, tid), at = row(q);
+      if (!WHOLE && over != 0) {
+        const uint4 rest = shift_right(v[s], over);
+        if (last >> s & 1u) v[s] = rest;
+      }
       if (padded && (past >> s & 1u)) v[s] = make_uint4(0, 0, 0, 0);
       if (n < TILE && row(index(s, fresh(tid))) >= n) v[s] = make_uint4(0, 0, 0, 0);
       if (kAll % THREADS == 0 || s * THREADS + tid < kAll)
@@ -322,14 +358,14 @@ __device__ __forceinline__ void each_state_element(float* s, int row, int col, i
 template <int SL>
 constexpr int scan_pairs() { return SL == 1 ? 4 : SL == 2 ? 2 : 1; }  // (sequence, head) pairs of a workgroup
 
-template <class T, int NK, int NV, int SL, bool STATE_ONLY, bool WIDE>
+template <class T, int NK, int NV, int SL, bool STATE_ONLY, bool WHOLE>
 __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 || (NK == 4 && SL == 1) ? 2 : 3) scan_kernel(const ScanArgs args) {
   typedef ScanTraits<T> Tr;
   typedef typename Tr::Frag Frag;
   constexpr int U = Tr::kSub, kTile = 16 * U, P = scan_pairs<SL>(), kThreads = 64 * SL * P, E = 16 / sizeof(T);
   constexpr int kPiecesX = NK * (int)sizeof(T), kPiecesZ = SL * NV * (int)sizeof(T);
-  typedef Stage<T, kPiecesX, P, kTile, kThreads, WIDE> StageX;
-  typedef Stage<T, kPiecesZ, P, kTile, kThreads, WIDE> StageZ;
+  typedef Stage<T, kPiecesX, P, kTile, kThreads, WHOLE> StageX;
+  typedef Stage<T, kPiecesZ, P, kTile, kThreads, WHOLE> StageZ;
   constexpr int kBytesX = StageX::kAll * 16, kBytesZ = StageZ::kAll * 16;
   __shared__ __align__(16) char lds_x[STATE_ONLY ? 16 : kBytesX];
   __shared__ __align__(16) char lds_y[kBytesX];
@@ -551,7 +587,7 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 || (NK == 
         if (__builtin_amdgcn_ballot_w64(!(fabsf(sum) < __builtin_inff())) != 0) {
           left_at = t0;
           if (lane == 0) lds_left[wave] = 1;
-        } else if (WIDE && !(sizeof(T) == 2 && r.out_f32)) {
+        } else if (sizeof(T) == 4 || !r.out_f32) {
 #pragma unroll
           for (int u = 0; u < U; ++u) {
             const int row = block_at(u) + i, swz = swizzle<kPiecesZ>(row);
@@ -563,7 +599,7 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 || (NK == 
               else *reinterpret_cast<shortx4*>(p + ((f / 8) ^ swz) * 16 + (f & 4) * 2) = pack4(o[u][c]);
             }
           }
-        } else if (active) {
+        } else if (active) {  // shares in fp32
           char* ob = const_cast<char*>(base(r.out, local));
           const int i0 = fresh(i), f0 = slice0 + 4 * fresh(g);
 #pragma unroll
@@ -576,8 +612,7 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 || (NK == 
                 for (int e = 0; e < 4; ++e) {
                   const int f = f0 + 16 * c + e;
                   if (f >= Dz) continue;
-                  if (sizeof(T) == 4 || r.out_f32) reinterpret_cast<float*>(row)[f] = o[u][c][e];
-                  else reinterpret_cast<bf16_t*>(row)[f] = to_bf16(o[u][c][e]);
+                  reinterpret_cast<float*>(row)[f] = o[u][c][e];
                 }
             }
         }
@@ -646,13 +681,22 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 || (NK == 
     }
     lds_barrier();
     if constexpr (!STATE_ONLY) {
-      if (WIDE && !(sizeof(T) == 2 && r.out_f32)) {
+      if (sizeof(T) == 4 || !r.out_f32) {
 #pragma unroll
         for (int s = 0; s < StageZ::kSlots; ++s) {
           const int q = StageZ::index(s, tid), row = StageZ::row(q), piece = StageZ::piece(q), which = StageZ::pair(q);
-          if ((out_on >> s & 1u) && row < n && lds_left[which * SL + piece * E / (16 * NV)] == 0)
-            *reinterpret_cast<uint4*>(to_out[s]) =
-                *reinterpret_cast<const uint4*>(lds_o + ((which * kTile + row) * kPiecesZ + (piece ^ swizzle<kPiecesZ>(row))) * 16);
+          if ((out_on >> s & 1u) && row < n && lds_left[which * SL + piece * E / (16 * NV)] == 0) {
+            const uint4 v = *reinterpret_cast<const uint4*>(lds_o + ((which * kTile + row) * kPiecesZ + (piece ^ swizzle<kPiecesZ>(row))) * 16);
+            if (WHOLE || piece * E + E <= Dz) {
+              store16(to_out[s], v);
+            } else {
+              T e[E];
+              __builtin_memcpy(e, &v, 16);
+#pragma unroll
+              for (int k = 0; k < E - 1; ++k)
+                if (piece * E + k < Dz) reinterpret_cast<T*>(to_out[s])[k] = e[k];
+            }
+          }
           to_out[s] += out_way;
         }
       }
@@ -694,19 +738,20 @@ inline int scan_nv(int dim) { return dim <= 16 ? 1 : 2; }
 inline int scan_slices(int dim) { return dim <= 32 ? 1 : (dim + 31) / 32; }
 
 // A scan of no steps has no valid row to point at: the caller never launches one.
-void launch_scan_f32(const ScanArgs& a, int dx, int dz, bool state_only, bool wide, hipStream_t s);
-void launch_scan_bf16(const ScanArgs& a, int dx, int dz, bool state_only, bool wide, hipStream_t s);
+void launch_scan_f32(const ScanArgs& a, int dx, int dz, bool state_only, hipStream_t s);
+void launch_scan_bf16(const ScanArgs& a, int dx, int dz, bool state_only, hipStream_t s);
 
 template <class T>
-inline void launch_scan(const ScanArgs& a, int dx, int dz, bool state_only, bool wide, hipStream_t s) {
+inline void launch_scan(const ScanArgs& a, int dx, int dz, bool state_only, hipStream_t s) {
   const int nk = scan_nk(dx), nv = scan_nv(dz), slices = scan_slices(dz);
+  const bool whole = dx * sizeof(T) % 16 == 0 && dz * sizeof(T) % 16 == 0;
 #define MARL_SCAN(K, V, SL)                                                                                               \
   if (nk == K && nv == V && slices == SL) {                                                                               \
     constexpr uint32_t P = scan_pairs<SL>();                                                                              \
     const dim3 grid((a.pairs + P - 1) / P * a.n_stretches * a.n_roles), block(64 * SL * P);                               \
-    if (state_only && wide) hipLaunchKernelGGL((scan_kernel<T, K, V, SL, true, true>), grid, block, 0, s, a);            \
+    if (state_only && whole) hipLaunchKernelGGL((scan_kernel<T, K, V, SL, true, true>), grid, block, 0, s, a);           \
     else if (state_only) hipLaunchKernelGGL((scan_kernel<T, K, V, SL, true, false>), grid, block, 0, s, a);              \
-    else if (wide) hipLaunchKernelGGL((scan_kernel<T, K, V, SL, false, true>), grid, block, 0, s, a);                    \
+    else if (whole) hipLaunchKernelGGL((scan_kernel<T, K, V, SL, false, true>), grid, block, 0, s, a);                   \
     else hipLaunchKernelGGL((scan_kernel<T, K, V, SL, false, false>), grid, block, 0, s, a);                             \
     return;                                                                                                               \
   }

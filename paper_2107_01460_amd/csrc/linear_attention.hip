@@ -218,7 +218,6 @@ ScanArray array_of(const marl_view& v, int elem, int dim, int share) {
   a.head = v.head * elem;
   a.share = (uint32_t)share;
   a.dim = dim;
-  a.wide = ((reinterpret_cast<uintptr_t>(a.data) | (uintptr_t)a.step | (uintptr_t)a.seq | (uintptr_t)a.head) & 15u) == 0 && dim * elem % 16 == 0;
   return a;
 }
 ScanState state_of(const float* p, uint32_t stretches, int row, int col) { return {const_cast<float*>(p), (int32_t)stretches, row, col}; }
@@ -233,12 +232,7 @@ int32_t scan(ScanArgs a, const marl_attention_dims& d, const Plan& p, int dx, in
   a.stretch = p.stretch;
   a.pairs = (uint32_t)p.pairs;
   if (p.pairs * a.n_roles * a.n_stretches >= ((int64_t)1 << 31)) return MARL_E_SIZE;
-  bool wide = true;
-  for (uint32_t u = 0; u < a.n_roles; ++u) {
-    const ScanRole& r = a.role[u];
-    wide = wide && r.y.wide && r.z.wide && (state_only || (r.x.wide && r.out.wide));
-  }
-  (d.precision == 0 ? launch_scan_f32 : launch_scan_bf16)(a, dx, dz, state_only, wide, s);
+  (d.precision == 0 ? launch_scan_f32 : launch_scan_bf16)(a, dx, dz, state_only, s);
   return launch_status();
 }
 

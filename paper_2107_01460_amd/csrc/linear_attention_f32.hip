@@ -2,5 +2,5 @@
 #include "linear_attention.h"
 
 namespace marl {
-void launch_scan_f32(const ScanArgs& a, int dx, int dz, bool state_only, bool wide, hipStream_t s) { launch_scan<float>(a, dx, dz, state_only, wide, s); }
+void launch_scan_f32(const ScanArgs& a, int dx, int dz, bool state_only, hipStream_t s) { launch_scan<float>(a, dx, dz, state_only, s); }
 }  // namespace marl
