@@ -7,24 +7,31 @@
 namespace marl {
 namespace {
 
-// Values of a row that a lane holds at most.  Element by element eight: half the loads one after another (10 007 rows of 147 bf16: 8.3 against 10 us),
-// sixteen only where a workgroup's 1024 lanes do not reach otherwise.
-constexpr int lane_values(int E, int width) { return E > 1 || width > 8192 ? 16 : 8; }
+constexpr int kLane = 16;           // values of a row that a lane holds at most
 constexpr int kMaxWidth = 16384;
 constexpr int kThreads = 256;
 
-// Columns of a lane: vectors of E consecutive values, vector u of lane l at ((u * TEAM) + l) * E; or single values (E = 1) where width or alignment
-// forbid 16-byte accesses.
+// Columns of a lane: vectors of E consecutive values (sixteen bytes, at any alignment; E = 1 for rows shorter than that), vector u of lane l at
+// ((u * TEAM) + l) * E.  A last vector that would pass the row's end is moved back to end with it: its first `skip` values are its neighbour's too, they
+// are computed and stored twice alike and counted once.
+template <int E>
+struct Columns {
+  int at, skip;  // first column; values to pass over in sums: E where there is nothing
+  __device__ __forceinline__ Columns(int vector, int width) {
+    const int c = vector * E;
+    at = c < width ? min(c, width - E) : 0;
+    skip = c < width ? c - at : E;
+  }
+};
 template <class T, int E>
 __device__ __forceinline__ void load_vec(float (&v)[E], const T* p) {
   if constexpr (E == 1) {
     v[0] = load_act(p, 0);
   } else if constexpr (sizeof(T) == 4) {
-    const float4 f = *reinterpret_cast<const float4*>(p);
-    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+    __builtin_memcpy(v, p, 16);
   } else {
-    const uint4 f = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {f.x, f.y, f.z, f.w};
+    uint32_t w[4];
+    __builtin_memcpy(w, p, 16);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       v[2 * k] = __uint_as_float(w[k] << 16);
@@ -38,9 +45,10 @@ __device__ __forceinline__ void store_vec(T* p, const float (&v)[E]) {
     if constexpr (sizeof(T) == 4) *p = v[0];
     else *p = to_bf16(v[0]);
   } else if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    __builtin_memcpy(p, v, 16);
   } else {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
+    const uint32_t w[4] = {pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+    __builtin_memcpy(p, w, 16);
   }
 }
 
@@ -61,21 +69,12 @@ __device__ __forceinline__ float team_sum(float v, float* scratch) {
   return v;
 }
 
-// Weights of a lane's columns (absent: `none`).  E > 1: 16-byte accesses
+// Weights of a lane's columns (absent: `none`)
 template <int E>
-__device__ __forceinline__ void load_weights(float (&w)[E], const float* p, int c, int width, float none) {
-  if (p == nullptr || c >= width) {
+__device__ __forceinline__ void load_weights(float (&w)[E], const float* p, int at, float none) {
 #pragma unroll
-    for (int k = 0; k < E; ++k) w[k] = none;
-  } else if constexpr (E == 1) {
-    w[0] = p[c];
-  } else {
-#pragma unroll
-    for (int k = 0; k < E; k += 4) {
-      const float4 f = *reinterpret_cast<const float4*>(p + c + k);
-      w[k] = f.x; w[k + 1] = f.y; w[k + 2] = f.z; w[k + 3] = f.w;
-    }
-  }
+  for (int k = 0; k < E; ++k) w[k] = none;
+  if (p != nullptr) __builtin_memcpy(w, p + at, 4 * E);
 }
 
 // Every workgroup takes every gridDim.x-th group of rows, so that weights are read once a workgroup and not once a row (from the L2 that was four
@@ -90,8 +89,9 @@ __global__ void __launch_bounds__(TEAM > kThreads ? TEAM : kThreads)
   float w[N][E], b[N][E];
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    load_weights<E>(w[u], weight, (u * TEAM + lane) * E, width, 1.f);
-    load_weights<E>(b[u], bias, (u * TEAM + lane) * E, width, 0.f);
+    const Columns<E> c(u * TEAM + lane, width);
+    load_weights<E>(w[u], weight, c.at, 1.f);
+    load_weights<E>(b[u], bias, c.at, 0.f);
   }
   const float inv = 1.f / (float)width;
   for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < rows; row0 += (int64_t)gridDim.x * kTeams) {
@@ -101,26 +101,22 @@ __global__ void __launch_bounds__(TEAM > kThreads ? TEAM : kThreads)
     float v[N][E];
     float sum = 0.f;
 #pragma unroll
+    for (int u = 0; u < N; ++u) load_vec<T, E>(v[u], xr + Columns<E>(u * TEAM + lane, width).at);
+#pragma unroll
     for (int u = 0; u < N; ++u) {
-      const int c = (u * TEAM + lane) * E;
-      load_vec<T, E>(v[u], xr + (c < width ? c : 0));
+      const int skip = Columns<E>(u * TEAM + lane, width).skip;
+#pragma unroll
+      for (int k = 0; k < E; ++k) sum += k >= skip ? v[u][k] : 0.f;
     }
-#pragma unroll
-    for (int u = 0; u < N; ++u)
-#pragma unroll
-      for (int k = 0; k < E; ++k) {
-        if ((u * TEAM + lane) * E >= width) v[u][k] = 0.f;
-        sum += v[u][k];
-      }
     const float mean = team_sum<TEAM>(sum, scratch) * inv;
     float sq = 0.f;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const bool in = (u * TEAM + lane) * E < width;
+      const int skip = Columns<E>(u * TEAM + lane, width).skip;
 #pragma unroll
       for (int k = 0; k < E; ++k) {
         v[u][k] -= mean;
-        sq += in ? v[u][k] * v[u][k] : 0.f;
+        sq += k >= skip ? v[u][k] * v[u][k] : 0.f;
       }
     }
     const float rstd = 1.f / sqrtf(team_sum<TEAM>(sq, scratch) * inv + eps);
@@ -128,11 +124,11 @@ __global__ void __launch_bounds__(TEAM > kThreads ? TEAM : kThreads)
       T* yr = y + row * ys;
 #pragma unroll
       for (int u = 0; u < N; ++u) {
-        const int c = (u * TEAM + lane) * E;
-        if (c < width) {
+        const Columns<E> c(u * TEAM + lane, width);
+        if (c.skip < E) {
 #pragma unroll
           for (int k = 0; k < E; ++k) v[u][k] = v[u][k] * rstd * w[u][k] + b[u][k];
-          store_vec<T, E>(yr + c, v[u]);
+          store_vec<T, E>(yr + c.at, v[u]);
         }
       }
       if (lane == 0) {
@@ -156,7 +152,7 @@ __global__ void __launch_bounds__(TEAM > kThreads ? TEAM : kThreads)
   float w[N][E], dw[N][E], db[N][E];
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    load_weights<E>(w[u], weight, (u * TEAM + lane) * E, width, 1.f);
+    load_weights<E>(w[u], weight, Columns<E>(u * TEAM + lane, width).at, 1.f);
 #pragma unroll
     for (int k = 0; k < E; ++k) dw[u][k] = db[u][k] = 0.f;
   }
@@ -169,25 +165,24 @@ __global__ void __launch_bounds__(TEAM > kThreads ? TEAM : kThreads)
     float h[N][E], g[N][E];
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const int c = (u * TEAM + lane) * E, from = c < width ? c : 0;
+      const int from = Columns<E>(u * TEAM + lane, width).at;
       load_vec<T, E>(h[u], xr + from);
       load_vec<T, E>(g[u], gr + from);
     }
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const bool in = (u * TEAM + lane) * E < width;
+      const int skip = Columns<E>(u * TEAM + lane, width).skip;
 #pragma unroll
       for (int k = 0; k < E; ++k) {
-        h[u][k] = in ? (h[u][k] - m) * r : 0.f;
-        if (!in) g[u][k] = 0.f;
+        h[u][k] = (h[u][k] - m) * r;
         if constexpr (WEIGHTS) {
           dw[u][k] += on ? g[u][k] * h[u][k] : 0.f;
           db[u][k] += on ? g[u][k] : 0.f;
         }
         g[u][k] *= w[u][k];
-        s1 += g[u][k];
-        s2 += g[u][k] * h[u][k];
+        s1 += k >= skip ? g[u][k] : 0.f;
+        s2 += k >= skip ? g[u][k] * h[u][k] : 0.f;
       }
     }
     s1 = team_sum<TEAM>(s1, scratch) * inv;
@@ -196,11 +191,11 @@ __global__ void __launch_bounds__(TEAM > kThreads ? TEAM : kThreads)
       T* o = dx + row * dxs;
 #pragma unroll
       for (int u = 0; u < N; ++u) {
-        const int c = (u * TEAM + lane) * E;
-        if (c < width) {
+        const Columns<E> c(u * TEAM + lane, width);
+        if (c.skip < E) {
 #pragma unroll
           for (int k = 0; k < E; ++k) g[u][k] = r * (g[u][k] - s1 - h[u][k] * s2);
-          store_vec<T, E>(o + c, g[u]);
+          store_vec<T, E>(o + c.at, g[u]);
         }
       }
     }
@@ -212,10 +207,10 @@ __global__ void __launch_bounds__(TEAM > kThreads ? TEAM : kThreads)
       for (int u = 0; u < N; ++u)
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-          const int c = (u * TEAM + lane) * E + k;
-          if (c < width) {
-            p[c] = dw[u][k];
-            p[width + c] = db[u][k];
+          const Columns<E> c(u * TEAM + lane, width);
+          if (k >= c.skip) {
+            p[c.at + k] = dw[u][k];
+            p[width + c.at + k] = db[u][k];
           }
         }
     } else {
@@ -230,10 +225,10 @@ __global__ void __launch_bounds__(TEAM > kThreads ? TEAM : kThreads)
             dw[u][k] += __shfl_xor(dw[u][k], m);
             db[u][k] += __shfl_xor(db[u][k], m);
           }
-          if ((threadIdx.x & 63) < TEAM) {
-            const int c = (u * TEAM + lane) * E + k;
-            shares[wave][0][c] = dw[u][k];
-            shares[wave][1][c] = db[u][k];
+          const Columns<E> c(u * TEAM + lane, width);
+          if ((threadIdx.x & 63) < TEAM && k >= c.skip) {
+            shares[wave][0][c.at + k] = dw[u][k];
+            shares[wave][1][c.at + k] = db[u][k];
           }
         }
       __syncthreads();
@@ -275,37 +270,34 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const float* __restric
   }
 }
 
-inline int team_of(int width, int E) {  // lanes that a row takes
-  const int most = lane_values(E, width);
+inline int team_of(int width) {  // lanes that a row takes
   int team = 8;
-  while (team < 64 && team * most < width) team *= 2;
-  return team * most >= width ? team : width <= 256 * most ? 256 : 1024;
+  while (team < 64 && team * kLane < width) team *= 2;
+  return team * kLane >= width ? team : width <= 256 * kLane ? 256 : 1024;
 }
-inline int64_t shares_of(int64_t rows, int width, int E) {  // workgroups of the gradient's kernel, each with its share of the column sums
-  const int team = team_of(width, E), teams = team >= kThreads ? 1 : kThreads / team;
+inline int64_t shares_of(int64_t rows, int width) {  // workgroups of the gradient's kernel, each with its share of the column sums
+  const int team = team_of(width), teams = team >= kThreads ? 1 : kThreads / team;
   const int64_t groups = (rows + teams - 1) / teams, most = team == 1024 ? 256 : 1024;
   return groups < most ? groups : most;
 }
-inline bool wide_rows(const void* p, int64_t stride, int elem) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(stride * elem)) & 15u) == 0; }  // (p may be null)
 
-// The instance for a team and its vectors a lane
-#define MARL_LN_TEAMS                                            \
-  constexpr int N = lane_values(E, 1) / E, kMost = 16 / E;       \
-  if (team == 8) MARL_LN(8, N);                                  \
-  else if (team == 16) MARL_LN(16, N);                           \
-  else if (team == 32) MARL_LN(32, N);                           \
-  else if (team == 64) MARL_LN(64, N);                           \
-  else if (team == 256) MARL_LN(256, N);                         \
-  else if (width <= 8192) MARL_LN(1024, N);                      \
-  else MARL_LN(1024, kMost)
+// The instance for a team.  (Rows shorter than sixteen bytes: the smallest.)
+#define MARL_LN_TEAMS                          \
+  constexpr int N = E == 1 ? 1 : kLane / E;    \
+  if (E == 1 || team == 8) MARL_LN(8);         \
+  else if (team == 16) MARL_LN(16);            \
+  else if (team == 32) MARL_LN(32);            \
+  else if (team == 64) MARL_LN(64);            \
+  else if (team == 256) MARL_LN(256);          \
+  else MARL_LN(1024)
 
 template <class T, int E>
 int32_t forward(int64_t rows, int width, const T* x, int64_t xs, const float* weight, const float* bias, float eps, T* y, int64_t ys, float* mean,
                 float* rstd, hipStream_t s) {
-  const int team = team_of(width, E);
+  const int team = team_of(width);
   const int64_t teams = team >= kThreads ? 1 : kThreads / team, groups = (rows + teams - 1) / teams, most = team == 1024 ? 512 : 2048;
   const int64_t blocks = groups < most ? groups : most;  // as many as the chip holds at once
-#define MARL_LN(TEAM, N)                                                                                                                     \
+#define MARL_LN(TEAM)                                                                                                                        \
   hipLaunchKernelGGL((layer_norm_kernel<T, E, TEAM, N>), dim3((unsigned)blocks), dim3(TEAM > kThreads ? TEAM : kThreads), 0, s, rows, width, x, \
                      xs, weight, bias, eps, y, ys, mean, rstd)
   MARL_LN_TEAMS;
@@ -316,9 +308,9 @@ int32_t forward(int64_t rows, int width, const T* x, int64_t xs, const float* we
 template <class T, int E, bool WEIGHTS>
 int32_t backward(int64_t rows, int width, const T* dy, int64_t dys, const T* x, int64_t xs, const float* weight, const float* mean,
                  const float* rstd, T* dx, int64_t dxs, float* part, hipStream_t s) {
-  const dim3 grid((unsigned)shares_of(rows, width, E));
-  const int team = team_of(width, E);
-#define MARL_LN(TEAM, N)                                                                                                                 \
+  const dim3 grid((unsigned)shares_of(rows, width));
+  const int team = team_of(width);
+#define MARL_LN(TEAM)                                                                                                                    \
   hipLaunchKernelGGL((layer_norm_backward_kernel<T, E, TEAM, N, WEIGHTS>), grid, dim3(TEAM > kThreads ? TEAM : kThreads), 0, s, rows, width, \
                      dy, dys, x, xs, weight, mean, rstd, dx, dxs, part)
   MARL_LN_TEAMS;
@@ -364,8 +356,7 @@ int32_t marl_layer_norm(int32_t precision, int64_t n_rows, int32_t width, const 
     if ((rc = check_floats(p)) != MARL_OK) return rc;
   hipStream_t s = (hipStream_t)stream;
   const int elem = precision == 0 ? 4 : 2;
-  const bool wide = wide_rows(x, x_stride, elem) && wide_rows(y, y_stride, elem) && wide_rows(weight, 0, 4) && wide_rows(bias, 0, 4) &&
-                    width * elem % 16 == 0;
+  const bool wide = width * elem >= 16;
   if (precision == 0)
     return (wide ? forward<float, 4> : forward<float, 1>)(n_rows, width, (const float*)x, x_stride, weight, bias, eps, (float*)y, y_stride, mean, rstd, s);
   return (wide ? forward<bf16_t, 8> : forward<bf16_t, 1>)(n_rows, width, (const bf16_t*)x, x_stride, weight, bias, eps, (bf16_t*)y, y_stride, mean,
@@ -376,8 +367,7 @@ int32_t marl_layer_norm_workspace(int64_t n_rows, int32_t width, int64_t* bytes)
   const int32_t rc = check(0, n_rows, width);
   if (rc != MARL_OK) return rc;
   if (bytes == nullptr) return MARL_E_NULL;
-  const int64_t wide = shares_of(n_rows, width, 8), single = shares_of(n_rows, width, 1);  // (alignment decides)
-  *bytes = (wide > single ? wide : single) * 2 * width * 4;
+  *bytes = shares_of(n_rows, width) * 2 * width * 4;
   return MARL_OK;
 }
 
@@ -401,9 +391,8 @@ int32_t marl_layer_norm_backward(int32_t precision, int64_t n_rows, int32_t widt
   int64_t shares = 0;
   if (n_rows > 0) {
     const int elem = precision == 0 ? 4 : 2;
-    const bool wide = wide_rows(dy, dy_stride, elem) && wide_rows(x, x_stride, elem) && wide_rows(dx, dx_stride, elem) &&
-                      wide_rows(weight, 0, 4) && width * elem % 16 == 0;
-    shares = shares_of(n_rows, width, wide ? 16 / elem : 1);
+    const bool wide = width * elem >= 16;
+    shares = shares_of(n_rows, width);
     rc = (precision == 0 ? backward_of<float> : backward_of<bf16_t>)(wide, weights, n_rows, width, dy, dy_stride, x, x_stride, weight, mean, rstd, dx,
                                                                      dx_stride, (float*)workspace, s);
     if (rc != MARL_OK) return rc;

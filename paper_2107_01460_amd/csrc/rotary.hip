@@ -77,8 +77,7 @@ __device__ __forceinline__ Piece<T, E> get(const T* p) {
   if constexpr (E == 1) {
     r.v[0] = *p;
   } else {
-    const uint4 u = *reinterpret_cast<const uint4*>(p);
-    __builtin_memcpy(&r, &u, 16);
+    __builtin_memcpy(&r, p, 16);  // (at any alignment)
   }
   return r;
 }
@@ -87,9 +86,7 @@ __device__ __forceinline__ void put(T* p, const Piece<T, E>& r) {
   if constexpr (E == 1) {
     *p = r.v[0];
   } else {
-    uint4 u;
-    __builtin_memcpy(&u, &r, 16);
-    *reinterpret_cast<uint4*>(p) = u;
+    __builtin_memcpy(p, &r, 16);
   }
 }
 __device__ __forceinline__ float widen(float v) { return v; }
@@ -249,15 +246,12 @@ int32_t marl_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, c
   const int elem = d.precision == 0 ? 4 : 2;
   const int n = k.data != nullptr ? 2 : 1;
   const marl_view in[2] = {q, k}, out[2] = {q_out, k_out};
-  uintptr_t low = 0;
   for (int u = 0; u < n; ++u) {
     if (in[u].data == nullptr || out[u].data == nullptr) return MARL_E_NULL;
     const uintptr_t pi = reinterpret_cast<uintptr_t>(in[u].data), po = reinterpret_cast<uintptr_t>(out[u].data);
     if (((pi | po) & odd) != 0) return MARL_E_ALIGN;
     a.a[u] = {static_cast<const char*>(in[u].data), static_cast<char*>(out[u].data), in[u].step, in[u].seq, in[u].head, out[u].step, out[u].seq,
               out[u].head};
-    for (int64_t x : {in[u].step, in[u].seq, in[u].head, out[u].step, out[u].seq, out[u].head}) low |= (uintptr_t)(x * elem);
-    low |= pi | po;
   }
   MARL_REQUIRE_PTR(table);
   if ((reinterpret_cast<uintptr_t>(positions) & 3u) != 0) return MARL_E_ALIGN;
@@ -275,7 +269,7 @@ int32_t marl_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, c
   a.dim = (uint32_t)d.dim_k;
   a.table_wide = rotary_dim % 8 == 0;
   const int E = 16 / elem;
-  const bool wide = (low & 15u) == 0 && d.dim_k % E == 0 && (interleaved ? true : rotary_dim / 2 % E == 0);
+  const bool wide = d.dim_k % E == 0 && (interleaved || rotary_dim / 2 % E == 0);
   hipStream_t s = (hipStream_t)stream;
   if (d.precision == 0) return wide ? rotate<float, 4>(a, interleaved != 0, s) : rotate<float, 1>(a, interleaved != 0, s);
   return wide ? rotate<bf16_t, 8>(a, interleaved != 0, s) : rotate<bf16_t, 1>(a, interleaved != 0, s);
