@@ -64,10 +64,13 @@ struct ScanTraits<bf16_t> {
   typedef shortx4 Frag;
   static constexpr int kSub = 2;            // products contract over 32 steps, and S is split into parts once for 32
 };
-// Feature of element e of lane group g in tile a of N tiles of sixteen x and y features.  bf16: two tiles deal a lane eight consecutive ones, 16 bytes.
+// Feature of element e of lane group g in tile a of N tiles of sixteen x and y features.  bf16: two tiles deal a lane eight consecutive ones, 16 bytes;
+// the last of an odd number stands alone.
+template <class T, int N>
+__host__ __device__ constexpr bool in_pair(int a) { return sizeof(T) == 2 && a < N / 2 * 2; }
 template <class T, int N>
 __device__ __forceinline__ int feat(int a, int g, int e) {
-  return sizeof(T) == 2 && N % 2 == 0 ? 32 * (a / 2) + 8 * g + 4 * (a & 1) + e : 16 * a + 4 * g + e;
+  return in_pair<T, N>(a) ? 32 * (a / 2) + 8 * g + 4 * (a & 1) + e : 16 * a + 4 * g + e;
 }
 
 __device__ __forceinline__ double ipow(float base, int m) {  // base^m, 0^0 = 1
@@ -209,16 +212,14 @@ __device__ __forceinline__ void rows_of(Rows<T, N>& r, const char* tile, int row
   if constexpr (sizeof(T) == 4) {
 #pragma unroll
     for (int t = 0; t < N; ++t) r.f[t] = *reinterpret_cast<const floatx4*>(p + ((4 * t + g) ^ swz) * 16);
-  } else if constexpr (N % 2 == 0) {
+  } else {
 #pragma unroll
-    for (int t = 0; t < N; t += 2) {
+    for (int t = 0; t + 1 < N; t += 2) {
       const shortx8 v = *reinterpret_cast<const shortx8*>(p + ((2 * t + g) ^ swz) * 16);
       r.f[t] = __builtin_shufflevector(v, v, 0, 1, 2, 3);
       r.f[t + 1] = __builtin_shufflevector(v, v, 4, 5, 6, 7);
     }
-  } else {
-#pragma unroll
-    for (int t = 0; t < N; ++t) r.f[t] = *reinterpret_cast<const shortx4*>(p + ((2 * t + (g >> 1)) ^ swz) * 16 + 8 * (g & 1));
+    if constexpr (N % 2 == 1) r.f[N - 1] = *reinterpret_cast<const shortx4*>(p + ((2 * (N - 1) + (g >> 1)) ^ swz) * 16 + 8 * (g & 1));
   }
 }
 // Columns: lane (i, g) gets one feature at steps 4 g .. 4 g + 3 of the block of sixteen steps that begins at `row`.  first: of the sixteen features,
@@ -337,14 +338,14 @@ struct Stage {
 };
 
 // The state's element (feat(a, g, e), first + 16 c + i) for every a, c, e of a lane: f(element's place in the lane's registers, its address or nullptr).
-// Addresses are a uniform part and one offset a lane.
+// Addresses are a uniform part and an offset of the lane.
 template <class T, int NK, int NV, class F>
 __device__ __forceinline__ void each_state_element(float* s, int row, int col, int Dx, int Dz, int first, int i, int g, F f) {
-  const int f0 = feat<T, NK>(0, g, 0);
-  const uint32_t lane = (uint32_t)(f0 * row + (first + i) * col);
   const bool whole = Dx == 16 * NK && first + 16 * NV <= Dz;
 #pragma unroll
-  for (int a = 0; a < NK; ++a)
+  for (int a = 0; a < NK; ++a) {
+    const int f0 = in_pair<T, NK>(a) ? 8 * g : 4 * g;
+    const uint32_t lane = (uint32_t)(f0 * row + (first + i) * col);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -353,13 +354,14 @@ __device__ __forceinline__ void each_state_element(float* s, int row, int col, i
         if (whole) f(a, c, e, p + lane);
         else f(a, c, e, f0 + feat<T, NK>(a, 0, e) < Dx && first + 16 * c + i < Dz ? p + lane : nullptr);
       }
+  }
 }
 
 template <int SL>
 constexpr int scan_pairs() { return SL == 1 ? 4 : SL == 2 ? 2 : 1; }  // (sequence, head) pairs of a workgroup
 
 template <class T, int NK, int NV, int SL, bool STATE_ONLY, bool WHOLE>
-__global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 || (NK == 4 && SL == 1) ? 2 : 3) scan_kernel(const ScanArgs args) {
+__global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 5 || (NK == 4 && SL == 1) ? 2 : 3) scan_kernel(const ScanArgs args) {
   typedef ScanTraits<T> Tr;
   typedef typename Tr::Frag Frag;
   constexpr int U = Tr::kSub, kTile = 16 * U, P = scan_pairs<SL>(), kThreads = 64 * SL * P, E = 16 / sizeof(T);
@@ -460,8 +462,8 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 || (NK == 
   const char* y_tile = lds_y + local * kTile * kPiecesX * 16;
   const char* z_tile = lds_z + local * kTile * kPiecesZ * 16;
   auto y_column = [&](int u, int a) {
-    constexpr bool kRuns = sizeof(T) == 2 && NK % 2 == 0;
-    return column<T, kPiecesX>(reinterpret_cast<const T*>(y_tile), block_at(u), kRuns ? 32 * (a / 2) + 4 * (a & 1) : 16 * a, kRuns ? 8 : 4, i, g);
+    const bool runs = in_pair<T, NK>(a);
+    return column<T, kPiecesX>(reinterpret_cast<const T*>(y_tile), block_at(u), runs ? 32 * (a / 2) + 4 * (a & 1) : 16 * a, runs ? 8 : 4, i, g);
   };
   auto z_column = [&](int u, int c) {
     return column<T, kPiecesZ>(reinterpret_cast<const T*>(z_tile), block_at(u), slice0 + 16 * c, 4, i, g);
@@ -498,13 +500,9 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 || (NK == 
 #pragma unroll
           for (int u = v; u < U; ++u) {
             floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (NK % 2 == 0) {
 #pragma unroll
-              for (int a = 0; a < NK; a += 2) acc = mma2(y.f[a], y.f[a + 1], x[u].f[a], x[u].f[a + 1], acc);
-            } else {
-#pragma unroll
-              for (int a = 0; a < NK; ++a) acc = mma(y.f[a], x[u].f[a], acc);
-            }
+            for (int a = 0; a + 1 < NK; a += 2) acc = mma2(y.f[a], y.f[a + 1], x[u].f[a], x[u].f[a + 1], acc);
+            if constexpr (NK % 2 == 1) acc = mma(y.f[NK - 1], x[u].f[NK - 1], acc);
             score[u][v] = acc;
           }
         }
@@ -515,24 +513,16 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 || (NK == 
           for (int c = 0; c < NV; ++c) o[u][c] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
-          if constexpr (NK % 2 == 0) {
 #pragma unroll
-            for (int a = 0; a < NK; a += 2) {
-              const Parts<T, 2> s0 = parts_of<T, 2>(S[a][c]), s1 = parts_of<T, 2>(S[a + 1][c]);
+          for (int a = 0; a < NK; a += 2) {
+            const Parts<T, 2> s0 = parts_of<T, 2>(S[a][c]), s1 = parts_of<T, 2>(S[min(a + 1, NK - 1)][c]);
 #pragma unroll
-              for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int p = kParts - 1; p >= 0; --p) o[u][c] = mma2(s0.p[p], s1.p[p], x[u].f[a], x[u].f[a + 1], o[u][c]);
-            }
-          } else {
-#pragma unroll
-            for (int a = 0; a < NK; ++a) {
-              const Parts<T, 2> s0 = parts_of<T, 2>(S[a][c]);
-#pragma unroll
-              for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int p = kParts - 1; p >= 0; --p) o[u][c] = mma(s0.p[p], x[u].f[a], o[u][c]);
-            }
+              for (int p = kParts - 1; p >= 0; --p) {
+                if (a + 1 < NK) o[u][c] = mma2(s0.p[p], s1.p[p], x[u].f[a], x[u].f[min(a + 1, NK - 1)], o[u][c]);
+                else o[u][c] = mma(s0.p[p], x[u].f[a], o[u][c]);
+              }
           }
         }
 #pragma unroll
@@ -733,7 +723,7 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 6 || (NK == 
 }
 
 // ---- launch: the instance by (padded) widths -------------------------------------------------------------------------------------------
-inline int scan_nk(int dim) { return dim <= 16 ? 1 : dim <= 32 ? 2 : dim <= 64 ? 4 : dim <= 96 ? 6 : 8; }
+inline int scan_nk(int dim) { return dim <= 96 ? (dim + 15) / 16 : 8; }
 inline int scan_nv(int dim) { return dim <= 16 ? 1 : 2; }
 inline int scan_slices(int dim) { return dim <= 32 ? 1 : (dim + 31) / 32; }
 
@@ -756,7 +746,7 @@ inline void launch_scan(const ScanArgs& a, int dx, int dz, bool state_only, hipS
     return;                                                                                                               \
   }
 #define MARL_SCAN_ALL(K) MARL_SCAN(K, 1, 1) MARL_SCAN(K, 2, 1) MARL_SCAN(K, 2, 2) MARL_SCAN(K, 2, 3) MARL_SCAN(K, 2, 4)
-  MARL_SCAN_ALL(1) MARL_SCAN_ALL(2) MARL_SCAN_ALL(4) MARL_SCAN_ALL(6) MARL_SCAN_ALL(8)
+  MARL_SCAN_ALL(1) MARL_SCAN_ALL(2) MARL_SCAN_ALL(3) MARL_SCAN_ALL(4) MARL_SCAN_ALL(5) MARL_SCAN_ALL(6) MARL_SCAN_ALL(8)
 #undef MARL_SCAN_ALL
 #undef MARL_SCAN
 }

@@ -95,7 +95,8 @@ def check(M, s, layout="tbhd", grad=True):
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("T,B,H,Hk,Dk,Dv", [
     (1, 1, 1, 1, 1, 1), (1, 5, 2, 1, 16, 16), (15, 3, 2, 2, 8, 24), (16, 6, 2, 2, 32, 32), (17, 4, 3, 1, 33, 31), (33, 2, 4, 2, 64, 64),
-    (40, 3, 2, 2, 65, 17), (50, 2, 1, 1, 128, 128), (31, 2, 2, 1, 100, 127), (64, 70, 2, 2, 16, 48), (128, 9, 4, 4, 32, 64), (20, 2, 2, 2, 17, 128)])
+    (40, 3, 2, 2, 65, 17), (50, 2, 1, 1, 128, 128), (31, 2, 2, 1, 100, 127), (64, 70, 2, 2, 16, 48), (128, 9, 4, 4, 32, 64), (20, 2, 2, 2, 17, 128),
+    (40, 3, 2, 2, 48, 80), (18, 2, 2, 1, 70, 44), (35, 2, 1, 1, 90, 112)])
 def test_sequences(M, T, B, H, Hk, Dk, Dv, dtype):
     print("case", T, B, H, Hk, Dk, Dv, dtype, flush=True)
     check(M, make(T, B, H, Hk, Dk, Dv, dtype, seed=T + Dk))
