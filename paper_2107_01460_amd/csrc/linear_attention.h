@@ -13,6 +13,10 @@
 // A workgroup of up to four wavefronts takes neighbouring heads (and all slices of their columns): a step's rows of neighbouring heads are one run of
 // memory, and steps are far apart in it (megabytes, when there are many sequences), so its wavefronts fetch and store whole runs together and hand
 // them to each other through LDS; the next tile is on its way in registers meanwhile.
+//
+// Measured (MI355X): output of 128 x 4096 steps of 8 heads of 64 in bf16 with states 732 us, 4.4 TB/s, 89 % of a copy's rate, bound by memory (a wavefront a
+// head with its own loads: 1070); gradient of 128 x 4096 steps of 4 heads of 32 in fp32 597 us, 3.5 TB/s, fp32 matrix cores busy 44 %; 32 768 steps of one
+// sequence with 8 heads of 128 in bf16 82 us for the scan, bound by the issue of vector instructions (about 700 a tile beside 100 matrix ones).
 #pragma once
 #include "split_bf16.h"
 
@@ -357,6 +361,8 @@ __device__ __forceinline__ void each_state_element(float* s, int row, int col, i
   }
 }
 
+// Wavefronts a SIMD: three where the registers allow it, two for 80 features and more (three: 66 to 143 registers spilled, 32 768 steps of 8 heads of 128 126 -> 355 us).
+// Slices of 32 columns: of 48 they spilled as much, and halved the wavefronts (gradient with heads of 40 and 72: 466 -> 890 us).
 template <int SL>
 constexpr int scan_pairs() { return SL == 1 ? 4 : SL == 2 ? 2 : 1; }  // (sequence, head) pairs of a workgroup
 
