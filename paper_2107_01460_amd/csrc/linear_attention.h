@@ -14,7 +14,7 @@
 // memory, and steps are far apart in it (megabytes, when there are many sequences), so its wavefronts fetch and store whole runs together and hand
 // them to each other through LDS; the next tile is on its way in registers meanwhile.
 //
-// Measured (MI355X): output of 128 x 4096 steps of 8 heads of 64 in bf16 with states 732 us, 4.4 TB/s, 89 % of a copy's rate, bound by memory (a wavefront a
+// Measured (MI355X): output of 128 x 4096 steps of 8 heads of 64 in bf16 with states 698 us, 4.6 TB/s, 94 % of a copy's rate, bound by memory (a wavefront a
 // head with its own loads: 1070); gradient of 128 x 4096 steps of 4 heads of 32 in fp32 597 us, 3.5 TB/s, fp32 matrix cores busy 44 %; 32 768 steps of one
 // sequence with 8 heads of 128 in bf16 82 us for the scan, bound by the issue of vector instructions (about 700 a tile beside 100 matrix ones).
 #pragma once
@@ -361,13 +361,15 @@ __device__ __forceinline__ void each_state_element(float* s, int row, int col, i
   }
 }
 
-// Wavefronts a SIMD: three where the registers allow it, two for 80 features and more (three: 66 to 143 registers spilled, 32 768 steps of 8 heads of 128 126 -> 355 us).
+// Wavefronts a SIMD that the registers are dealt out for: three up to 48 features, two above, because a spilled register costs more than a wavefront: its
+// reload waits for every load and store on its way (64 features, rollout of the header: three with 7 registers spilled 732 us, two with none 698; 128 features,
+// 32 768 steps: three with 100 spilled 355, two 126).
 // Slices of 32 columns: of 48 they spilled as much, and halved the wavefronts (gradient with heads of 40 and 72: 466 -> 890 us).
 template <int SL>
 constexpr int scan_pairs() { return SL == 1 ? 4 : SL == 2 ? 2 : 1; }  // (sequence, head) pairs of a workgroup
 
 template <class T, int NK, int NV, int SL, bool STATE_ONLY, bool WHOLE>
-__global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 5 || (NK == 4 && SL == 1) ? 2 : 3) scan_kernel(const ScanArgs args) {
+__global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 4 || (NK == 3 && SL == 1) ? 2 : 3) scan_kernel(const ScanArgs args) {
   typedef ScanTraits<T> Tr;
   typedef typename Tr::Frag Frag;
   constexpr int U = Tr::kSub, kTile = 16 * U, P = scan_pairs<SL>(), kThreads = 64 * SL * P, E = 16 / sizeof(T);
