@@ -208,6 +208,12 @@ int32_t check_view(const marl_view& v, int precision, bool used) {
   if (v.data == nullptr) return MARL_E_NULL;
   return (reinterpret_cast<uintptr_t>(v.data) & (precision == 0 ? 3u : 1u)) != 0 ? MARL_E_ALIGN : MARL_OK;
 }
+// An output's elements are places of their own: no stride of zero along a dimension that there is
+int32_t check_output(const marl_view& v, const marl_attention_dims& d, int heads, bool used) {
+  if (!used) return MARL_OK;
+  const bool overlaps = (v.step == 0 && d.n_steps > 1) || (v.seq == 0 && d.n_seqs > 1) || (v.head == 0 && heads > 1);
+  return overlaps ? MARL_E_CONFIG : MARL_OK;
+}
 #define MARL_CHECK(x)                                        \
   do {                                                       \
     const int32_t rc_ = (x);                                 \
@@ -311,6 +317,7 @@ int32_t marl_linear_attention(const marl_attention_dims* dims, marl_view q, marl
   const Plan p = plan_of(d, false);
   const bool used = d.n_steps > 0 && d.n_seqs > 0;
   for (const marl_view& x : {q, k, v, out}) MARL_CHECK(check_view(x, d.precision, used));
+  MARL_CHECK(check_output(out, d, d.n_heads, used));
   MARL_OPTIONAL_PTR(state); MARL_OPTIONAL_PTR(next_state);
   if (p.bytes > 0 && used) MARL_REQUIRE_PTR(workspace);
   if (decay == nullptr) return MARL_E_NULL;
@@ -355,6 +362,9 @@ int32_t marl_linear_attention_backward(const marl_attention_dims* dims, marl_vie
   const Plan p = plan_of(d, true);
   const bool used = d.n_steps > 0 && d.n_seqs > 0;
   for (const marl_view& x : {q, k, v, dout, dq, dk, dv}) MARL_CHECK(check_view(x, d.precision, used));
+  MARL_CHECK(check_output(dq, d, d.n_heads, used));
+  MARL_CHECK(check_output(dk, d, d.n_kv_heads, used));
+  MARL_CHECK(check_output(dv, d, d.n_kv_heads, used));
   MARL_OPTIONAL_PTR(state); MARL_OPTIONAL_PTR(dnext_state); MARL_OPTIONAL_PTR(dstate);
   if (p.bytes > 0 && used) MARL_REQUIRE_PTR(workspace);
   if (decay == nullptr) return MARL_E_NULL;
@@ -441,6 +451,7 @@ int32_t marl_linear_attention_step(const marl_attention_dims* dims, marl_view q,
   if (d.n_steps != 1) return MARL_E_SIZE;
   if (d.n_seqs == 0) return MARL_OK;
   for (const marl_view& x : {q, k, v, out}) MARL_CHECK(check_view(x, d.precision, true));
+  MARL_CHECK(check_output(out, d, d.n_heads, true));
   if (decay == nullptr) return MARL_E_NULL;
   if ((reinterpret_cast<uintptr_t>(decay) & 3u) != 0) return MARL_E_ALIGN;
   MARL_REQUIRE_PTR(state); MARL_REQUIRE_PTR(next_state);

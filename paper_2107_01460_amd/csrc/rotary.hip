@@ -251,6 +251,8 @@ int32_t marl_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, c
     if (in[u].data == nullptr || out[u].data == nullptr) return MARL_E_NULL;
     const uintptr_t pi = reinterpret_cast<uintptr_t>(in[u].data), po = reinterpret_cast<uintptr_t>(out[u].data);
     if (((pi | po) & odd) != 0) return MARL_E_ALIGN;
+    if ((out[u].step == 0 && d.n_steps > 1) || (out[u].seq == 0 && d.n_seqs > 1) || (out[u].head == 0 && (u == 0 ? d.n_heads : d.n_kv_heads) > 1))
+      return MARL_E_CONFIG;  // an output's elements are places of their own
     a.a[u] = {static_cast<const char*>(in[u].data), static_cast<char*>(out[u].data), in[u].step, in[u].seq, in[u].head, out[u].step, out[u].seq,
               out[u].head};
   }

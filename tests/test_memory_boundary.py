@@ -72,6 +72,21 @@ def test_attention_pointers(M):
     assert attend(M, dims(M, n_seqs=0), q=None, ws=None) == OK     # nothing to do
 
 
+def test_outputs_that_overlap_themselves(M):
+    L, d = M.lib(), dims(M)
+    one, V = dims(M, n_steps=1), M.binding.View
+    v = view(M)
+    for bad in (V(GOOD, 0, 32, 16), V(GOOD, 64, 0, 16), V(GOOD, 64, 32, 0)):
+        assert L.marl_linear_attention(C.byref(d), v, v, v, GOOD, None, None, bad, None, GOOD, None) == CONFIG
+        for k in range(3):
+            out = [bad if i == k else v for i in range(3)]
+            assert L.marl_linear_attention_backward(C.byref(d), v, v, v, GOOD, None, None, v, None, *out, None, GOOD, None) == CONFIG
+        assert L.marl_rotary(C.byref(d), v, v, GOOD, 8, 8, None, 0, 0, 0, v, bad, None) == CONFIG
+    assert L.marl_linear_attention_step(C.byref(one), v, v, v, GOOD, GOOD, None, V(GOOD, 0, 0, 16), GOOD, None) == CONFIG
+    assert L.marl_layer_norm(0, 4, 8, GOOD, 8, None, None, 1e-5, GOOD, 7, None, None, None) == CONFIG
+    assert L.marl_layer_norm_backward(0, 4, 8, GOOD, 8, GOOD, 8, None, GOOD, GOOD, GOOD, 0, None, None, None, None) == CONFIG
+
+
 def test_attention_workspace(M):
     n = C.c_int64()
     need = lambda back, **kw: (M.lib().marl_linear_attention_workspace(C.byref(dims(M, **kw)), back, C.byref(n)), n.value)[1]
