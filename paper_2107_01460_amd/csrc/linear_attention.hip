@@ -57,8 +57,8 @@ Plan plan_of(const marl_attention_dims& d, bool backward) {
 
 // ---- the states along the stretches: one thread per element ------------------------------------------------------------------------
 // Bound by memory: every stretch's state in and out (64 stretches of 8 states of 128 x 128: 67 MB, 15 us), 32 loads of a thread on their way together.
-// in: states each stretch forms by itself; out: the state that comes into it.  carry 0: an episode ended in the stretch (or the power of
-// the decay underflowed), nothing of what came in is left, infinities included.
+// in: states each stretch forms by itself; out: the state that comes into it.  Behind a stretch in which an episode ended nothing of what came in is left,
+// infinities and NaNs included; without an end these go on whatever the decay's power is.
 struct JoinArgs {
   float* states;
   const float *carry, *first;
@@ -86,7 +86,8 @@ __global__ void __launch_bounds__(256) join_kernel(JoinArgs a0, JoinArgs a1, uin
       if (p0 + u >= a.n) break;
       const int p = a.reverse ? a.n - 1 - (p0 + u) : p0 + u;
       a.states[(pair * a.n + p) * size + e] = run;
-      run = c[u] == 0.f ? v[u] : c[u] * run + v[u];
+      const float left = c[u] == kCarryEnded ? 0.f : c[u] != kCarryVanished ? c[u] * run : fabsf(run) < __builtin_inff() ? 0.f : run;
+      run = left + v[u];
     }
   }
   if (a.last != nullptr) a.last[at] = run;
