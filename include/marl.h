@@ -335,7 +335,10 @@ typedef struct marl_attention_dims {
  * one sequence with flags.  next_state (nullable; may be `state`) is zero where the last step ended an episode.  T = 0: next_state = state.
  * A step's output depends on the steps of its own episode up to it only, infinities and NaNs included.
  * bf16: products have bf16 operands where these are exact or split into parts, sums and the state are fp32; outputs are rounded once.
- * workspace: marl_linear_attention_workspace bytes.  Errors: MARL_E_NULL, MARL_E_ALIGN, MARL_E_SIZE, MARL_E_CONFIG, MARL_E_LAUNCH. */
+ * workspace: marl_linear_attention_workspace bytes.  Errors: MARL_E_NULL, MARL_E_ALIGN, MARL_E_CONFIG, MARL_E_LAUNCH; MARL_E_SIZE for n_seqs * n_heads
+ * above 2^26 or so many that a launch would have 2^32 work-items: 64 a sequence and head for each 32 columns or part of them (32 to 64: 128, 65 to
+ * 96: 192, more: 256), of dim_v, in the gradient 3 times (dim_k = dim_v), otherwise twice those of dim_k and once those of dim_v; the workspace's query
+ * says so too. */
 int32_t marl_linear_attention(const marl_attention_dims* dims, marl_view q, marl_view k, marl_view v, const float* decay,
                               const float* state, const uint8_t* done, marl_view out, float* next_state, void* workspace,
                               void* stream);

@@ -150,6 +150,9 @@ inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) &
     if ((p) != nullptr && marl::misaligned(p)) return MARL_E_ALIGN; \
   } while (0)
 
+// A launch has fewer than 2^32 work-items along a dimension of its grid.
+inline bool launchable(int64_t blocks, int64_t threads) { return blocks * threads < ((int64_t)1 << 32); }
+
 inline int32_t launch_status() { return hipGetLastError() == hipSuccess ? MARL_OK : MARL_E_LAUNCH; }
 
 // ---- Philox4x32-10 (Salmon et al., SC'11, Section 4) -------------------------------------

@@ -201,8 +201,26 @@ int32_t check_dims(const marl_attention_dims* d) {
   if (d->n_heads < 1 || d->n_kv_heads < 1 || d->n_heads % d->n_kv_heads != 0) return MARL_E_CONFIG;
   if (d->dim_k < 1 || d->dim_k > kMaxDim || d->dim_v < 1 || d->dim_v > kMaxDim) return MARL_E_CONFIG;
   if (d->seqs_per_flag < 1 || d->n_seqs % d->seqs_per_flag != 0) return MARL_E_CONFIG;
-  if ((int64_t)d->n_seqs * d->n_heads > ((int64_t)1 << 26)) return MARL_E_SIZE;  // workgroup counts are 32-bit
+  const int64_t pairs = (int64_t)d->n_seqs * d->n_heads;
+  if (pairs > ((int64_t)1 << 26) || pairs * d->n_steps > ((int64_t)1 << 48)) return MARL_E_SIZE;  // (workspaces of 64-bit sizes)
   return MARL_OK;
+}
+// Every launch of a call within what a grid can be, before the first of them.  (The gradient's scans have two work-items or more for each element of a step
+// of dk or dv, two heads sharing one at least, so that sum_heads_kernel's 32-bit places fit too.)
+int32_t check_launches(const marl_attention_dims& d, const Plan& p, bool backward) {
+  auto scan = [&](int roles, int dz) {
+    const int slices = scan_slices(dz), group = slices == 1 ? scan_pairs<1>() : slices == 2 ? scan_pairs<2>() : scan_pairs<4>();
+    return launchable((p.pairs + group - 1) / group * p.n_stretches * roles, 64 * slices * group);
+  };
+  bool fits = true;
+  if (d.n_steps == 0 || p.n_stretches > 1) fits = launchable((p.pairs * d.dim_k * d.dim_v + 255) / 256, 256);  // join
+  if (d.n_steps > 0) {
+    if (p.n_stretches > 1) fits = fits && scan(backward ? 2 : 1, d.dim_v);
+    if (!backward) fits = fits && scan(1, d.dim_v);
+    else if (d.dim_k == d.dim_v) fits = fits && scan(3, d.dim_k);
+    else fits = fits && scan(2, d.dim_k) && scan(1, d.dim_v);
+  }
+  return fits ? MARL_OK : MARL_E_SIZE;
 }
 int32_t check_view(const marl_view& v, int precision, bool used) {
   if (!used) return MARL_OK;
@@ -242,21 +260,18 @@ int32_t scan(ScanArgs a, const marl_attention_dims& d, const Plan& p, int dx, in
   a.n_stretches = p.n_stretches;
   a.stretch = p.stretch;
   a.pairs = (uint32_t)p.pairs;
-  if (p.pairs * a.n_roles * a.n_stretches >= ((int64_t)1 << 31)) return MARL_E_SIZE;
   (d.precision == 0 ? launch_scan_f32 : launch_scan_bf16)(a, dx, dz, state_only, s);
   return launch_status();
 }
 
 int32_t join(JoinArgs a0, JoinArgs a1, int n_args, const marl_attention_dims& d, const Plan& p, hipStream_t s) {
   const int64_t total = p.pairs * d.dim_k * d.dim_v, blocks = (total + 255) / 256;
-  if (blocks >= ((int64_t)1 << 31)) return MARL_E_SIZE;
   hipLaunchKernelGGL(join_kernel, dim3((unsigned)blocks, n_args), dim3(256), 0, s, a0, a1, (uint32_t)(d.dim_k * d.dim_v), total);
   return launch_status();
 }
 
 int32_t sum_heads(const marl_attention_dims& d, const Plan& p, const float* part, const marl_view& out, int dim, hipStream_t s) {
   const int64_t per_step = (int64_t)d.n_seqs * d.n_kv_heads * dim;
-  if (per_step >= ((int64_t)1 << 31)) return MARL_E_SIZE;
   auto launch = [&](auto zero, auto v) {
     typedef decltype(zero) T;
     constexpr int V = decltype(v)::value;
@@ -277,11 +292,14 @@ template <class T>
 int32_t step(const marl_attention_dims& d, const marl_view& q, const marl_view& k, const marl_view& v, const float* decay, const float* state,
              const uint8_t* fresh, const marl_view& out, float* next, hipStream_t s) {
   const uint32_t pairs = (uint32_t)d.n_seqs * (uint32_t)d.n_heads;
-#define MARL_STEP(V, TEAM)                                                                                                              \
-  hipLaunchKernelGGL((step_kernel<T, V, TEAM>), dim3((pairs + 256 / TEAM - 1) / (256 / TEAM)), dim3(256), 0, s, (const T*)q.data,       \
-                     (const T*)k.data, (const T*)v.data, (T*)out.data, q.seq, q.head, k.seq, k.head, v.seq, v.head, out.seq, out.head, \
-                     decay, state, fresh, next, pairs, (uint32_t)d.n_heads, (uint32_t)(d.n_heads / d.n_kv_heads),                      \
-                     (uint32_t)d.seqs_per_flag, d.dim_k, d.dim_v, d.scale)
+#define MARL_STEP(V, TEAM)                                                                                                               \
+  do {                                                                                                                                   \
+    const uint32_t blocks = (pairs + 256 / TEAM - 1) / (256 / TEAM);                                                                     \
+    if (!launchable(blocks, 256)) return MARL_E_SIZE;                                                                                    \
+    hipLaunchKernelGGL((step_kernel<T, V, TEAM>), dim3(blocks), dim3(256), 0, s, (const T*)q.data, (const T*)k.data, (const T*)v.data,   \
+                       (T*)out.data, q.seq, q.head, k.seq, k.head, v.seq, v.head, out.seq, out.head, decay, state, fresh, next, pairs,  \
+                       (uint32_t)d.n_heads, (uint32_t)(d.n_heads / d.n_kv_heads), (uint32_t)d.seqs_per_flag, d.dim_k, d.dim_v, d.scale); \
+  } while (0)
   // A wavefront a state, or a workgroup from more than 32 x 32 on, with its loads on their way together (16 384 states of 32 x 32: 99 against 120 us;
   // of 32 x 64 199 against 186, 8192 of 64 x 64 210 against 192; columns one by one: the same to 2 %).
   if (d.dim_v % 4 == 0) {
@@ -306,7 +324,9 @@ extern "C" {
 int32_t marl_linear_attention_workspace(const marl_attention_dims* dims, int32_t backward, int64_t* bytes) {
   MARL_CHECK(check_dims(dims));
   if (bytes == nullptr) return MARL_E_NULL;
-  *bytes = plan_of(*dims, backward != 0).bytes;
+  const Plan p = plan_of(*dims, backward != 0);
+  MARL_CHECK(check_launches(*dims, p, backward != 0));
+  *bytes = p.bytes;
   return MARL_OK;
 }
 
@@ -316,6 +336,7 @@ int32_t marl_linear_attention(const marl_attention_dims* dims, marl_view q, marl
   MARL_CHECK(check_dims(dims));
   const marl_attention_dims& d = *dims;
   const Plan p = plan_of(d, false);
+  MARL_CHECK(check_launches(d, p, false));
   const bool used = d.n_steps > 0 && d.n_seqs > 0;
   for (const marl_view& x : {q, k, v, out}) MARL_CHECK(check_view(x, d.precision, used));
   MARL_CHECK(check_output(out, d, d.n_heads, used));
@@ -361,6 +382,7 @@ int32_t marl_linear_attention_backward(const marl_attention_dims* dims, marl_vie
   MARL_CHECK(check_dims(dims));
   const marl_attention_dims& d = *dims;
   const Plan p = plan_of(d, true);
+  MARL_CHECK(check_launches(d, p, true));
   const bool used = d.n_steps > 0 && d.n_seqs > 0;
   for (const marl_view& x : {q, k, v, dout, dq, dk, dv}) MARL_CHECK(check_view(x, d.precision, used));
   MARL_CHECK(check_output(dq, d, d.n_heads, used));

@@ -201,8 +201,9 @@ int32_t rotate(RotaryArgs a, bool interleaved, hipStream_t s) {
   const uint32_t items = inside ? a.dim / E : a.pair_items + (a.dim - a.rotary) / E, per_token = (a.heads[0] + a.heads[1]) * items;
   a.items = divisor(items);
   a.per_token = divisor(per_token);
+  if (a.tokens > ((int64_t)1 << 40) / per_token) return MARL_E_SIZE;  // (the product below)
   const int64_t blocks = (a.tokens * per_token + 256 * kItems - 1) / (256 * kItems);
-  if (blocks >= ((int64_t)1 << 31)) return MARL_E_SIZE;
+  if (!launchable(blocks, 256)) return MARL_E_SIZE;
   if (interleaved) hipLaunchKernelGGL((rotary_kernel<T, E, true>), dim3((unsigned)blocks), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((rotary_kernel<T, E, false>), dim3((unsigned)blocks), dim3(256), 0, s, a);
   return launch_status();
@@ -224,7 +225,7 @@ int32_t marl_rotary_table(const marl_rotary_dims* dims, float* table, void* stre
   if (d.scaling == 3 && (!(d.trained_length > 0.f) || !(d.fast > d.slow))) return MARL_E_CONFIG;
   MARL_REQUIRE_PTR(table);
   const int64_t blocks = ((int64_t)d.n_positions * (d.rotary_dim / 2) + 255) / 256;
-  if (blocks >= ((int64_t)1 << 31)) return MARL_E_SIZE;
+  if (!launchable(blocks, 256)) return MARL_E_SIZE;
   hipLaunchKernelGGL(rotary_table_kernel, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, d, table);
   return launch_status();
 }
