@@ -3,13 +3,15 @@
 The memory is linear attention with a decay for each head, on queries and keys turned by rotary positions (the step in the episode), between
 layer norms.  It has two forms with the same parameters: ``forward`` takes whole rollouts, [T][B][D] observations with the done flags of a
 trajectory, and has gradients; ``step`` takes one step of every sequence and a state of constant size, as an acting loop does.  The norms, the
-rotation and the attention run in the library's kernels; the projections between them are plain products of torch.
+rotation and the attention run in the library's kernels; the projections between them are plain products of torch.  The kernels have first derivatives;
+asking for a second raises.
 
 B sequences are the agents of all environments, an environment's side by side, as in the trajectory arrays.
 """
 import math
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -29,6 +31,7 @@ class Attend(torch.autograd.Function):
         return out, next_state
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout, dnext_state):
         q, k, v, decay, state, done = ctx.saved_tensors
         dq, dk, dv = (torch.empty_like(x, memory_format=torch.contiguous_format) for x in (q, k, v))
@@ -52,6 +55,7 @@ class LayerNorm(torch.autograd.Function):
         return out.reshape(x.shape)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         rows, weight, mean, rstd = ctx.saved_tensors
         dx = torch.empty_like(rows)
@@ -72,6 +76,7 @@ class Rotate(torch.autograd.Function):
         return q_out, k_out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dq, dk):
         table, positions = ctx.saved_tensors
         q_out, k_out = torch.empty_like(dq, memory_format=torch.contiguous_format), torch.empty_like(dk, memory_format=torch.contiguous_format)
