@@ -16,11 +16,17 @@ from torch.autograd.function import once_differentiable
 from . import binding as B
 
 
+def _rows(x):
+    """x with its last dimension contiguous, as the kernels read it: x itself but for transposed tensors and expanded numbers."""
+    return x if x.shape[-1] <= 1 or x.stride(-1) == 1 else x.contiguous()
+
+
 class Attend(torch.autograd.Function):
     """(out, next_state) = linear attention of q, k, v [T][B][heads][D]; gradients of q, k, v and the state."""
 
     @staticmethod
     def forward(ctx, q, k, v, decay, state, done, scale):
+        q, k, v, state = _rows(q), _rows(k), _rows(v), None if state is None else state.contiguous()
         T, n, H, Dk = q.shape
         out = torch.empty((T, n, H, v.shape[3]), dtype=q.dtype, device=q.device)
         next_state = torch.empty((n, H, Dk, v.shape[3]), dtype=torch.float32, device=q.device)
@@ -46,7 +52,7 @@ class LayerNorm(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, weight, bias, eps):
-        rows = x.reshape(-1, x.shape[-1])
+        rows = _rows(x.reshape(-1, x.shape[-1]))
         out = torch.empty_like(rows)
         mean, rstd = (torch.empty(rows.shape[0], dtype=torch.float32, device=x.device) for _ in range(2))
         B.layer_norm(rows, weight, bias, out, mean, rstd, eps)
@@ -61,7 +67,7 @@ class LayerNorm(torch.autograd.Function):
         dx = torch.empty_like(rows)
         dw = None if weight is None else torch.empty_like(weight)
         db = torch.empty(rows.shape[1], dtype=torch.float32, device=rows.device) if ctx.has_bias else None
-        B.layer_norm_backward(dout.reshape(rows.shape), rows, weight, mean, rstd, dx, dw, db, B.alloc_workspace(B.layer_norm_workspace(*rows.shape)))
+        B.layer_norm_backward(_rows(dout.reshape(rows.shape)), rows, weight, mean, rstd, dx, dw, db, B.alloc_workspace(B.layer_norm_workspace(*rows.shape)))
         return dx.reshape(dout.shape), dw, db, None
 
 
@@ -72,7 +78,7 @@ class Rotate(torch.autograd.Function):
     def forward(ctx, q, k, table, positions):
         ctx.save_for_backward(table, positions)
         q_out, k_out = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k))
-        B.rotary(q, k, table, q_out, k_out, positions=positions)
+        B.rotary(_rows(q), _rows(k), table, q_out, k_out, positions=positions)
         return q_out, k_out
 
     @staticmethod
@@ -80,7 +86,7 @@ class Rotate(torch.autograd.Function):
     def backward(ctx, dq, dk):
         table, positions = ctx.saved_tensors
         q_out, k_out = torch.empty_like(dq, memory_format=torch.contiguous_format), torch.empty_like(dk, memory_format=torch.contiguous_format)
-        B.rotary(dq, dk, table, q_out, k_out, positions=positions, inverse=True)
+        B.rotary(_rows(dq), _rows(dk), table, q_out, k_out, positions=positions, inverse=True)
         return q_out, k_out, None, None
 
 
