@@ -356,6 +356,11 @@ def _floats(t, shape, name):
     return t.data_ptr()
 
 
+def _written(*outputs):
+    """Tells autograd that these (None: absent) have changed, so that a backward pass that kept their old values raises."""
+    torch.autograd.graph.increment_version([t for t in outputs if t is not None])
+
+
 def _view(t, shape, dtype, name):
     if t.dtype != dtype or t.shape != shape or not t.is_cuda:
         raise _refused(f"{name}: {dtype} {list(shape)} on the GPU")
@@ -426,6 +431,7 @@ def linear_attention(q, k, v, decay, out, workspace=None, state=None, next_state
                                    _view(v, (T, B, Hk, Dv), dt, "v"), _floats(decay, (H,), "decay"), _floats(state, states, "state"), flags,
                                    _view(out, (T, B, H, Dv), dt, "out"), _floats(next_state, states, "next_state"),
                                    _workspace(workspace, need.value), _stream(stream)))
+    _written(out, next_state)
 
 
 def linear_attention_backward(q, k, v, decay, dout, dq, dk, dv, workspace=None, state=None, dnext_state=None, dstate=None, done=None, scale=1.0,
@@ -439,6 +445,7 @@ def linear_attention_backward(q, k, v, decay, dout, dq, dk, dv, workspace=None, 
         C.byref(dims), _view(q, qs, dt, "q"), _view(k, ks, dt, "k"), _view(v, vs, dt, "v"), _floats(decay, (H,), "decay"),
         _floats(state, states, "state"), flags, _view(dout, os, dt, "dout"), _floats(dnext_state, states, "dnext_state"), _view(dq, qs, dt, "dq"),
         _view(dk, ks, dt, "dk"), _view(dv, vs, dt, "dv"), _floats(dstate, states, "dstate"), _workspace(workspace, need.value), _stream(stream)))
+    _written(dq, dk, dv, dstate)
 
 
 def linear_attention_step(q, k, v, decay, state, out, next_state=None, done=None, scale=1.0, stream=None):
@@ -456,6 +463,7 @@ def linear_attention_step(q, k, v, decay, state, out, next_state=None, done=None
         C.byref(dims), _step_view(q, (B, H, Dk), dt, "q"), _step_view(k, (B, Hk, Dk), dt, "k"), _step_view(v, (B, Hk, Dv), dt, "v"),
         _floats(decay, (H,), "decay"), before, flags, _step_view(out, (B, H, Dv), dt, "out"),
         before if next_state is None else _floats(next_state, states, "next_state"), _stream(stream)))
+    _written(out, state if next_state is None else next_state)
 
 
 def _rows(t, shape, dtype, name):
@@ -473,6 +481,7 @@ def layer_norm(x, weight, bias, out, mean=None, rstd=None, eps=1e-5, stream=None
     _check(lib().marl_layer_norm(precision, n, width, *_rows(x, shape, dt, "x"), _floats(weight, (width,), "weight"),
                                  _floats(bias, (width,), "bias"), eps, *_rows(out, shape, dt, "out"), _floats(mean, (n,), "mean"),
                                  _floats(rstd, (n,), "rstd"), _stream(stream)))
+    _written(out, mean, rstd)
 
 
 def layer_norm_workspace(rows, width):
@@ -493,6 +502,7 @@ def layer_norm_backward(dout, x, weight, mean, rstd, dx, dweight=None, dbias=Non
         precision, n, width, *_rows(dout, shape, dt, "dout"), *_rows(x, shape, dt, "x"), _floats(weight, (width,), "weight"),
         _floats(mean, (n,), "mean"), _floats(rstd, (n,), "rstd"), *_rows(dx, shape, dt, "dx"), _floats(dweight, (width,), "dweight"),
         _floats(dbias, (width,), "dbias"), _workspace(workspace, need), _stream(stream)))
+    _written(dx, dweight, dbias)
 
 
 ROTARY_SCALING = {None: 0, "linear": 1, "base": 2, "by_turns": 3}
@@ -529,6 +539,7 @@ def rotary(q, k, table, q_out, k_out, positions=None, first_position=0, interlea
         C.byref(AttentionDims.from_buffer_copy(_DIMS.pack(precision, T, B, H, Hk, D, D, per, 1.0))), _view(q, qs, dt, "q"),
         none if k is None else _view(k, ks, dt, "k"), _floats(table, (P, R), "table"), P, R, at, first_position, interleaved, inverse,
         _view(q_out, qs, dt, "q_out"), none if k is None else _view(k_out, ks, dt, "k_out"), _stream(stream)))
+    _written(q_out, k_out)
 
 
 KERNEL_CLASSES = {"gemm_nn": 0, "gemm_nt": 1, "gemm_tn": 2, "env_step": 3, "gae": 4, "fused_train": 5, "rollout": 6}
