@@ -417,9 +417,9 @@ def _workspace(t, need):
         if need > 0:
             raise _refused(f"workspace: {need} bytes")
         return None
-    if t.nbytes < need:
-        raise _refused(f"workspace: {need} bytes")
-    return _ptr(t)
+    if t.nbytes < need or not t.is_contiguous() or not t.is_cuda:
+        raise _refused(f"workspace: {need} contiguous bytes on the GPU")
+    return t.data_ptr()
 
 
 def linear_attention(q, k, v, decay, out, workspace=None, state=None, next_state=None, done=None, scale=1.0, stream=None):
