@@ -332,7 +332,7 @@ typedef struct marl_attention_dims {
  *   S_t = keep_t g S_{t-1} + k_t v_t^T,   out_t = scale * S_t^T q_t,   next_state = keep_T S_{T-1}
  * S_{-1} = state [B][n_heads][dim_k][dim_v] (NULL: zero), keep_t = 0 where done [T][B / seqs_per_flag] (NULL: none) is nonzero at t - 1,
  * otherwise 1: a nonzero done_t says that step t ended an episode, as in marl_traj, so packed sequences of different lengths are
- * one sequence with flags.  next_state (nullable; may be `state`) is zero where the last step ended an episode.  T = 0: next_state = state.
+ * one sequence with flags.  next_state (nullable; may be `state`, MARL_E_CONFIG where it overlaps it otherwise) is zero where the last step ended an episode.  T = 0: next_state = state.
  * A step's output depends on the steps of its own episode up to it only, infinities and NaNs included.
  * bf16: products have bf16 operands where these are exact or split into parts, sums and the state are fp32; outputs are rounded once.
  * workspace: marl_linear_attention_workspace bytes.  Errors: MARL_E_NULL, MARL_E_ALIGN, MARL_E_CONFIG, MARL_E_LAUNCH; MARL_E_SIZE for n_seqs * n_heads
@@ -343,7 +343,7 @@ int32_t marl_linear_attention(const marl_attention_dims* dims, marl_view q, marl
                               const float* state, const uint8_t* done, marl_view out, float* next_state, void* workspace,
                               void* stream);
 
-/* Its gradient: dq, dk, dv, and dstate [B][n_heads][dim_k][dim_v] (nullable, not dnext_state itself) from dout and dnext_state (NULL: zero).  dk and dv of a head that
+/* Its gradient: dq, dk, dv, and dstate [B][n_heads][dim_k][dim_v] (nullable; MARL_E_CONFIG where it overlaps state or dnext_state) from dout and dnext_state (NULL: zero).  dk and dv of a head that
  * query heads share are sums over these, in a fixed order.  The decays are constants of the layer: they have no gradient. */
 int32_t marl_linear_attention_backward(const marl_attention_dims* dims, marl_view q, marl_view k, marl_view v,
                                        const float* decay, const float* state, const uint8_t* done, marl_view dout,
@@ -352,7 +352,7 @@ int32_t marl_linear_attention_backward(const marl_attention_dims* dims, marl_vie
 
 /* One step, for acting: next_state = keep g state + k v^T, out = scale * next_state^T q, with n_steps = 1 (the views' step strides
  * are not used).  fresh [B / seqs_per_flag] (NULL: none): nonzero where an episode begins with this step, keep = 0 there.
- * next_state may be `state`. */
+ * next_state may be `state` (MARL_E_CONFIG where it overlaps it otherwise). */
 int32_t marl_linear_attention_step(const marl_attention_dims* dims, marl_view q, marl_view k, marl_view v,
                                    const float* decay, const float* state, const uint8_t* fresh, marl_view out,
                                    float* next_state, void* stream);

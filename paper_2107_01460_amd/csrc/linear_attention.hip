@@ -233,6 +233,12 @@ int32_t check_output(const marl_view& v, const marl_attention_dims& d, int heads
   const bool overlaps = (v.step == 0 && d.n_steps > 1) || (v.seq == 0 && d.n_seqs > 1) || (v.head == 0 && heads > 1);
   return overlaps ? MARL_E_CONFIG : MARL_OK;
 }
+// Two arrays of states share memory
+bool overlapping(const marl_attention_dims& d, const float* a, const float* b) {
+  if (a == nullptr || b == nullptr) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return (x < y ? y - x : x - y) < (uintptr_t)d.n_seqs * d.n_heads * d.dim_k * d.dim_v * 4;
+}
 #define MARL_CHECK(x)                                        \
   do {                                                       \
     const int32_t rc_ = (x);                                 \
@@ -341,6 +347,7 @@ int32_t marl_linear_attention(const marl_attention_dims* dims, marl_view q, marl
   for (const marl_view& x : {q, k, v, out}) MARL_CHECK(check_view(x, d.precision, used));
   MARL_CHECK(check_output(out, d, d.n_heads, used));
   MARL_OPTIONAL_PTR(state); MARL_OPTIONAL_PTR(next_state);
+  if (next_state != state && overlapping(d, next_state, state)) return MARL_E_CONFIG;
   if (p.bytes > 0 && used) MARL_REQUIRE_PTR(workspace);
   if (decay == nullptr) return MARL_E_NULL;
   if ((reinterpret_cast<uintptr_t>(decay) & 3u) != 0) return MARL_E_ALIGN;
@@ -389,6 +396,7 @@ int32_t marl_linear_attention_backward(const marl_attention_dims* dims, marl_vie
   MARL_CHECK(check_output(dk, d, d.n_kv_heads, used));
   MARL_CHECK(check_output(dv, d, d.n_kv_heads, used));
   MARL_OPTIONAL_PTR(state); MARL_OPTIONAL_PTR(dnext_state); MARL_OPTIONAL_PTR(dstate);
+  if (overlapping(d, dstate, state) || overlapping(d, dstate, dnext_state)) return MARL_E_CONFIG;
   if (p.bytes > 0 && used) MARL_REQUIRE_PTR(workspace);
   if (decay == nullptr) return MARL_E_NULL;
   if ((reinterpret_cast<uintptr_t>(decay) & 3u) != 0) return MARL_E_ALIGN;
@@ -478,6 +486,7 @@ int32_t marl_linear_attention_step(const marl_attention_dims* dims, marl_view q,
   if (decay == nullptr) return MARL_E_NULL;
   if ((reinterpret_cast<uintptr_t>(decay) & 3u) != 0) return MARL_E_ALIGN;
   MARL_REQUIRE_PTR(state); MARL_REQUIRE_PTR(next_state);
+  if (next_state != state && overlapping(d, next_state, state)) return MARL_E_CONFIG;
   return (d.precision == 0 ? step<float> : step<bf16_t>)(d, q, k, v, decay, state, fresh, out, next_state, (hipStream_t)stream);
 }
 

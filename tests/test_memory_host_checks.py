@@ -4,7 +4,7 @@ import ctypes as C
 import pytest
 import torch
 
-from test_memory_boundary import CONFIG, GOOD, M, dims, view  # noqa: F401  (M: the fixture)
+from test_memory_boundary import CONFIG, GOOD, OK, M, dims, view  # noqa: F401  (M: the fixture)
 
 
 def test_workspace_in_host_memory(M):  # noqa: F811
@@ -13,3 +13,22 @@ def test_workspace_in_host_memory(M):  # noqa: F811
         with pytest.raises(M.MarlError, match="on the GPU"):
             M.binding._workspace(torch.empty(256, dtype=torch.uint8), need)
     assert M.binding._workspace(None, 0) is None
+
+
+def test_gradient_of_the_state_over_states(M):  # noqa: F811
+    """dstate is written while other workgroups still read state and dnext_state: it overlaps neither, wholly or in part."""
+    d, v = dims(M), view(M)
+    size = d.n_seqs * d.n_heads * d.dim_k * d.dim_v * 4
+    grad = lambda state, dnext, dstate, d=d: M.lib().marl_linear_attention_backward(C.byref(d), v, v, v, GOOD, state, None, v, dnext, v, v, v, dstate, GOOD, None)
+    for at in (GOOD, GOOD + 16, GOOD + size - 16, GOOD - 16, GOOD - size + 16):
+        assert grad(GOOD, None, at) == CONFIG and grad(None, GOOD, at) == CONFIG
+    nothing = dims(M, n_seqs=0)
+    assert grad(GOOD, GOOD, GOOD, nothing) == OK
+
+
+def test_next_state_over_a_part_of_the_state(M):  # noqa: F811
+    """next_state may be the state, but not a part of it and something else."""
+    d, one, v = dims(M), dims(M, n_steps=1), view(M)
+    for at in (GOOD + 16, GOOD - 16):
+        assert M.lib().marl_linear_attention(C.byref(d), v, v, v, GOOD, GOOD, None, view(M, GOOD + (1 << 20)), at, GOOD, None) == CONFIG
+        assert M.lib().marl_linear_attention_step(C.byref(one), v, v, v, GOOD, GOOD, None, view(M, GOOD + (1 << 20)), at, None) == CONFIG
