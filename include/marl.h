@@ -313,7 +313,7 @@ int32_t marl_timing_read(int32_t kernel_class, double* total_ms, int64_t* launch
 
 /* An array [T][B][heads][dim] in place: element (t, b, h, d) at data + (t * step + b * seq + h * head + d) elements, `data` aligned to its
  * elements.  An input may be broadcast (strides of zero).  Outputs overlap neither themselves (MARL_E_CONFIG for a stride of zero) nor each other
- * nor an input (marl_rotary: an output may be its input). */
+ * nor an input (MARL_E_CONFIG where the two begin at one place; marl_rotary: an output may be its input, with the same strides). */
 typedef struct marl_view {
   void* data;
   int64_t step, seq, head;

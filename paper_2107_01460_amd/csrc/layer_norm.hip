@@ -339,6 +339,8 @@ int32_t check_rows(const void* p, int32_t precision) {
   return (reinterpret_cast<uintptr_t>(p) & (precision == 0 ? 3u : 1u)) != 0 ? MARL_E_ALIGN : MARL_OK;
 }
 bool overlapping(int64_t rows, int32_t width, int64_t stride) { return rows > 1 && (stride < 0 ? -stride : stride) < width; }  // rows of an output
+// Rows written over the ones that are read, in other places
+bool moved(int64_t rows, const void* out, int64_t out_stride, const void* in, int64_t in_stride) { return out == in && rows > 1 && out_stride != in_stride; }
 int32_t check_floats(const float* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0 ? MARL_E_ALIGN : MARL_OK; }
 
 }  // namespace
@@ -355,6 +357,7 @@ int32_t marl_layer_norm(int32_t precision, int64_t n_rows, int32_t width, const 
   if (rc != MARL_OK || n_rows == 0) return rc;
   if (!(eps >= 0.f) || overlapping(n_rows, width, y_stride)) return MARL_E_CONFIG;
   if ((rc = check_rows(x, precision)) != MARL_OK || (rc = check_rows(y, precision)) != MARL_OK) return rc;
+  if (moved(n_rows, y, y_stride, x, x_stride)) return MARL_E_CONFIG;
   for (const float* p : {weight, bias, (const float*)mean, (const float*)rstd})
     if ((rc = check_floats(p)) != MARL_OK) return rc;
   hipStream_t s = (hipStream_t)stream;
@@ -386,7 +389,7 @@ int32_t marl_layer_norm_backward(int32_t precision, int64_t n_rows, int32_t widt
   if (n_rows > 0) {
     for (const void* p : {dy, x, (const void*)dx})
       if ((rc = check_rows(p, precision)) != MARL_OK) return rc;
-    if (overlapping(n_rows, width, dx_stride)) return MARL_E_CONFIG;
+    if (overlapping(n_rows, width, dx_stride) || moved(n_rows, dx, dx_stride, dy, dy_stride) || moved(n_rows, dx, dx_stride, x, x_stride)) return MARL_E_CONFIG;
     if (mean == nullptr || rstd == nullptr) return MARL_E_NULL;
     if ((rc = check_floats(mean)) != MARL_OK || (rc = check_floats(rstd)) != MARL_OK) return rc;
     if (weights) MARL_REQUIRE_PTR(workspace);

@@ -1,4 +1,5 @@
 // Linear attention: the calls, the join of the stretches of a long sequence, the sum over shared heads, the single step.
+#include <initializer_list>
 #include <type_traits>
 
 #include "linear_attention.h"
@@ -233,6 +234,13 @@ int32_t check_output(const marl_view& v, const marl_attention_dims& d, int heads
   const bool overlaps = (v.step == 0 && d.n_steps > 1) || (v.seq == 0 && d.n_seqs > 1) || (v.head == 0 && heads > 1);
   return overlaps ? MARL_E_CONFIG : MARL_OK;
 }
+// An output that begins where one of the others does
+int32_t check_places(const marl_view& out, std::initializer_list<marl_view> others, bool used) {
+  if (used)
+    for (const marl_view& x : others)
+      if (x.data == out.data) return MARL_E_CONFIG;
+  return MARL_OK;
+}
 // Two arrays of states share memory
 bool overlapping(const marl_attention_dims& d, const float* a, const float* b) {
   if (a == nullptr || b == nullptr) return false;
@@ -294,24 +302,27 @@ int32_t sum_heads(const marl_attention_dims& d, const Plan& p, const float* part
   return launch_status();
 }
 
+// Threads that take a state: a wavefront, or a workgroup from more than 32 x 32 on, with its loads on their way together (16 384 states of 32 x 32: 99 against
+// 120 us; of 32 x 64 199 against 186, 8192 of 64 x 64 210 against 192; columns one by one: the same to 2 %, and a thread for each of them).
+int step_team(const marl_attention_dims& d) { return d.dim_k * d.dim_v <= 1024 && (d.dim_v % 4 == 0 || d.dim_v <= 64) ? 64 : 256; }
+int64_t step_blocks(const marl_attention_dims& d) {
+  const int64_t pairs = (int64_t)d.n_seqs * d.n_heads, teams = 256 / step_team(d);
+  return (pairs + teams - 1) / teams;
+}
+
 template <class T>
 int32_t step(const marl_attention_dims& d, const marl_view& q, const marl_view& k, const marl_view& v, const float* decay, const float* state,
              const uint8_t* fresh, const marl_view& out, float* next, hipStream_t s) {
   const uint32_t pairs = (uint32_t)d.n_seqs * (uint32_t)d.n_heads;
-#define MARL_STEP(V, TEAM)                                                                                                               \
-  do {                                                                                                                                   \
-    const uint32_t blocks = (pairs + 256 / TEAM - 1) / (256 / TEAM);                                                                     \
-    if (!launchable(blocks, 256)) return MARL_E_SIZE;                                                                                    \
-    hipLaunchKernelGGL((step_kernel<T, V, TEAM>), dim3(blocks), dim3(256), 0, s, (const T*)q.data, (const T*)k.data, (const T*)v.data,   \
-                       (T*)out.data, q.seq, q.head, k.seq, k.head, v.seq, v.head, out.seq, out.head, decay, state, fresh, next, pairs,  \
-                       (uint32_t)d.n_heads, (uint32_t)(d.n_heads / d.n_kv_heads), (uint32_t)d.seqs_per_flag, d.dim_k, d.dim_v, d.scale); \
-  } while (0)
-  // A wavefront a state, or a workgroup from more than 32 x 32 on, with its loads on their way together (16 384 states of 32 x 32: 99 against 120 us;
-  // of 32 x 64 199 against 186, 8192 of 64 x 64 210 against 192; columns one by one: the same to 2 %).
+#define MARL_STEP(V, TEAM)                                                                                                              \
+  hipLaunchKernelGGL((step_kernel<T, V, TEAM>), dim3((unsigned)step_blocks(d)), dim3(256), 0, s, (const T*)q.data, (const T*)k.data,    \
+                     (const T*)v.data, (T*)out.data, q.seq, q.head, k.seq, k.head, v.seq, v.head, out.seq, out.head, decay, state, fresh, \
+                     next, pairs, (uint32_t)d.n_heads, (uint32_t)(d.n_heads / d.n_kv_heads), (uint32_t)d.seqs_per_flag, d.dim_k,        \
+                     d.dim_v, d.scale)
   if (d.dim_v % 4 == 0) {
-    if (d.dim_k * d.dim_v <= 1024) MARL_STEP(4, 64);
+    if (step_team(d) == 64) MARL_STEP(4, 64);
     else MARL_STEP(4, 256);
-  } else if (d.dim_v <= 64 && d.dim_k * d.dim_v <= 1024) {
+  } else if (step_team(d) == 64) {
     MARL_STEP(1, 64);
   } else {
     MARL_STEP(1, 256);
@@ -351,6 +362,7 @@ int32_t marl_linear_attention(const marl_attention_dims* dims, marl_view q, marl
   if (p.bytes > 0 && used) MARL_REQUIRE_PTR(workspace);
   if (decay == nullptr) return MARL_E_NULL;
   if ((reinterpret_cast<uintptr_t>(decay) & 3u) != 0) return MARL_E_ALIGN;
+  MARL_CHECK(check_places(out, {q, k, v}, used));
   if (d.n_seqs == 0) return MARL_OK;
   hipStream_t s = (hipStream_t)stream;
   if (d.n_steps == 0) return next_state == nullptr ? MARL_OK : join({nullptr, nullptr, state, next_state, 0, 0}, {}, 1, d, p, s);
@@ -400,6 +412,9 @@ int32_t marl_linear_attention_backward(const marl_attention_dims* dims, marl_vie
   if (p.bytes > 0 && used) MARL_REQUIRE_PTR(workspace);
   if (decay == nullptr) return MARL_E_NULL;
   if ((reinterpret_cast<uintptr_t>(decay) & 3u) != 0) return MARL_E_ALIGN;
+  MARL_CHECK(check_places(dq, {q, k, v, dout, dk, dv}, used));
+  MARL_CHECK(check_places(dk, {q, k, v, dout, dv}, used));
+  MARL_CHECK(check_places(dv, {q, k, v, dout}, used));
   if (d.n_seqs == 0) return MARL_OK;
   hipStream_t s = (hipStream_t)stream;
   if (d.n_steps == 0) return dstate == nullptr ? MARL_OK : join({nullptr, nullptr, dnext_state, dstate, 0, 1}, {}, 1, d, p, s);
@@ -479,7 +494,7 @@ int32_t marl_linear_attention_step(const marl_attention_dims* dims, marl_view q,
                                    float* next_state, void* stream) {
   MARL_CHECK(check_dims(dims));
   const marl_attention_dims& d = *dims;
-  if (d.n_steps != 1) return MARL_E_SIZE;
+  if (d.n_steps != 1 || !launchable(step_blocks(d), 256)) return MARL_E_SIZE;
   if (d.n_seqs == 0) return MARL_OK;
   for (const marl_view& x : {q, k, v, out}) MARL_CHECK(check_view(x, d.precision, true));
   MARL_CHECK(check_output(out, d, d.n_heads, true));
@@ -487,6 +502,7 @@ int32_t marl_linear_attention_step(const marl_attention_dims* dims, marl_view q,
   if ((reinterpret_cast<uintptr_t>(decay) & 3u) != 0) return MARL_E_ALIGN;
   MARL_REQUIRE_PTR(state); MARL_REQUIRE_PTR(next_state);
   if (next_state != state && overlapping(d, next_state, state)) return MARL_E_CONFIG;
+  MARL_CHECK(check_places(out, {q, k, v}, true));
   return (d.precision == 0 ? step<float> : step<bf16_t>)(d, q, k, v, decay, state, fresh, out, next_state, (hipStream_t)stream);
 }
 

@@ -194,16 +194,20 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs args) {
   }
 }
 
-template <class T, int E>
-int32_t rotate(RotaryArgs a, bool interleaved, hipStream_t s) {
+// The items of a head and of a token, and the workgroups for all tokens: 0 where no launch has so many
+int64_t lay_out(RotaryArgs& a, int E, bool interleaved) {
   const bool inside = interleaved && E > 1;
   a.pair_items = inside ? ((uint32_t)a.rotary + E - 1) / E : (uint32_t)a.rotary / 2 / E;
   const uint32_t items = inside ? a.dim / E : a.pair_items + (a.dim - a.rotary) / E, per_token = (a.heads[0] + a.heads[1]) * items;
+  if (a.tokens > ((int64_t)1 << 40) / per_token) return 0;  // (the product below)
   a.items = divisor(items);
   a.per_token = divisor(per_token);
-  if (a.tokens > ((int64_t)1 << 40) / per_token) return MARL_E_SIZE;  // (the product below)
   const int64_t blocks = (a.tokens * per_token + 256 * kItems - 1) / (256 * kItems);
-  if (!launchable(blocks, 256)) return MARL_E_SIZE;
+  return launchable(blocks, 256) ? blocks : 0;
+}
+
+template <class T, int E>
+int32_t rotate(const RotaryArgs& a, int64_t blocks, bool interleaved, hipStream_t s) {
   if (interleaved) hipLaunchKernelGGL((rotary_kernel<T, E, true>), dim3((unsigned)blocks), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((rotary_kernel<T, E, false>), dim3((unsigned)blocks), dim3(256), 0, s, a);
   return launch_status();
@@ -254,6 +258,9 @@ int32_t marl_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, c
     if (((pi | po) & odd) != 0) return MARL_E_ALIGN;
     if ((out[u].step == 0 && d.n_steps > 1) || (out[u].seq == 0 && d.n_seqs > 1) || (out[u].head == 0 && (u == 0 ? d.n_heads : d.n_kv_heads) > 1))
       return MARL_E_CONFIG;  // an output's elements are places of their own
+    if (out[u].data == in[u].data && ((out[u].step != in[u].step && d.n_steps > 1) || (out[u].seq != in[u].seq && d.n_seqs > 1) ||
+                                      (out[u].head != in[u].head && (u == 0 ? d.n_heads : d.n_kv_heads) > 1)))
+      return MARL_E_CONFIG;  // in place: the strides agree
     a.a[u] = {static_cast<const char*>(in[u].data), static_cast<char*>(out[u].data), in[u].step, in[u].seq, in[u].head, out[u].step, out[u].seq,
               out[u].head};
   }
@@ -274,9 +281,12 @@ int32_t marl_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, c
   a.table_wide = rotary_dim % 8 == 0;
   const int E = 16 / elem;
   const bool wide = d.dim_k % E == 0 && (interleaved || rotary_dim / 2 % E == 0);
+  const int64_t blocks = lay_out(a, wide ? E : 1, interleaved != 0);
+  if (blocks == 0) return MARL_E_SIZE;
+  if (n == 2 && (q_out.data == k_out.data || q_out.data == k.data || k_out.data == q.data)) return MARL_E_CONFIG;
   hipStream_t s = (hipStream_t)stream;
-  if (d.precision == 0) return wide ? rotate<float, 4>(a, interleaved != 0, s) : rotate<float, 1>(a, interleaved != 0, s);
-  return wide ? rotate<bf16_t, 8>(a, interleaved != 0, s) : rotate<bf16_t, 1>(a, interleaved != 0, s);
+  if (d.precision == 0) return wide ? rotate<float, 4>(a, blocks, interleaved != 0, s) : rotate<float, 1>(a, blocks, interleaved != 0, s);
+  return wide ? rotate<bf16_t, 8>(a, blocks, interleaved != 0, s) : rotate<bf16_t, 1>(a, blocks, interleaved != 0, s);
 }
 
 }  // extern "C"
