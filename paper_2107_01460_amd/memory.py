@@ -111,6 +111,9 @@ class MemoryCritic(torch.nn.Module):
         kv_heads = heads if kv_heads is None else kv_heads
         if width % heads or heads % kv_heads:
             raise B.MarlError("width is a multiple of heads, heads of kv_heads")
+        device = torch.device(device)
+        if device.type == "cuda" and device.index not in (None, torch.cuda.current_device()):
+            raise B.MarlError(f"{device} is not the current GPU, where the kernels run (torch.cuda.set_device)")
         self.heads, self.kv_heads, self.dim, self.dtype = heads, kv_heads, width // heads, dtype
         h = 4.0 * (horizon / 4.0) ** (torch.arange(heads, dtype=torch.float64) / max(heads - 1, 1))
         self.register_buffer("decay", (1 - 1 / h).float().to(device))
