@@ -111,6 +111,8 @@ class MemoryCritic(torch.nn.Module):
         kv_heads = heads if kv_heads is None else kv_heads
         if width % heads or heads % kv_heads:
             raise B.MarlError("width is a multiple of heads, heads of kv_heads")
+        if not 2 <= width // heads <= 128:
+            raise B.MarlError(f"heads of {width // heads}: 2 to 128")
         device = torch.device(device)
         if device.type == "cuda" and device.index not in (None, torch.cuda.current_device()):
             raise B.MarlError(f"{device} is not the current GPU, where the kernels run (torch.cuda.set_device)")

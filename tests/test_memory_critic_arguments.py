@@ -17,3 +17,9 @@ def test_a_device_that_is_not_the_current_one(monkeypatch):
     for device in ("cuda:1", torch.device("cuda", 3)):
         with pytest.raises(StandIn.MarlError, match="current"):
             memory.MemoryCritic(8, width=16, heads=2, layers=1, device=device)
+
+
+def test_heads_wider_than_the_attention_takes():
+    with pytest.raises(StandIn.MarlError, match="128"):
+        memory.MemoryCritic(8, width=258, heads=2, layers=1, device="cpu")
+    memory.MemoryCritic(8, width=256, heads=2, layers=1, device="cpu")
