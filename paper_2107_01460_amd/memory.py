@@ -95,9 +95,10 @@ def episode_positions(done, first):
     T = done.shape[0]
     t = torch.arange(T, device=done.device, dtype=torch.int64)[:, None]
     starts = torch.zeros((T, done.shape[1]), dtype=torch.int64, device=done.device)   # the last step that began an episode, -first before any did
+    if T == 0:
+        return starts.int()
     starts[0] = -first.long()
-    if T > 1:
-        starts[1:] = torch.where(done[:-1] != 0, t[1:], starts[0])
+    starts[1:] = torch.where(done[:-1] != 0, t[1:], starts[0])
     return (t - starts.cummax(0).values).int()
 
 
