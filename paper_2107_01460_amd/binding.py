@@ -384,8 +384,8 @@ def _flags(t, lead, B, name):
     """(pointer, sequences that share a flag) of flags [environments], behind the dimensions `lead`."""
     if t is None:
         return None, 1
-    n = t.shape[-1]
-    if t.dtype not in (torch.uint8, torch.bool) or t.shape[:-1] != lead or not t.is_contiguous() or not t.is_cuda:
+    n = t.shape[-1] if t.dim() else 0
+    if t.dim() == 0 or t.dtype not in (torch.uint8, torch.bool) or t.shape[:-1] != lead or not t.is_contiguous() or not t.is_cuda:
         raise _refused(f"{name}: contiguous uint8 {list(lead)}[environments] on the GPU")
     if B == 0:
         return t.data_ptr(), 1
@@ -530,8 +530,8 @@ def rotary(q, k, table, q_out, k_out, positions=None, first_position=0, interlea
     P, R = table.shape
     at, per = None, 1
     if positions is not None:
-        n = positions.shape[-1]
-        if positions.dtype != torch.int32 or positions.shape[:-1] != (T,) or not positions.is_contiguous() or not positions.is_cuda or B and (n == 0 or B % n):
+        n = positions.shape[-1] if positions.dim() else 0
+        if positions.dim() == 0 or positions.dtype != torch.int32 or positions.shape[:-1] != (T,) or not positions.is_contiguous() or not positions.is_cuda or B and (n == 0 or B % n):
             raise _refused(f"positions: contiguous int32 [{T}][environments] of {B} sequences, on the GPU")
         at, per = positions.data_ptr(), B // n if B else 1
     none = View()

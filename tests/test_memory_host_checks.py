@@ -63,3 +63,11 @@ def test_in_place_with_other_strides(M):  # noqa: F811
     q, k, qo, ko = V(GOOD, 64, 32, 16), V(GOOD + 4096, 64, 32, 16), V(OUT, 64, 32, 16), V(OUT + 4096, 64, 32, 16)
     for outs in ((V(GOOD, 128, 32, 16), ko), (qo, V(GOOD + 4096, 64, 48, 16)), (k, ko), (qo, q), (qo, qo)):
         assert L.marl_rotary(C.byref(d), q, k, GOOD, 8, 8, None, 0, 0, 0, *outs, None) == CONFIG
+
+
+def test_numbers_in_place_of_arrays(M):  # noqa: F811
+    """Flags and positions without a dimension are refused like any other wrong shape."""
+    with pytest.raises(M.MarlError, match="done"):
+        M.binding._flags(torch.tensor(1, dtype=torch.uint8), (4,), 6, "done")
+    with pytest.raises(M.MarlError, match="positions"):
+        M.rotary(torch.zeros(4, 6, 2, 8), None, torch.zeros(9, 8), torch.zeros(4, 6, 2, 8), None, positions=torch.tensor(3, dtype=torch.int32))
