@@ -89,18 +89,21 @@ __device__ __forceinline__ double ipow(float base, int m) {  // base^m, 0^0 = 1
 }
 
 // ---- products of 16 x 16 outputs; the contraction index of element e of lane group g is the same on both sides -----------------------
+// bf16: one instruction, of 32 along the contraction, half of it zeros where there is one tile.  It takes no longer than the one of 16, and the two must not meet: a
+// product that adds to the result of one of the other length, a few instructions behind it, gets half of that result or none of it, and the compiler puts no wait
+// between them (back to back, half of all values were wrong; of one length, none).
 __device__ __forceinline__ floatx4 mma(floatx4 a, floatx4 b, floatx4 c) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
   return c;
 }
-__device__ __forceinline__ floatx4 mma(shortx4 a, shortx4 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ shortx8 both(shortx4 a, shortx4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 // over two tiles' contraction: one instruction of twice the length in bf16
 __device__ __forceinline__ floatx4 mma2(floatx4 a0, floatx4 a1, floatx4 b0, floatx4 b1, floatx4 c) { return mma(a1, b1, mma(a0, b0, c)); }
 __device__ __forceinline__ floatx4 mma2(shortx4 a0, shortx4 a1, shortx4 b0, shortx4 b1, floatx4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, both(a0, a1)), __builtin_bit_cast(bf16x8, both(b0, b1)), c, 0, 0, 0);
 }
+__device__ __forceinline__ floatx4 mma(shortx4 a, shortx4 b, floatx4 c) { return mma2(a, shortx4{}, b, shortx4{}, c); }
 
 __device__ __forceinline__ shortx4 pack4(floatx4 v) {
   const uint2 u = make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]));
@@ -579,8 +582,8 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 4 || (NK == 
           for (int c = 0; c < NV; ++c)
 #pragma unroll
             for (int p = kParts - 1; p >= 0; --p) {
-              if (u == 0) o[u][c] = mma(zt[0][c], w[0].p[p], o[u][c]);
-              else if constexpr (U > 1) o[u][c] = mma2(zt[0][c], zt[1][c], w[0].p[p], w[1].p[p], o[u][c]);
+              if constexpr (U == 1) o[u][c] = mma(zt[0][c], w[0].p[p], o[u][c]);
+              else o[u][c] = mma2(zt[0][c], zt[1][c], w[0].p[p], u == 0 ? Frag{} : w[1].p[p], o[u][c]);
             }
 #pragma unroll
           for (int c = 0; c < NV; ++c) sum += (o[u][c][0] + o[u][c][1]) + (o[u][c][2] + o[u][c][3]);
