@@ -49,16 +49,16 @@ struct ScanArgs {
   ScanRole role[kMaxRoles];
   const float* decay;
   const uint8_t* done;
-  float* carry;          // states only: [sequence, head][stretch] factor from a stretch's first state to its last, or one of the two below
+  float* carry;          // states only: [sequence, head][stretch] factor from a stretch's first state to its last, or kCarryEnded
   int32_t T, B;
   uint32_t n_roles, H, seqs_per_flag, n_stretches;
   int32_t stretch;       // steps of a stretch, whole tiles
   uint32_t pairs;        // B * H
 };
 
-// A carry that is no factor (a decay is none below 0): an episode ended in the stretch, so that nothing of what came in is left; the power of a decay above 0
-// is one that 32 bits do not hold, so that of what came in only an infinity or a NaN is left, as step by step.
-constexpr float kCarryEnded = -2.f, kCarryVanished = -3.f;
+// A carry that is no factor (a decay is none below 0): an episode ended in the stretch, so that nothing of what came in is left.  A power of a decay above 0 that
+// 32 bits do not hold is rounded up to the least number that they do, not down to 0: an infinity that came in stays one, as step by step.
+constexpr float kCarryEnded = -2.f, kCarryLeast = 0x1p-149f;
 
 template <class T>
 struct ScanTraits;
@@ -736,7 +736,7 @@ __global__ void __launch_bounds__(64 * SL * scan_pairs<SL>(), NK >= 4 || (NK == 
   }
   if (STATE_ONLY && role_index == 0 && slice0 == 0 && lane == 0) {
     const float factor = (float)ipow(decay, t_end - t_begin);
-    args.carry[pair * args.n_stretches + stretch] = any_end ? kCarryEnded : factor == 0.f && decay != 0.f ? kCarryVanished : factor;
+    args.carry[pair * args.n_stretches + stretch] = any_end ? kCarryEnded : factor == 0.f && decay != 0.f ? kCarryLeast : factor;
   }
 }
 

@@ -87,8 +87,7 @@ __global__ void __launch_bounds__(256) join_kernel(JoinArgs a0, JoinArgs a1, uin
       if (p0 + u >= a.n) break;
       const int p = a.reverse ? a.n - 1 - (p0 + u) : p0 + u;
       a.states[(pair * a.n + p) * size + e] = run;
-      const float left = c[u] == kCarryEnded ? 0.f : c[u] != kCarryVanished ? c[u] * run : fabsf(run) < __builtin_inff() ? 0.f : run;
-      run = left + v[u];
+      run = c[u] == kCarryEnded ? v[u] : c[u] * run + v[u];
     }
   }
   if (a.last != nullptr) a.last[at] = run;
