@@ -40,17 +40,17 @@ def same_places(M, s):
 @pytest.mark.parametrize("decay", [0.0, 0.1, 0.75, 0.99])
 @pytest.mark.parametrize("bad,at", [(NAN, 10), (INF, 10), (-INF, 300), (NAN, 300), (NAN, 511)])
 def test_in_a_sequence_that_is_cut(M, bad, at, decay, dtype):
-    for name in ("k", "q", "v", "dout"):
-        for ends in ((), (400,), (5, 64, 383)):
-            s = make(512, 2, 2, 1, 32, 16, dtype, seed=at)
-            s["decay"] = torch.tensor([decay, 0.9], device="cuda")
-            s["done"] = torch.zeros((512, 2), dtype=torch.uint8, device="cuda")
-            for t in ends:
-                s["done"][t, 0] = 1
-            assert M.linear_attention_workspace(s["q"], s["k"], s["v"]) > 0
-            s[name][at, 0, 0, 7] = bad
-            print("case", name, ends, bad, at, decay, dtype, flush=True)
-            same_places(M, s)
+    """In k, q, v and dout in turn, without an end, with one behind it and with several: twelve pairs of sequences, the first of each pair with the bad value and the ends."""
+    kinds = [(name, ends) for name in ("k", "q", "v", "dout") for ends in ((), (400,), (5, 64, 383))]
+    s = make(512, 2 * len(kinds), 2, 1, 32, 16, dtype, seed=at)
+    s["decay"] = torch.tensor([decay, 0.9], device="cuda")
+    s["done"] = torch.zeros((512, 2 * len(kinds)), dtype=torch.uint8, device="cuda")
+    for i, (name, ends) in enumerate(kinds):
+        for t in ends:
+            s["done"][t, 2 * i] = 1
+        s[name][at, 2 * i, 0, 7] = bad
+    assert M.linear_attention_workspace(s["q"], s["k"], s["v"]) > 0
+    same_places(M, s)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
