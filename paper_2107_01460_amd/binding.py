@@ -356,9 +356,13 @@ def _floats(t, shape, name):
     return t.data_ptr()
 
 
+# Tells autograd that tensors have changed, so that a backward pass that kept their old values raises (0.2 us without the public name's wrapper, 0.5 with it).
+_raise_versions = getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)
+
+
 def _written(*outputs):
-    """Tells autograd that these (None: absent) have changed, so that a backward pass that kept their old values raises."""
-    torch.autograd.graph.increment_version([t for t in outputs if t is not None])
+    """Of outputs that may be None: absent."""
+    _raise_versions([t for t in outputs if t is not None])
 
 
 def _view(t, shape, dtype, name):
@@ -431,7 +435,7 @@ def linear_attention(q, k, v, decay, out, workspace=None, state=None, next_state
                                    _view(v, (T, B, Hk, Dv), dt, "v"), _floats(decay, (H,), "decay"), _floats(state, states, "state"), flags,
                                    _view(out, (T, B, H, Dv), dt, "out"), _floats(next_state, states, "next_state"),
                                    _workspace(workspace, need.value), _stream(stream)))
-    _written(out, next_state)
+    _raise_versions((out,) if next_state is None else (out, next_state))
 
 
 def linear_attention_backward(q, k, v, decay, dout, dq, dk, dv, workspace=None, state=None, dnext_state=None, dstate=None, done=None, scale=1.0,
@@ -463,7 +467,7 @@ def linear_attention_step(q, k, v, decay, state, out, next_state=None, done=None
         C.byref(dims), _step_view(q, (B, H, Dk), dt, "q"), _step_view(k, (B, Hk, Dk), dt, "k"), _step_view(v, (B, Hk, Dv), dt, "v"),
         _floats(decay, (H,), "decay"), before, flags, _step_view(out, (B, H, Dv), dt, "out"),
         before if next_state is None else _floats(next_state, states, "next_state"), _stream(stream)))
-    _written(out, state if next_state is None else next_state)
+    _raise_versions((out, state if next_state is None else next_state))
 
 
 def _rows(t, shape, dtype, name):
@@ -539,7 +543,7 @@ def rotary(q, k, table, q_out, k_out, positions=None, first_position=0, interlea
         C.byref(AttentionDims.from_buffer_copy(_DIMS.pack(precision, T, B, H, Hk, D, D, per, 1.0))), _view(q, qs, dt, "q"),
         none if k is None else _view(k, ks, dt, "k"), _floats(table, (P, R), "table"), P, R, at, first_position, interleaved, inverse,
         _view(q_out, qs, dt, "q_out"), none if k is None else _view(k_out, ks, dt, "k_out"), _stream(stream)))
-    _written(q_out, k_out)
+    _raise_versions((q_out,) if k_out is None else (q_out, k_out))
 
 
 KERNEL_CLASSES = {"gemm_nn": 0, "gemm_nt": 1, "gemm_tn": 2, "env_step": 3, "gae": 4, "fused_train": 5, "rollout": 6}
