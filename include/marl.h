@@ -334,7 +334,8 @@ typedef struct marl_attention_dims {
  * otherwise 1: a nonzero done_t says that step t ended an episode, as in marl_traj, so packed sequences of different lengths are
  * one sequence with flags.  next_state (nullable; may be `state`, MARL_E_CONFIG where it overlaps it otherwise) is zero where the last step ended an episode.  T = 0: next_state = state.
  * A step's output depends on the steps of its own episode up to it only, infinities and NaNs included.
- * bf16: products have bf16 operands where these are exact or split into parts, sums and the state are fp32; outputs are rounded once.
+ * bf16: products have bf16 operands, which are exact or a sum of parts: scores and the state, where an output comes of them, two parts (2^-16 of each term), what enters
+ * the state three (2^-24); sums and the state are fp32; outputs are rounded once.
  * workspace: marl_linear_attention_workspace bytes.  Errors: MARL_E_NULL, MARL_E_ALIGN, MARL_E_CONFIG, MARL_E_LAUNCH; MARL_E_SIZE for n_seqs * n_heads
  * above 2^26 or so many that a launch would have 2^32 work-items: 64 a sequence and head for each 32 columns or part of them (32 to 64: 128, 65 to
  * 96: 192, more: 256), of dim_v, in the gradient 3 times (dim_k = dim_v), otherwise twice those of dim_k and once those of dim_v; the workspace's query

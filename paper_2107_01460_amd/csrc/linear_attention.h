@@ -14,9 +14,11 @@
 // memory, and steps are far apart in it (megabytes, when there are many sequences), so its wavefronts fetch and store whole runs together and hand
 // them to each other through LDS; the next tile is on its way in registers meanwhile.
 //
-// Measured (MI355X): output of 128 x 4096 steps of 8 heads of 64 in bf16 with states 698 us, 4.6 TB/s, 94 % of a copy's rate, bound by memory (a wavefront a
-// head with its own loads: 1070); gradient of 128 x 4096 steps of 4 heads of 32 in fp32 597 us, 3.5 TB/s, fp32 matrix cores busy 44 %; 32 768 steps of one
-// sequence with 8 heads of 128 in bf16 82 us for the scan, bound by the issue of vector instructions (about 700 a tile beside 100 matrix ones).
+// Measured (MI355X): output of 128 x 4096 steps of 8 heads of 64 in bf16 with states 697 us, 4.6 TB/s, 94 % of a copy's rate, bound by memory (a wavefront a
+// head with its own loads: 1070); gradient of 128 x 4096 steps of 4 heads of 32 in fp32 599 us, 1.84 GB read and 0.87 written beyond the L2, 4.5 TB/s, where every
+// array once is 1.2 and 0.87 (dk and dv share their arrays in the L2, dq, which walks the other way, reads its own again); 32 768 steps of one sequence with 8 query
+// heads of 128 on 2 in bf16 81 us for the scan, 0.30 GB beyond the L2, 3.7 TB/s (each query head reads the shared keys and values anew: every array once is 0.20),
+// vector ALUs busy 50 %, matrix cores 27 %: none of them full, two wavefronts a SIMD.
 #pragma once
 #include "split_bf16.h"
 
@@ -113,8 +115,9 @@ __device__ __forceinline__ floatx4 unpack4(shortx4 s) {
   const uint2 u = __builtin_bit_cast(uint2, s);
   return floatx4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u)};
 }
-// fp32 values as operands beside exact ones.  bf16: as a sum of two parts (relative error 2^-16: scores and S, where the result is an output of
-// eight bits) or of three (2^-24: what enters a state that goes on).
+// fp32 values as operands beside exact ones.  bf16: as a sum of two parts (relative error 2^-16 of a term: scores and S, where the result is an output of eight bits
+// or a share of one) or of three (2^-24: what enters a state that goes on).  Three for the outputs too: 3e-5 instead of 1e-4 of them rounded to another neighbour (the
+// error against 64 bits, that of rounding, is 0.0017 either way), at 728 us instead of 697 for the rollout of the header, 146 instead of 130 for 32 768 steps.
 template <class T, int P>
 struct Parts {
   typename ScanTraits<T>::Frag p[sizeof(T) == 4 ? 1 : P];
@@ -368,9 +371,13 @@ __device__ __forceinline__ void each_state_element(float* s, int row, int col, i
   }
 }
 
-// Wavefronts a SIMD that the registers are dealt out for: three up to 48 features, two above, because a spilled register costs more than a wavefront: its
-// reload waits for every load and store on its way (64 features, rollout of the header: three with 7 registers spilled 732 us, two with none 698; 128 features,
-// 32 768 steps: three with 100 spilled 355, two 126).
+// Wavefronts a SIMD that the registers are dealt out for: three up to 48 features (48 with one slice: two), two above, because a spilled register costs more than a
+// wavefront: its reload waits for every load and store on its way (64 features, rollout of the header: three with 7 registers spilled 732 us, two with none 698;
+// 128 features, 32 768 steps: three with 100 spilled 355, two 126).
+// Of the 280 instances 23 spill all the same, by the compiler's account: 48 features with two slices in bf16 7 to 9 registers; 96 features with one slice 3 to 4 in fp32,
+// 19 to 25 in bf16; 128 features with fewer than four slices 1 to 27 in fp32 (with four 1 to 2), 4 to 22 in bf16, where the output with one slice and rows that are no whole
+// pieces keeps 1 KB of its staged pieces in scratch and runs one wavefront a SIMD.  (The pairs of a workgroup go by its slices alone: four pairs of 128 features
+// are eight pieces a thread of x and of y each.)
 // Slices of 32 columns: of 48 they spilled as much, and halved the wavefronts (gradient with heads of 40 and 72: 466 -> 890 us).
 template <int SL>
 constexpr int scan_pairs() { return SL == 1 ? 4 : SL == 2 ? 2 : 1; }  // (sequence, head) pairs of a workgroup

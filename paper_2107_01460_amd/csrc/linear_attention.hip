@@ -20,8 +20,9 @@ struct Plan {
 
 // A call with few sequences is cut over time into stretches: their own states first, joined along time, then every stretch with the state that
 // comes in.  The states cost a second reading of k and v and half the matrix products again, so only while there are fewer wavefronts than
-// the chip holds: 8 for each of the 256 compute units.  (32 768 steps of 8 heads of 128, with a state: 147 us; aiming at 1024, 1536 or 4096 wavefronts 183, 171, 174.
-// Gradient of 8192 steps of 8 heads of 64: 59; 68, 60, 55.)  No stretch is shorter than 64 steps.
+// the chip holds: 8 for each of the 256 compute units.  (32 768 steps of 8 query heads of 128, with a state, when this was chosen: 147 us; aiming at 1024, 1536 or
+// 4096 wavefronts 183, 171, 174.  Gradient of 8192 steps of 8 heads of 64: 59; 68, 60, 55.  Now 151 and 57.)  A gradient counts three times the slices of dim_v, its
+// wavefronts where the widths agree; where they do not, it launches twice those of dim_k, then once those of dim_v.  No stretch is shorter than 64 steps.
 Plan plan_of(const marl_attention_dims& d, bool backward) {
   constexpr int64_t kWaves = 2048;
   Plan p{};
