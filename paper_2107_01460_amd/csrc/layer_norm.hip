@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(TEAM > kThreads ? TEAM : kThreads)
   }
 }
 
-// The gradient: a workgroup keeps its shares of the two column sums in registers over its rows: its teams' are added
+// The gradient (rows of more than 4096 values with column sums spill 5 to 9 registers): a workgroup keeps its shares of the two column sums in registers over its rows: its teams' are added
 // through LDS at the end and written out, [workgroup][2][width], for column_sum_kernel.
 template <class T, int E, int TEAM, int N, bool WEIGHTS>
 __global__ void __launch_bounds__(TEAM > kThreads ? TEAM : kThreads)
