@@ -401,6 +401,64 @@ int32_t marl_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, c
                     int32_t rotary_dim, const int32_t* positions, int32_t first_position, int32_t interleaved,
                     int32_t inverse, marl_view q_out, marl_view k_out, void* stream);
 
+/* Norm of each head of q [T][B][n_heads][dim] and, with the same positions, k [T][B][n_kv_heads][dim] (k.data NULL: q alone), then the rotation of marl_rotary, in
+ * one pass: u = x * rstd * weight, rstd = 1 / sqrt(mean(x^2) + eps) over a head's dim (1..256) elements, weight [dim] for all heads of q, of k (fp32; NULL: 1); the
+ * first rotary_dim elements of u are rotated, the others copied.  positions and first_position as in marl_rotary, but a row whose position is negative holds no
+ * step: zeros.  A position behind the table gives NaNs in the rotated elements.  An output may be its input, with the same strides.  The values between norm and
+ * rotation are not rounded.  dims: precision, n_steps, n_seqs, n_heads, n_kv_heads, dim_k, seqs_per_flag are read. */
+int32_t marl_norm_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, const float* q_weight, const float* k_weight, float eps,
+                         const float* table, int32_t n_positions, int32_t rotary_dim, const int32_t* positions, int32_t first_position,
+                         int32_t interleaved, marl_view q_out, marl_view k_out, void* stream);
+
+/* Its gradient: dq, dk from the gradients dq_out, dk_out of its outputs, and the sums over all rows dq_weight, dk_weight [dim] (fp32, nullable, added in an order that
+ * depends on the sizes only).  Rows that hold no step: zeros, and nothing of theirs enters the sums.  dq may be dq_out or q with the same strides, dk likewise.  workspace:
+ * marl_norm_rotary_workspace bytes, where a sum is asked for. */
+int32_t marl_norm_rotary_backward(const marl_attention_dims* dims, marl_view dq_out, marl_view dk_out, marl_view q, marl_view k, const float* q_weight,
+                                  const float* k_weight, float eps, const float* table, int32_t n_positions, int32_t rotary_dim,
+                                  const int32_t* positions, int32_t first_position, int32_t interleaved, marl_view dq, marl_view dk,
+                                  float* dq_weight, float* dk_weight, void* workspace, void* stream);
+int32_t marl_norm_rotary_workspace(const marl_attention_dims* dims, int64_t* bytes);
+
+/* The cache of window attention: keys [B][n_kv_heads][sinks + window][dim_k] and values [B][n_kv_heads][sinks + window][dim_v], elements of `precision`, 16-byte
+ * aligned; both NULL: none.  It holds the last steps of the episode that is going on in each sequence: its step e (0 the first) in slot e if e < sinks, otherwise in
+ * slot sinks + (e - sinks) % window, the newest of a slot.  How many steps it holds is told by positions, not kept: it needs no clearing at an episode's end, and what
+ * lies in other slots is never used. */
+typedef struct marl_window_cache {
+  void *keys, *values;
+} marl_window_cache;
+
+/* Attention over the last `window` (1 or more) steps of an episode, the present one among them, and its first `sinks` (0 or more; together at most 2^30).
+ * positions [T][B / seqs_per_flag] int32: the step in its episode of each row; negative: the row holds no step (recordings of unequal length side by side).  NULL:
+ * first_position + t.  With p_i the position of row i, per sequence and query head: row i sees the steps j of its episode, i - p_i <= j <= i, with i - j < window or
+ * j - (i - p_i) < sinks;
+ *   s_ij = scale q_i . k_j,   lse_i = log(sum_j exp(s_ij)),   out_i = sum_j exp(s_ij - lse_i) v_j.
+ * A row alone decides what it sees, so positions need not count up.  Steps before row 0 (j < 0) come from `cache`, which holds the p_0 steps before it; without a
+ * cache they are not seen.  A row that holds no step: out 0, lse -infinity.  What a row does not see does not enter its output, infinities and NaNs included.
+ * lse [B][n_heads][T] fp32 (nullable): kept for the gradient.  next_cache (nullable; may be `cache`, MARL_E_CONFIG where it overlaps it otherwise): the cache behind the
+ * last row that holds a step; its slots that hold no step, and where there is no cache those of steps before row 0, are left as they were.  A sequence without a step:
+ * the cache itself.
+ * bf16: scores and statistics are fp32 sums of exact products; the weights, and in the gradient what multiplies keys and queries, are rounded to bf16 once (2^-9 of each
+ * term); outputs are rounded once.  workspace: marl_window_attention_workspace bytes.  Errors as in marl_linear_attention; MARL_E_CONFIG for window or sinks
+ * out of range. */
+int32_t marl_window_attention(const marl_attention_dims* dims, int32_t window, int32_t sinks, marl_view q, marl_view k, marl_view v,
+                              const int32_t* positions, int32_t first_position, marl_window_cache cache, marl_view out, float* lse,
+                              marl_window_cache next_cache, void* workspace, void* stream);
+
+/* Its gradient: dq, dk, dv from dout, and the call's own out and lse.  Steps of the cache are constants.  dk and dv of a head that query heads share are sums over
+ * these, in a fixed order.  Rows that hold no step: zeros.  The outputs begin nowhere where another array does. */
+int32_t marl_window_attention_backward(const marl_attention_dims* dims, int32_t window, int32_t sinks, marl_view q, marl_view k, marl_view v,
+                                       const int32_t* positions, int32_t first_position, marl_window_cache cache, marl_view out,
+                                       const float* lse, marl_view dout, marl_view dq, marl_view dk, marl_view dv, void* workspace,
+                                       void* stream);
+
+/* One step, for acting (n_steps = 1; the views' step strides are not used): k and v are put into the cache's slot of positions [B / seqs_per_flag], then q attends to
+ * the steps that the cache holds, which are those that it sees.  A negative position: out 0, the cache as it was. */
+int32_t marl_window_attention_step(const marl_attention_dims* dims, int32_t window, int32_t sinks, marl_view q, marl_view k, marl_view v,
+                                   const int32_t* positions, marl_window_cache cache, marl_view out, void* workspace, void* stream);
+
+/* Workspace of marl_window_attention (call = 0), its gradient (1) or a step (2) in bytes, into *bytes.  Touches no GPU. */
+int32_t marl_window_attention_workspace(const marl_attention_dims* dims, int32_t window, int32_t sinks, int32_t call, int64_t* bytes);
+
 /* Human-readable name of a status code (static storage, host).  Part of the error convention of this boundary,
  * not of the paper's method. */
 const char* marl_status_string(int32_t status);

@@ -9,7 +9,8 @@ from .binding import (  # noqa: F401
     policy_forward, sample_actions, rollout, rollout_static, compute_gae, ppo_update, status_string, alloc_workspace,
     timing_enable, timing_read, KERNEL_CLASSES, EvalStats, evaluate, RecState, rollout_recurrent, ppo_update_recurrent, train_step, alloc_counters,
     linear_attention, linear_attention_backward, linear_attention_step, linear_attention_workspace, layer_norm, layer_norm_backward,
-    layer_norm_workspace, rotary, rotary_table,
+    layer_norm_workspace, rotary, rotary_table, norm_rotary, norm_rotary_backward, norm_rotary_workspace, window_attention, window_attention_backward,
+    window_attention_step, window_attention_workspace,
 )
 from .trainer import Trainer  # noqa: F401,E402
 from .memory import MemoryCritic, episode_positions  # noqa: F401,E402

@@ -62,6 +62,10 @@ class View(C.Structure):
     _fields_ = [("data", C.c_void_p), ("step", C.c_int64), ("seq", C.c_int64), ("head", C.c_int64)]
 
 
+class WindowCache(C.Structure):
+    _fields_ = [("keys", C.c_void_p), ("values", C.c_void_p)]
+
+
 class RotaryDims(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_positions", "rotary_dim", "scaling")] + [
         (n, C.c_float) for n in ("base", "factor", "trained_length", "slow", "fast", "amplitude")]
@@ -71,6 +75,8 @@ EXPORTS = ("marl_query_sizes", "marl_env_reset", "marl_observe", "marl_env_step"
            "marl_sample_actions", "marl_rollout", "marl_rollout_static", "marl_compute_gae", "marl_ppo_update", "marl_train_step", "marl_evaluate", "marl_rollout_recurrent", "marl_ppo_update_recurrent",
            "marl_linear_attention", "marl_linear_attention_backward", "marl_linear_attention_step", "marl_linear_attention_workspace",
            "marl_layer_norm", "marl_layer_norm_backward", "marl_layer_norm_workspace", "marl_rotary_table", "marl_rotary",
+           "marl_norm_rotary", "marl_norm_rotary_backward", "marl_norm_rotary_workspace", "marl_window_attention", "marl_window_attention_backward",
+           "marl_window_attention_step", "marl_window_attention_workspace",
            "marl_timing_enable",
            "marl_timing_read", "marl_status_string")
 
@@ -110,6 +116,13 @@ def lib():
         L.marl_layer_norm_workspace.argtypes = [i64, i32, C.POINTER(i64)]
         L.marl_rotary_table.argtypes = [C.POINTER(RotaryDims), vp, vp]
         L.marl_rotary.argtypes = [ap, View, View, vp, i32, i32, vp, i32, i32, i32, View, View, vp]
+        L.marl_norm_rotary.argtypes = [ap, View, View, vp, vp, C.c_float, vp, i32, i32, vp, i32, i32, View, View, vp]
+        L.marl_norm_rotary_backward.argtypes = [ap, View, View, View, View, vp, vp, C.c_float, vp, i32, i32, vp, i32, i32, View, View, vp, vp, vp, vp]
+        L.marl_norm_rotary_workspace.argtypes = [ap, C.POINTER(i64)]
+        L.marl_window_attention.argtypes = [ap, i32, i32, View, View, View, vp, i32, WindowCache, View, vp, WindowCache, vp, vp]
+        L.marl_window_attention_backward.argtypes = [ap, i32, i32, View, View, View, vp, i32, WindowCache, View, vp, View, View, View, View, vp, vp]
+        L.marl_window_attention_step.argtypes = [ap, i32, i32, View, View, View, vp, WindowCache, View, vp, vp]
+        L.marl_window_attention_workspace.argtypes = [ap, i32, i32, i32, C.POINTER(i64)]
         L.marl_timing_enable.argtypes = [C.c_int32]
         L.marl_timing_read.argtypes = [C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_int64), C.POINTER(C.c_double)]
         L.marl_status_string.argtypes = [C.c_int32]
@@ -544,6 +557,148 @@ def rotary(q, k, table, q_out, k_out, positions=None, first_position=0, interlea
         none if k is None else _view(k, ks, dt, "k"), _floats(table, (P, R), "table"), P, R, at, first_position, interleaved, inverse,
         _view(q_out, qs, dt, "q_out"), none if k is None else _view(k_out, ks, dt, "k_out"), _stream(stream)))
     _raise_versions((q_out,) if k_out is None else (q_out, k_out))
+
+
+def _positions(t, lead, B):
+    """(pointer, sequences that share a position) of positions [environments], behind the dimensions `lead`."""
+    if t is None:
+        return None, 1
+    n = t.shape[-1] if t.dim() else 0
+    if t.dim() == 0 or t.dtype != torch.int32 or t.shape[:-1] != lead or not t.is_contiguous() or not t.is_cuda or B and (n == 0 or B % n):
+        raise _refused(f"positions: contiguous int32 {list(lead)}[environments] of {B} sequences, on the GPU")
+    return t.data_ptr(), B // n if B else 1
+
+
+def _norm_dims(q, k, table, positions):
+    """(dims, shapes of q and of k, table rows, rotated elements, positions' pointer) of arrays [T][B][heads][D]; k may be None"""
+    precision = _PRECISION.get(q.dtype)
+    if precision is None or q.dim() != 4 or k is not None and k.dim() != 4:
+        raise _refused("q, k: float32 or bfloat16 [T][B][heads][D]")
+    T, B, H, D = q.shape
+    Hk = 1 if k is None else k.shape[2]
+    if table.dim() != 2:
+        raise _refused("table: [positions][rotary_dim]")
+    at, per = _positions(positions, (T,), B)
+    return AttentionDims.from_buffer_copy(_DIMS.pack(precision, T, B, H, Hk, D, D, per, 1.0)), (T, B, H, D), (T, B, Hk, D), *table.shape, at
+
+
+def norm_rotary(q, k, q_weight, k_weight, table, q_out, k_out, eps=1e-6, positions=None, first_position=0, interleaved=False, stream=None):
+    """Every head of q and k divided by the root of its mean square and weighted, then rotated as by rotary(); weights (and k, k_out) may be None.  Rows of
+    negative positions: zeros.  The outputs may be the inputs."""
+    dims, qs, ks, P, R, at = _norm_dims(q, k, table, positions)
+    dt, D, none = q.dtype, q.shape[3], View()
+    _check(lib().marl_norm_rotary(
+        C.byref(dims), _view(q, qs, dt, "q"), none if k is None else _view(k, ks, dt, "k"), _floats(q_weight, (D,), "q_weight"),
+        _floats(k_weight, (D,), "k_weight"), eps, _floats(table, (P, R), "table"), P, R, at, first_position, interleaved, _view(q_out, qs, dt, "q_out"),
+        none if k is None else _view(k_out, ks, dt, "k_out"), _stream(stream)))
+    _raise_versions((q_out,) if k is None else (q_out, k_out))
+
+
+def norm_rotary_workspace(q, k):
+    """Bytes of workspace that the gradient of norm_rotary needs for arrays of these shapes."""
+    if q.dtype not in _PRECISION or q.dim() != 4 or k is not None and k.dim() != 4:
+        raise _refused("q, k: float32 or bfloat16 [T][B][heads][D]")
+    n, (T, B, H, D) = C.c_int64(), q.shape
+    Hk = 1 if k is None else k.shape[2]
+    _check(lib().marl_norm_rotary_workspace(C.byref(AttentionDims(_PRECISION[q.dtype], T, B, H, Hk, D, D, 1, 1.0)), C.byref(n)))
+    return n.value
+
+
+def norm_rotary_backward(dq_out, dk_out, q, k, q_weight, k_weight, table, dq, dk, dq_weight=None, dk_weight=None, workspace=None, eps=1e-6, positions=None,
+                         first_position=0, interleaved=False, stream=None):
+    """dq, dk and the weights' gradients dq_weight, dk_weight (may be None) of norm_rotary from those of its outputs."""
+    dims, qs, ks, P, R, at = _norm_dims(q, k, table, positions)
+    dt, D, none, need, L = q.dtype, q.shape[3], View(), C.c_int64(), lib()
+    if dq_weight is not None or dk_weight is not None:
+        _check(L.marl_norm_rotary_workspace(C.byref(dims), C.byref(need)))
+    _check(L.marl_norm_rotary_backward(
+        C.byref(dims), _view(dq_out, qs, dt, "dq_out"), none if k is None else _view(dk_out, ks, dt, "dk_out"), _view(q, qs, dt, "q"),
+        none if k is None else _view(k, ks, dt, "k"), _floats(q_weight, (D,), "q_weight"), _floats(k_weight, (D,), "k_weight"), eps,
+        _floats(table, (P, R), "table"), P, R, at, first_position, interleaved, _view(dq, qs, dt, "dq"), none if k is None else _view(dk, ks, dt, "dk"),
+        _floats(dq_weight, (D,), "dq_weight"), None if k is None else _floats(dk_weight, (D,), "dk_weight"), _workspace(workspace, need.value), _stream(stream)))
+    _written(dq, dq_weight, *((dk, dk_weight) if k is not None else ()))
+
+
+WINDOW_CALLS = {"forward": 0, "backward": 1, "step": 2}
+_CACHE = struct.Struct("=2Q")
+assert _CACHE.size == C.sizeof(WindowCache)
+_NO_CACHE = WindowCache()
+
+
+def _cache(cache, shape, dk, dv, dtype, name):
+    """Of (keys [B][Hk][slots][Dk], values [B][Hk][slots][Dv]), or None"""
+    if cache is None:
+        return _NO_CACHE
+    keys, values = cache
+    if keys.dtype != dtype or values.dtype != dtype or keys.shape != (*shape, dk) or values.shape != (*shape, dv) or not (
+            keys.is_contiguous() and values.is_contiguous() and keys.is_cuda and values.is_cuda):
+        raise _refused(f"{name}: contiguous {dtype} {[*shape, dk]} and {[*shape, dv]} on the GPU")
+    return WindowCache.from_buffer_copy(_CACHE.pack(keys.data_ptr(), values.data_ptr()))
+
+
+def _window_dims(q, k, v, positions, scale):
+    """(dims, T, B, H, Hk, Dk, Dv, positions' pointer) of arrays [T][B][heads][D]"""
+    precision = _PRECISION.get(q.dtype)
+    if precision is None or q.dim() != 4 or v.dim() != 4 or k.dim() != 4:
+        raise _refused("q, k, v: float32 or bfloat16 [T][B][heads][D]")
+    T, B, H, Dk = q.shape
+    _, _, Hk, Dv = v.shape
+    at, per = _positions(positions, (T,), B)
+    return AttentionDims.from_buffer_copy(_DIMS.pack(precision, T, B, H, Hk, Dk, Dv, per, scale)), T, B, H, Hk, Dk, Dv, at
+
+
+def window_attention_workspace(q, k, v, window, sinks=0, kind="forward"):
+    """Bytes of workspace that window_attention ("forward"), its gradient ("backward") or a step ("step") needs for arrays of these shapes, [T][B][heads][D]
+    (of a step [B][heads][D] or [1][B][heads][D])."""
+    if kind == "step" and q.dim() == 3:
+        q, k, v = q[None], k[None], v[None]
+    n = C.c_int64()
+    _check(lib().marl_window_attention_workspace(C.byref(_window_dims(q, k, v, None, 1.0)[0]), window, sinks, WINDOW_CALLS[kind], C.byref(n)))
+    return n.value
+
+
+def window_attention(q, k, v, out, window, sinks=0, lse=None, positions=None, first_position=0, cache=None, next_cache=None, scale=1.0, workspace=None,
+                     stream=None):
+    """out [T][B][Hq][Dv] (and lse [B][Hq][T]) of attention over the last `window` steps of an episode and its first `sinks`; positions [T][environments]: each
+    row's step in its episode, negative for none.  cache, next_cache: (keys, values) before and behind the call, [B][Hk][sinks + window][D]."""
+    dims, T, B, H, Hk, Dk, Dv, at = _window_dims(q, k, v, positions, scale)
+    dt, shape = q.dtype, (B, Hk, sinks + window)
+    before = _cache(cache, shape, Dk, Dv, dt, "cache")
+    _check(lib().marl_window_attention(
+        C.byref(dims), window, sinks, _view(q, (T, B, H, Dk), dt, "q"), _view(k, (T, B, Hk, Dk), dt, "k"), _view(v, (T, B, Hk, Dv), dt, "v"), at,
+        first_position, before, _view(out, (T, B, H, Dv), dt, "out"), _floats(lse, (B, H, T), "lse"),
+        before if next_cache is cache else _cache(next_cache, shape, Dk, Dv, dt, "next_cache"), _workspace(workspace, 0), _stream(stream)))
+    _written(out, lse, *(next_cache or ()))
+
+
+def window_attention_backward(q, k, v, out, lse, dout, dq, dk, dv, window, sinks=0, positions=None, first_position=0, cache=None, scale=1.0, workspace=None,
+                              stream=None):
+    """Gradients dq, dk, dv of window_attention from dout and what it kept; the cache's steps are constants."""
+    dims, T, B, H, Hk, Dk, Dv, at = _window_dims(q, k, v, positions, scale)
+    dt, need, L = q.dtype, C.c_int64(), lib()
+    qs, ks, vs, os = (T, B, H, Dk), (T, B, Hk, Dk), (T, B, Hk, Dv), (T, B, H, Dv)
+    _check(L.marl_window_attention_workspace(C.byref(dims), window, sinks, 1, C.byref(need)))
+    _check(L.marl_window_attention_backward(
+        C.byref(dims), window, sinks, _view(q, qs, dt, "q"), _view(k, ks, dt, "k"), _view(v, vs, dt, "v"), at, first_position,
+        _cache(cache, (B, Hk, sinks + window), Dk, Dv, dt, "cache"), _view(out, os, dt, "out"), _floats(lse, (B, H, T), "lse"), _view(dout, os, dt, "dout"),
+        _view(dq, qs, dt, "dq"), _view(dk, ks, dt, "dk"), _view(dv, vs, dt, "dv"), _workspace(workspace, need.value), _stream(stream)))
+    _written(dq, dk, dv)
+
+
+def window_attention_step(q, k, v, cache, positions, out, window, sinks=0, scale=1.0, workspace=None, stream=None):
+    """One step: q [B][Hq][Dk], k, v [B][Hk][D], out [B][Hq][Dv], positions [environments].  k and v go into the cache, which is read with them."""
+    precision, dt = _PRECISION.get(q.dtype), q.dtype
+    if precision is None or q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        raise _refused("q, k, v: float32 or bfloat16 [B][heads][D]")
+    B, H, Dk = q.shape
+    _, Hk, Dv = v.shape
+    at, per = _positions(positions, (), B)
+    dims, need, L = AttentionDims.from_buffer_copy(_DIMS.pack(precision, 1, B, H, Hk, Dk, Dv, per, scale)), C.c_int64(), lib()
+    _check(L.marl_window_attention_workspace(C.byref(dims), window, sinks, 2, C.byref(need)))
+    _check(L.marl_window_attention_step(
+        C.byref(dims), window, sinks, _step_view(q, (B, H, Dk), dt, "q"), _step_view(k, (B, Hk, Dk), dt, "k"), _step_view(v, (B, Hk, Dv), dt, "v"), at,
+        _cache(cache, (B, Hk, sinks + window), Dk, Dv, dt, "cache"), _step_view(out, (B, H, Dv), dt, "out"), _workspace(workspace, need.value), _stream(stream)))
+    _raise_versions((out, *cache))
 
 
 KERNEL_CLASSES = {"gemm_nn": 0, "gemm_nt": 1, "gemm_tn": 2, "env_step": 3, "gae": 4, "fused_train": 5, "rollout": 6}

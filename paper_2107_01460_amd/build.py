@@ -12,6 +12,8 @@ SOURCES = ["api.hip", "env_kernels.hip", "gae_kernels.hip", "policy_kernels.hip"
            "recurrent_kernels.hip", "rollout_v3.hip", "rollout_v5.hip", "rollout_v7.hip"]
 # the operators of sequence memories
 MEMORY_SOURCES = ["linear_attention.hip", "linear_attention_f32.hip", "linear_attention_bf16.hip", "layer_norm.hip", "rotary.hip"]
+# attention over a window, and the norm of heads with their rotation
+WINDOW_SOURCES = ["window_attention_f32.hip", "window_attention_bf16.hip", "window_attention.hip", "norm_rotary.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I", INCLUDE, "-I", CSRC,
          # packed fp32 ALU forms are kept off on this target
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -25,7 +27,7 @@ def _compile(src):
 
 
 def build(verbose=True):
-    sources = SOURCES + MEMORY_SOURCES
+    sources = WINDOW_SOURCES + SOURCES + MEMORY_SOURCES
     with ThreadPoolExecutor(max_workers=min(os.cpu_count() or 8, len(sources))) as ex:
         objs = list(ex.map(_compile, sources))
     subprocess.check_call(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs])

@@ -1,0 +1,504 @@
+// The norm of each head of queries and keys with the rotation by position in the same pass, and its gradient.
+//   u = x r w,  r = 1 / sqrt(mean(x^2) + eps),  y = turn(u);   with du = turn back(dy) and g = du w:  dx = r g - x r^3 mean(g x),  dw = sum over rows of du x r
+// Bound by memory: every element in and out once; table rows, weights and the partners of a rotation come from caches.
+#include "common.h"
+#include "attention_checks.h"
+
+namespace marl {
+namespace {
+
+constexpr int kMaxNormDim = 256;
+
+// Division of n < 2^31 by a number fixed at launch: a product and a shift.
+struct Divisor {
+  uint32_t d = 1, magic = 0;
+  int shift = 0;
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return __umulhi(2 * n, magic) >> (shift - 31); }
+};
+Divisor divisor(uint32_t d) {
+  Divisor r;
+  r.d = d;
+  int lg = 0;
+  while ((1u << lg) < d) ++lg;
+  r.shift = 31 + lg;
+  r.magic = (uint32_t)(((uint64_t)1 << r.shift) / d + 1);
+  return r;
+}
+
+struct NormArray {
+  const char *x, *dy;
+  char* out;  // y, or dx
+  int64_t x_step, x_seq, x_head, dy_step, dy_seq, dy_head, out_step, out_seq, out_head;  // bytes
+  const float* weight;
+  float* part;  // [workgroups][dim]: a workgroup's share of dw
+  Divisor heads;
+  int64_t rows;
+};
+struct NormArgs {
+  NormArray a[2];  // q, k
+  const float* table;
+  const int32_t* positions;
+  int32_t n_positions, first, rotary, dim, inter;
+  float eps;
+  uint32_t n_flags;
+  Divisor B, seqs_per_flag;
+  uint32_t blocks_q;  // workgroups of q; those of k follow
+};
+
+// E elements of a row from `col` on, which may begin before the row or end behind it: zeros there, and nothing outside the row is read.
+template <class T, bool WHOLE>
+__device__ __forceinline__ void get(float (&f)[16 / sizeof(T)], const char* row, int col, int dim) {
+  constexpr int E = 16 / sizeof(T);
+  const T* p = reinterpret_cast<const T*>(row);
+  T v[E];
+  if constexpr (WHOLE) {
+    __builtin_memcpy(v, p + col, 16);  // (at any alignment)
+  } else if (dim >= E) {
+    const int base = min(max(col, 0), dim - E), by = col - base;  // moved down by `by` elements
+    unsigned __int128 w;
+    __builtin_memcpy(&w, p + base, 16);
+    if (by > 0) w = by < E ? w >> 8 * (int)sizeof(T) * by : 0;
+    if (by < 0) w = by > -E ? w << 8 * (int)sizeof(T) * -by : 0;
+    __builtin_memcpy(v, &w, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = col + e >= 0 && col + e < dim ? p[col + e] : (T)0;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) f[e] = load_act(v, e);
+}
+template <class T, bool WHOLE>
+__device__ __forceinline__ void put(char* row, int col, int dim, const float (&f)[16 / sizeof(T)]) {
+  constexpr int E = 16 / sizeof(T);
+  T v[E];
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = f[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      const uint32_t u = pack2_bf16(f[e], f[e + 1]);
+      __builtin_memcpy(v + e, &u, 4);
+    }
+  }
+  T* p = reinterpret_cast<T*>(row) + col;
+  if (WHOLE || col + E <= dim) {
+    __builtin_memcpy(p, v, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (col + e < dim) p[e] = v[e];
+  }
+}
+template <int L>
+__device__ __forceinline__ float sum_of(float v) {  // over L lanes next to each other, in all of them
+#pragma unroll
+  for (int m = 1; m < L; m *= 2) v += __shfl_xor(v, m);
+  return v;
+}
+
+// What a lane's E columns are to the rotation
+template <class T, bool INTER, bool WHOLE>
+struct Columns {
+  static constexpr int E = 16 / sizeof(T);
+  int col, half, rotary;
+  // the table's cosines and sines for a position's row, 1 and 0 behind the rotated part; sine with the sign of an element's partner
+  __device__ __forceinline__ void angles(const float* row, bool known, float (&c)[E], float (&s)[E]) const {
+    const float none = __builtin_nanf("");
+    if constexpr (WHOLE && !INTER) {
+      const bool on = col < rotary;
+      const int at = on ? (col < half ? col : col - half) : 0;
+      const float sign = col < half ? -1.f : 1.f;
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        float a[4], b[4];
+        __builtin_memcpy(a, row + at + e, 16);
+        __builtin_memcpy(b, row + half + at + e, 16);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          c[e + x] = on ? known ? a[x] : none : 1.f;
+          s[e + x] = on ? known ? sign * b[x] : none : 0.f;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int i = col + e;
+        const bool on = i < rotary;
+        const int at = !on ? 0 : INTER ? i / 2 : i < half ? i : i - half;
+        const float sign = INTER ? (e % 2 == 0 ? -1.f : 1.f) : i < half ? -1.f : 1.f;
+        c[e] = on ? known ? row[at] : none : 1.f;
+        s[e] = on ? known ? sign * row[half + at] : none : 0.f;
+      }
+    }
+  }
+  // each element's partner: inside the vector, or half the rotated part away
+  template <class F>
+  __device__ __forceinline__ void partners(const float (&own)[E], float (&p)[E], F load) const {
+    if constexpr (INTER) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) p[e] = own[e ^ 1];
+    } else if constexpr (WHOLE) {
+      if (col < rotary) load(p, col < half ? col + half : col - half);
+      else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) p[e] = 0.f;
+      }
+    } else {
+      float up[E], down[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) up[e] = down[e] = 0.f;
+      if (col < half) load(up, col + half);
+      if (col + E > half && col < rotary) load(down, col - half);
+#pragma unroll
+      for (int e = 0; e < E; ++e) p[e] = col + e < half ? up[e] : col + e < rotary ? down[e] : 0.f;
+    }
+  }
+};
+
+constexpr int kNormRows = 2;  // rows of a lane on their way together
+
+// L lanes take a row.  A workgroup takes one array's rows: forward one run of them, gradient every so many.
+template <class T, int L, bool INTER, bool WHOLE, bool GRADIENT>
+__global__ void __launch_bounds__(256) norm_rotary_kernel(const NormArgs args) {
+  constexpr int E = 16 / sizeof(T), kAtOnce = 256 / L;
+  const bool second = blockIdx.x >= args.blocks_q;
+  const NormArray& a = args.a[second];
+  const uint32_t block = second ? blockIdx.x - args.blocks_q : blockIdx.x, blocks = second ? gridDim.x - args.blocks_q : args.blocks_q;
+  const int dim = args.dim, lane = threadIdx.x % L;
+  Columns<T, INTER, WHOLE> cols{lane * E, args.rotary / 2, args.rotary};
+  const int col = cols.col;
+  const bool on = col < dim;
+  float w[E], wp[E];  // weights, and the partners'
+  auto weights = [&](float (&f)[E], int from) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) f[e] = from + e >= 0 && from + e < dim ? a.weight[from + e] : 0.f;
+  };
+  if (a.weight == nullptr || !on) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) w[e] = wp[e] = 1.f;
+  } else {
+    weights(w, col);
+    if constexpr (!GRADIENT) cols.partners(w, wp, weights);
+  }
+  float dw[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) dw[e] = 0.f;
+  const int64_t run = (int64_t)kAtOnce * kNormRows;
+  for (int64_t first = block * run; first < a.rows; first += blocks * run) {
+    // (a run's first token and the rest by 32-bit division)
+    const int64_t token0 = first / a.heads.d;
+    const uint32_t in0 = (uint32_t)(first - token0 * a.heads.d) + threadIdx.x / L;
+    const int64_t t00 = token0 / args.B.d;
+    const uint32_t b0 = (uint32_t)(token0 - t00 * args.B.d);
+    struct Row {
+      float x[E], xp[E], dy[E], dyp[E];
+      char* out;
+      int position;
+      bool here;
+    } row[kNormRows];
+#pragma unroll
+    for (int u = 0; u < kNormRows; ++u) {
+      Row& r = row[u];
+      const uint32_t at = in0 + u * kAtOnce, more = a.heads(at), head = at - more * a.heads.d;
+      const uint32_t bb = b0 + more, over = args.B(bb), b = bb - over * args.B.d;
+      const int64_t t = t00 + over;
+      r.here = first + u * kAtOnce + threadIdx.x / L < a.rows;
+#pragma unroll
+      for (int e = 0; e < E; ++e) r.x[e] = r.xp[e] = r.dy[e] = r.dyp[e] = 0.f;
+      r.position = -1;
+      r.out = nullptr;
+      if (!r.here) continue;
+      r.position = args.positions != nullptr ? args.positions[t * args.n_flags + args.seqs_per_flag(b)] : args.first + (int)t;
+      r.out = a.out + t * a.out_step + b * a.out_seq + head * a.out_head;
+      if (!on) continue;
+      const char* x = a.x + t * a.x_step + b * a.x_seq + head * a.x_head;
+      get<T, WHOLE>(r.x, x, col, dim);
+      if constexpr (!GRADIENT) {
+        cols.partners(r.x, r.xp, [&](float (&f)[E], int from) { get<T, WHOLE>(f, x, from, dim); });
+      } else {
+        const char* dy = a.dy + t * a.dy_step + b * a.dy_seq + head * a.dy_head;
+        get<T, WHOLE>(r.dy, dy, col, dim);
+        cols.partners(r.dy, r.dyp, [&](float (&f)[E], int from) { get<T, WHOLE>(f, dy, from, dim); });
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kNormRows; ++u) {
+      Row& r = row[u];
+      float squares = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) squares = __builtin_fmaf(r.x[e], r.x[e], squares);
+      squares = sum_of<L>(squares);
+      const float power = squares / (float)dim + args.eps, rstd = 1.f / __builtin_sqrtf(power);
+      const bool known = r.position < args.n_positions;
+      float c[E], s[E], y[E];
+      cols.angles(args.table + (int64_t)(known ? max(r.position, 0) : 0) * args.rotary, known, c, s);
+      if constexpr (!GRADIENT) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = r.x[e] * rstd * w[e] * c[e] + r.xp[e] * rstd * wp[e] * s[e];
+      } else {
+        float g[E], du[E], dot = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          du[e] = r.dy[e] * c[e] - r.dyp[e] * s[e];
+          g[e] = du[e] * w[e];
+          if (on) dot = __builtin_fmaf(g[e], r.x[e], dot);
+        }
+        dot = sum_of<L>(dot);
+        const float back = rstd * rstd * (dot / (float)dim);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          y[e] = rstd * (g[e] - r.x[e] * back);
+          if (r.position >= 0 && on) dw[e] = __builtin_fmaf(du[e], r.x[e] * rstd, dw[e]);
+        }
+      }
+      if (r.position < 0) {  // no step: zeros
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = 0.f;
+      }
+      if (r.here && on) put<T, WHOLE>(r.out, col, dim, y);
+    }
+  }
+  if constexpr (GRADIENT) {
+    if (a.part == nullptr) return;
+    // the lanes that took the same columns, in the order of the threads
+    __shared__ float sums[256 / L][L * E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[threadIdx.x / L][lane * E + e] = dw[e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < dim; i += 256) {
+      float sum = 0.f;
+      for (int r = 0; r < 256 / L; ++r) sum += sums[r][i];
+      a.part[(int64_t)block * dim + i] = sum;
+    }
+  }
+}
+
+// dw: the workgroups' shares, 32 columns a workgroup, in a fixed order
+struct WeightArgs {
+  const float* part[2];
+  float* out[2];
+  int32_t n[2], dim;
+};
+__global__ void __launch_bounds__(1024) norm_weight_kernel(const WeightArgs a) {
+  __shared__ float sums[32][33];
+  const int which = blockIdx.y, c = threadIdx.x % 32, r = threadIdx.x / 32, col = blockIdx.x * 32 + c;
+  if (a.out[which] == nullptr) return;
+  float sum = 0.f;
+  if (col < a.dim) {
+#pragma unroll 8
+    for (int i = r; i < a.n[which]; i += 32) sum += a.part[which][(int64_t)i * a.dim + col];
+  }
+  sums[r][c] = sum;
+  __syncthreads();
+  if (r == 0 && col < a.dim) {
+    float all = 0.f;
+    for (int i = 0; i < 32; ++i) all += sums[i][c];
+    a.out[which][col] = all;
+  }
+}
+
+int lanes_of(int precision, int dim) {
+  const int units = (dim + (precision == 0 ? 3 : 7)) / (precision == 0 ? 4 : 8);
+  int L = 1;
+  while (L < units) L *= 2;
+  return L;
+}
+// Workgroups of an array: a run of rows each, in the gradient as many as fill the chip
+constexpr int64_t kGradientBlocks = 2048;
+int64_t blocks_of(int64_t rows, int L, bool gradient) {
+  const int64_t run = 256 / L * kNormRows, n = (rows + run - 1) / run;
+  return gradient && n > kGradientBlocks ? kGradientBlocks : n;
+}
+
+template <class T, int L, bool GRADIENT>
+void launch_lanes(const NormArgs& a, unsigned blocks, bool inter, bool whole, hipStream_t s) {
+  if (inter && whole) hipLaunchKernelGGL((norm_rotary_kernel<T, L, true, true, GRADIENT>), dim3(blocks), dim3(256), 0, s, a);
+  else if (inter) hipLaunchKernelGGL((norm_rotary_kernel<T, L, true, false, GRADIENT>), dim3(blocks), dim3(256), 0, s, a);
+  else if (whole) hipLaunchKernelGGL((norm_rotary_kernel<T, L, false, true, GRADIENT>), dim3(blocks), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((norm_rotary_kernel<T, L, false, false, GRADIENT>), dim3(blocks), dim3(256), 0, s, a);
+}
+template <class T, bool GRADIENT>
+void launch_norm(const NormArgs& a, int L, unsigned blocks, bool inter, bool whole, hipStream_t s) {
+  if (L == 1) launch_lanes<T, 1, GRADIENT>(a, blocks, inter, whole, s);
+  else if (L == 2) launch_lanes<T, 2, GRADIENT>(a, blocks, inter, whole, s);
+  else if (L == 4) launch_lanes<T, 4, GRADIENT>(a, blocks, inter, whole, s);
+  else if (L == 8) launch_lanes<T, 8, GRADIENT>(a, blocks, inter, whole, s);
+  else if (L == 16) launch_lanes<T, 16, GRADIENT>(a, blocks, inter, whole, s);
+  else if (L == 32) launch_lanes<T, 32, GRADIENT>(a, blocks, inter, whole, s);
+  else if constexpr (sizeof(T) == 4) launch_lanes<T, 64, GRADIENT>(a, blocks, inter, whole, s);
+}
+
+int32_t check_norm(const marl_attention_dims* dims, bool k) {
+  if (dims == nullptr) return MARL_E_NULL;
+  const marl_attention_dims& d = *dims;
+  if (d.precision != 0 && d.precision != 1) return MARL_E_CONFIG;
+  if (d.n_steps < 0 || d.n_steps > (1 << 30) || d.n_seqs < 0 || d.n_seqs > (1 << 30) || d.dim_k < 1 || d.dim_k > kMaxNormDim) return MARL_E_SIZE;
+  if (d.n_heads < 1 || d.n_heads > (1 << 14) || (k && (d.n_kv_heads < 1 || d.n_kv_heads > (1 << 14)))) return MARL_E_CONFIG;
+  if (d.seqs_per_flag < 1 || d.n_seqs % d.seqs_per_flag != 0) return MARL_E_CONFIG;
+  const int64_t tokens = (int64_t)d.n_steps * d.n_seqs;
+  if (tokens > ((int64_t)1 << 48) / (1 << 15)) return MARL_E_SIZE;
+  const int L = lanes_of(d.precision, d.dim_k);
+  const int64_t blocks = blocks_of(tokens * d.n_heads, L, false) + (k ? blocks_of(tokens * d.n_kv_heads, L, false) : 0);
+  return launchable(blocks, 256) ? MARL_OK : MARL_E_SIZE;
+}
+int32_t check_turn(const marl_attention_dims& d, float eps, const float* table, int32_t n_positions, int32_t rotary_dim, const int32_t* positions,
+                   int32_t first, int32_t interleaved) {
+  if (n_positions < 1 || rotary_dim < 2 || rotary_dim > d.dim_k) return MARL_E_SIZE;
+  if (rotary_dim % 2 != 0 || interleaved < 0 || interleaved > 1 || !(eps >= 0.f) || !(eps < __builtin_inff())) return MARL_E_CONFIG;
+  if (positions == nullptr && (int64_t)first + d.n_steps > 0x7fffffff) return MARL_E_SIZE;
+  MARL_REQUIRE_PTR(table);
+  return (reinterpret_cast<uintptr_t>(positions) & 3u) != 0 ? MARL_E_ALIGN : MARL_OK;
+}
+int32_t check_vector(const float* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0 ? MARL_E_ALIGN : MARL_OK; }
+// An output in the place of an input has its strides
+int32_t check_in_place(const marl_view& out, const marl_view& in, const marl_attention_dims& d, int heads) {
+  if (out.data != in.data) return MARL_OK;
+  return (out.step != in.step && d.n_steps > 1) || (out.seq != in.seq && d.n_seqs > 1) || (out.head != in.head && heads > 1) ? MARL_E_CONFIG : MARL_OK;
+}
+
+NormArray array_of(const marl_attention_dims& d, const marl_view& x, const marl_view* dy, const marl_view& out, int heads, const float* weight) {
+  const int elem = d.precision == 0 ? 4 : 2;
+  NormArray a{};
+  a.x = static_cast<const char*>(x.data);
+  a.x_step = x.step * elem;
+  a.x_seq = x.seq * elem;
+  a.x_head = x.head * elem;
+  if (dy != nullptr) {
+    a.dy = static_cast<const char*>(dy->data);
+    a.dy_step = dy->step * elem;
+    a.dy_seq = dy->seq * elem;
+    a.dy_head = dy->head * elem;
+  }
+  a.out = static_cast<char*>(out.data);
+  a.out_step = out.step * elem;
+  a.out_seq = out.seq * elem;
+  a.out_head = out.head * elem;
+  a.weight = weight;
+  a.heads = divisor((uint32_t)heads);
+  a.rows = (int64_t)d.n_steps * d.n_seqs * heads;
+  return a;
+}
+NormArgs args_of(const marl_attention_dims& d, float eps, const float* table, int32_t n_positions, int32_t rotary_dim, const int32_t* positions,
+                 int32_t first, int32_t interleaved) {
+  NormArgs a{};
+  a.table = table;
+  a.positions = positions;
+  a.n_positions = n_positions;
+  a.first = first;
+  a.rotary = rotary_dim;
+  a.dim = d.dim_k;
+  a.inter = interleaved;
+  a.eps = eps;
+  a.n_flags = (uint32_t)(d.n_seqs / d.seqs_per_flag);
+  a.B = divisor((uint32_t)d.n_seqs);
+  a.seqs_per_flag = divisor((uint32_t)d.seqs_per_flag);
+  return a;
+}
+int32_t run(NormArgs& a, const marl_attention_dims& d, bool gradient, bool k, hipStream_t s) {
+  const int L = lanes_of(d.precision, d.dim_k), E = d.precision == 0 ? 4 : 8;
+  const bool whole = d.dim_k % E == 0 && (a.inter || a.rotary / 2 % E == 0);
+  a.blocks_q = (uint32_t)blocks_of(a.a[0].rows, L, gradient);
+  const unsigned blocks = a.blocks_q + (k ? (unsigned)blocks_of(a.a[1].rows, L, gradient) : 0);
+  if (d.precision == 0) (gradient ? launch_norm<float, true> : launch_norm<float, false>)(a, L, blocks, a.inter != 0, whole, s);
+  else (gradient ? launch_norm<bf16_t, true> : launch_norm<bf16_t, false>)(a, L, blocks, a.inter != 0, whole, s);
+  return launch_status();
+}
+
+}  // namespace
+}  // namespace marl
+
+using namespace marl;
+
+extern "C" {
+
+int32_t marl_norm_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, const float* q_weight, const float* k_weight, float eps,
+                         const float* table, int32_t n_positions, int32_t rotary_dim, const int32_t* positions, int32_t first_position,
+                         int32_t interleaved, marl_view q_out, marl_view k_out, void* stream) {
+  const bool two = k.data != nullptr;
+  MARL_CHECK(check_norm(dims, two));
+  const marl_attention_dims& d = *dims;
+  const bool used = d.n_steps > 0 && d.n_seqs > 0;
+  if (!used) return MARL_OK;
+  MARL_CHECK(check_turn(d, eps, table, n_positions, rotary_dim, positions, first_position, interleaved));
+  MARL_CHECK(check_vector(q_weight));
+  MARL_CHECK(check_vector(k_weight));
+  const marl_view in[2] = {q, k}, out[2] = {q_out, k_out};
+  for (int u = 0; u < (two ? 2 : 1); ++u) {
+    const int heads = u == 0 ? d.n_heads : d.n_kv_heads;
+    MARL_CHECK(check_view(in[u], d.precision, true));
+    MARL_CHECK(check_view(out[u], d.precision, true));
+    MARL_CHECK(check_output(out[u], d, heads, true));
+    MARL_CHECK(check_in_place(out[u], in[u], d, heads));
+  }
+  if (two && (q_out.data == k_out.data || q_out.data == k.data || k_out.data == q.data)) return MARL_E_CONFIG;
+  NormArgs a = args_of(d, eps, table, n_positions, rotary_dim, positions, first_position, interleaved);
+  a.a[0] = array_of(d, q, nullptr, q_out, d.n_heads, q_weight);
+  if (two) a.a[1] = array_of(d, k, nullptr, k_out, d.n_kv_heads, k_weight);
+  return run(a, d, false, two, (hipStream_t)stream);
+}
+
+int32_t marl_norm_rotary_workspace(const marl_attention_dims* dims, int64_t* bytes) {
+  MARL_CHECK(check_norm(dims, true));
+  if (bytes == nullptr) return MARL_E_NULL;
+  *bytes = 2 * ((kGradientBlocks * dims->dim_k * 4 + 255) / 256 * 256);
+  return MARL_OK;
+}
+
+int32_t marl_norm_rotary_backward(const marl_attention_dims* dims, marl_view dq_out, marl_view dk_out, marl_view q, marl_view k, const float* q_weight,
+                                  const float* k_weight, float eps, const float* table, int32_t n_positions, int32_t rotary_dim,
+                                  const int32_t* positions, int32_t first_position, int32_t interleaved, marl_view dq, marl_view dk,
+                                  float* dq_weight, float* dk_weight, void* workspace, void* stream) {
+  const bool two = k.data != nullptr;
+  MARL_CHECK(check_norm(dims, two));
+  const marl_attention_dims& d = *dims;
+  const bool used = d.n_steps > 0 && d.n_seqs > 0;
+  MARL_CHECK(check_vector(q_weight));
+  MARL_CHECK(check_vector(k_weight));
+  MARL_CHECK(check_vector(dq_weight));
+  MARL_CHECK(check_vector(dk_weight));
+  if (dq_weight != nullptr && dq_weight == dk_weight) return MARL_E_CONFIG;
+  const bool weights = dq_weight != nullptr || (two && dk_weight != nullptr);
+  const marl_view in[2] = {q, k}, grad[2] = {dq_out, dk_out}, out[2] = {dq, dk};
+  if (used) {
+    MARL_CHECK(check_turn(d, eps, table, n_positions, rotary_dim, positions, first_position, interleaved));
+    if (weights) MARL_REQUIRE_PTR(workspace);
+    for (int u = 0; u < (two ? 2 : 1); ++u) {
+      const int heads = u == 0 ? d.n_heads : d.n_kv_heads;
+      MARL_CHECK(check_view(in[u], d.precision, true));
+      MARL_CHECK(check_view(grad[u], d.precision, true));
+      MARL_CHECK(check_view(out[u], d.precision, true));
+      MARL_CHECK(check_output(out[u], d, heads, true));
+      MARL_CHECK(check_in_place(out[u], in[u], d, heads));
+      MARL_CHECK(check_in_place(out[u], grad[u], d, heads));
+    }
+    if (two) {
+      MARL_CHECK(check_places(dq, {k, dk_out, dk}, true));
+      MARL_CHECK(check_places(dk, {q, dq_out}, true));
+    }
+  }
+  hipStream_t s = (hipStream_t)stream;
+  NormArgs a = args_of(d, eps, table, n_positions, rotary_dim, positions, first_position, interleaved);
+  const int64_t half = (kGradientBlocks * d.dim_k * 4 + 255) / 256 * 256;
+  WeightArgs w{};
+  w.dim = d.dim_k;
+  if (used) {
+    a.a[0] = array_of(d, q, &dq_out, dq, d.n_heads, q_weight);
+    if (two) a.a[1] = array_of(d, k, &dk_out, dk, d.n_kv_heads, k_weight);
+    if (dq_weight != nullptr) a.a[0].part = static_cast<float*>(workspace);
+    if (two && dk_weight != nullptr) a.a[1].part = reinterpret_cast<float*>(static_cast<char*>(workspace) + half);
+    MARL_CHECK(run(a, d, true, two, s));
+    const int L = lanes_of(d.precision, d.dim_k);
+    w.part[0] = a.a[0].part;
+    w.part[1] = a.a[1].part;
+    w.n[0] = (int32_t)blocks_of(a.a[0].rows, L, true);
+    w.n[1] = two ? (int32_t)blocks_of(a.a[1].rows, L, true) : 0;
+  }
+  if (!weights) return MARL_OK;
+  w.out[0] = dq_weight;
+  w.out[1] = two ? dk_weight : nullptr;
+  hipLaunchKernelGGL(norm_weight_kernel, dim3((d.dim_k + 31) / 32, 2), dim3(1024), 0, s, w);
+  return launch_status();
+}
+
+}  // extern "C"

@@ -1,0 +1,777 @@
+// Attention over a window of the last steps and the first steps of an episode, on the matrix cores.
+//
+// Row i (a query) sees column j (a key) where j is a step of i's episode up to i and i - j < window or j is among the episode's first `sinks` steps:
+//   s_ij = scale q_i . k_j,  lse_i = log sum_j exp s_ij,  P_ij = exp(s_ij - lse_i),  out_i = sum_j P_ij v_j
+//   delta_i = dout_i . out_i,  dS_ij = P_ij (dout_i . v_j - delta_i),  dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i
+//
+// All three passes (output; dq; dk and dv) are one scheme.  A wavefront owns 32 rows of two arrays ("own": queries, or keys and values), whose
+// rows stay in registers as the second operand, one row a lane; tiles of 32 rows of two other arrays ("streamed") go through LDS, fetched one tile ahead and shared by
+// the workgroup's wavefronts.  The first product S^T = Y own^T leaves a lane 16 of the 32 streamed rows of its own column; that layout is the second operand
+// of the next product, acc^T += Y^T P, as it is, once the contraction runs over the streamed rows in the order in which the registers hold them.
+// So scores and weights never leave the registers; softmax statistics are one number a lane, joined between the two halves of a wavefront.
+// Y^T comes from the same row-major tile: transposed reads of 4 x 16 for bf16, single elements for fp32.
+//
+// bf16: inputs are exact operands, sums are fp32.  P and dS are rounded once to bf16 as operands (2^-9 of each term; the statistics lse and the row
+// sums come from the fp32 values): about what the output's own rounding is, and half the matrix products of keeping two parts.  fp32: fp32 products.
+//
+// Zero times infinity: a product of tiles multiplies masked places by zero.  The loop runs without care for it; a workgroup that finds
+// an infinity or a NaN in its sums runs once more, adding the streamed rows one by one to the columns that see them only.
+#pragma once
+#include <type_traits>
+
+#include "common.h"
+
+namespace marl {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kTile = 32;
+
+struct WindowArray {
+  char* data;
+  int64_t step, seq, head;  // bytes
+};
+struct WindowArgs {
+  WindowArray q, k, v, out, dout, dq, dk, dv;
+  const char *cache_k, *cache_v;  // [B][Hk][slots][dim], null: none
+  const int32_t* positions;       // null: first + t
+  int32_t first;
+  uint32_t n_flags, seqs_per_flag;
+  float *lse, *delta;  // [B][H][T]
+  int2* reach;         // [n_flags][tiles]: of a tile's rows, the earliest and the latest beginning of an episode
+  int32_t T;
+  uint32_t B, H, Hk, group;
+  int32_t dk_dim, dv_dim, window, sinks;
+  float scale, c;      // c = |scale| log2(e)
+  uint32_t flip;       // the sign of a negative scale, for the elements of an own array (two of bf16, one of fp32)
+  uint32_t heads_each; // query heads of a key head that a workgroup takes
+  uint32_t blocks_t;   // workgroups along time
+};
+
+__device__ __forceinline__ int position_of(const WindowArgs& a, int t, uint32_t env) {
+  return a.positions != nullptr ? a.positions[(int64_t)t * a.n_flags + env] : a.first + t;
+}
+
+// What a row sees.  Rows that hold no step see nothing.
+struct Row {
+  int i, start, lo;       // steps from `lo` to i
+  uint32_t span, n_sinks; // i - lo; first steps from `start` on
+  int position;           // negative: no step
+  __device__ __forceinline__ bool valid() const { return position >= 0; }
+  __device__ __forceinline__ bool sees(int j) const { return (uint32_t)(j - lo) <= span || (uint32_t)(j - start) < n_sinks; }
+};
+__device__ __forceinline__ Row row_of(const WindowArgs& a, int i, uint32_t env) {
+  Row r;
+  r.i = i;
+  r.position = i < a.T ? position_of(a, i, env) : -1;
+  if (r.position < 0) {
+    r.position = -1;
+    r.start = r.lo = 0x7fffffff;
+    r.span = r.n_sinks = 0;
+    return r;
+  }
+  r.start = i - r.position;
+  r.lo = max(r.start, i - a.window + 1);
+  r.span = (uint32_t)(i - r.lo);
+  r.n_sinks = (uint32_t)(min(a.sinks - 1, r.position) + 1);
+  return r;
+}
+
+// What a rare branch computes from a value that never changes goes through here: the compiler otherwise keeps it in registers across the loop.
+__device__ __forceinline__ int fresh(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+template <class F>
+__device__ __forceinline__ int wave_reduce(int v, F f) {
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) v = f(v, __shfl_xor(v, m));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_min(int v) { return wave_reduce(v, [](int a, int b) { return min(a, b); }); }
+__device__ __forceinline__ int wave_max(int v) { return wave_reduce(v, [](int a, int b) { return max(a, b); }); }
+
+// ---- 16 bytes of a row ---------------------------------------------------------------------------------------------------------------
+// Elements from `col` on, zeros behind the row's `dim`; nothing behind the row is read.
+template <class T>
+__device__ __forceinline__ uint4 load_unit(const char* row, int col, int dim) {
+  constexpr int E = 16 / sizeof(T), kBits = 8 * sizeof(T);
+  const T* p = reinterpret_cast<const T*>(row);
+  unsigned __int128 w = 0;
+  if (dim >= E) {  // at any alignment; at the row's end its last 16 bytes, moved into place
+    const int base = min(col, dim - E);
+    __builtin_memcpy(&w, p + base, 16);
+    if (dim % E != 0) w = col - base < E ? w >> kBits * (col - base) : 0;
+    else if (col != base) w = 0;
+  } else if (col == 0) {
+#pragma unroll 1
+    for (int e = 0; e < dim; ++e) {
+      uint32_t u = 0;
+      __builtin_memcpy(&u, p + e, sizeof(T));
+      w |= (unsigned __int128)u << kBits * e;
+    }
+  }
+  uint4 r;
+  __builtin_memcpy(&r, &w, 16);
+  return r;
+}
+
+// ---- tiles in LDS -------------------------------------------------------------------------------------------------------------------
+// Rows of DP elements and 16 bytes, so that eight consecutive rows' 16-byte pieces lie in different banks.
+template <class T, int DP>
+struct TileShape {
+  static constexpr int kStride = DP * (int)sizeof(T) + 16;
+  static constexpr int kBytes = kTile * kStride;
+  static constexpr int kUnits = DP * (int)sizeof(T) / 16;  // of a row
+};
+
+// A workgroup's fetch of a tile, held in registers until the tile's place is free.
+template <class T, int DP, int WAVES>
+struct Fetch {
+  static constexpr int kThreads = 64 * WAVES, kAll = kTile * TileShape<T, DP>::kUnits, kEach = (kAll + kThreads - 1) / kThreads;
+  uint4 v[kEach];
+  // rows from `rows` on, `step` bytes apart, `count` of them; the others zero
+  __device__ __forceinline__ void request(const char* rows, int64_t step, int count, int dim) {
+    constexpr int E = 16 / sizeof(T);
+    const bool whole = dim % E == 0;  // no unit ends inside
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int at = threadIdx.x + u * kThreads, row = at / TileShape<T, DP>::kUnits, c = at % TileShape<T, DP>::kUnits;
+      v[u] = make_uint4(0, 0, 0, 0);
+      if (whole && row < count && c * E < dim) __builtin_memcpy(&v[u], rows + row * step + 16 * c, 16);  // (at any alignment)
+    }
+    if (whole) return;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int at = fresh(threadIdx.x) + u * kThreads, row = at / TileShape<T, DP>::kUnits, c = at % TileShape<T, DP>::kUnits;
+      if (row < count) v[u] = load_unit<T>(rows + row * step, c * E, dim);
+    }
+  }
+  __device__ __forceinline__ void store(char* tile) const {
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int at = threadIdx.x + u * kThreads, row = at / TileShape<T, DP>::kUnits, c = at % TileShape<T, DP>::kUnits;
+      if (kAll % kThreads == 0 || at < kAll) *reinterpret_cast<uint4*>(tile + row * TileShape<T, DP>::kStride + 16 * c) = v[u];
+    }
+  }
+};
+
+// ---- products ----------------------------------------------------------------------------------------------------------------------
+// The row among 32 that register r of a 32 x 32 result holds in half h of a wavefront
+__device__ __forceinline__ constexpr int result_row(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
+
+template <class T, int DP>
+struct Products;
+
+template <int DP>
+struct Products<bf16_t, DP> {
+  typedef TileShape<bf16_t, DP> Shape;
+  struct Own {
+    bf16x8_t v[DP / 16];
+  };
+  static __device__ __forceinline__ void load_own(Own& own, const char* row, int dim, bool on, uint32_t flip) {
+    const int h = (threadIdx.x & 63) / 32;
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (on) u = load_unit<bf16_t>(row, 16 * s + 8 * h, dim);
+      u.x ^= flip; u.y ^= flip; u.z ^= flip; u.w ^= flip;
+      __builtin_memcpy(&own.v[s], &u, 16);
+    }
+  }
+  static __device__ __forceinline__ float dot(const Own& a, const Own& b) {  // of this half's elements
+    float s = 0.f;
+#pragma unroll
+    for (int n = 0; n < DP / 16; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += (float)a.v[n][e] * (float)b.v[n][e];
+    return s;
+  }
+  static __device__ __forceinline__ f32x16_t score(const char* tile, const Own& own) {
+    const int lane = threadIdx.x & 63;
+    const char* p = tile + (lane % 32) * Shape::kStride + 16 * (lane / 32);
+    f32x16_t s = {0.f};
+#pragma unroll
+    for (int n = 0; n < DP / 16; ++n) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8_t*>(p + 32 * n), own.v[n], s, 0, 0, 0);
+    return s;
+  }
+  typedef short s16x8_t __attribute__((ext_vector_type(8)));
+  // Four streamed rows of sixteen columns, transposed, for rows 16 g of columns 32 t
+  static __device__ __forceinline__ s16x8_t turned(const char* tile, int t, int g) {
+    const int lane = threadIdx.x & 63;
+    const char* p = tile + (16 * g + 4 * (lane / 32) + lane % 16 / 4) * Shape::kStride + 2 * (32 * t + 16 * (lane / 16 % 2) + 4 * (lane % 4));
+    typedef __attribute__((address_space(3))) i16x4_t* Lds;
+    const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 8 * Shape::kStride));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  static __device__ __forceinline__ bf16x8_t pack(const float* p) {
+    uint4 u = make_uint4(pack2_bf16(p[0], p[1]), pack2_bf16(p[2], p[3]), pack2_bf16(p[4], p[5]), pack2_bf16(p[6], p[7]));
+    bf16x8_t r;
+    __builtin_memcpy(&r, &u, 16);
+    return r;
+  }
+  template <int N>
+  static __device__ __forceinline__ void add(f32x16_t (&acc)[N], const char* tile, const float (&p)[16]) {
+    const bf16x8_t w[2] = {pack(p), pack(p + 8)};
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int t = 0; t < N; ++t)
+        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, turned(tile, t, g)), w[g], acc[t], 0, 0, 0);
+  }
+};
+
+template <int DP>
+struct Products<float, DP> {
+  typedef TileShape<float, DP> Shape;
+  struct Own {
+    float4 v[DP / 8];
+  };
+  static __device__ __forceinline__ void load_own(Own& own, const char* row, int dim, bool on, uint32_t flip) {
+    const int h = (threadIdx.x & 63) / 32;
+#pragma unroll
+    for (int s = 0; s < DP / 8; ++s) {
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (on) u = load_unit<float>(row, 8 * s + 4 * h, dim);
+      u.x ^= flip; u.y ^= flip; u.z ^= flip; u.w ^= flip;
+      __builtin_memcpy(&own.v[s], &u, 16);
+    }
+  }
+  static __device__ __forceinline__ float dot(const Own& a, const Own& b) {
+    float s = 0.f;
+#pragma unroll
+    for (int n = 0; n < DP / 8; ++n) s += a.v[n].x * b.v[n].x + a.v[n].y * b.v[n].y + a.v[n].z * b.v[n].z + a.v[n].w * b.v[n].w;
+    return s;
+  }
+  static __device__ __forceinline__ f32x16_t score(const char* tile, const Own& own) {
+    const int lane = threadIdx.x & 63;
+    const char* p = tile + (lane % 32) * Shape::kStride + 16 * (lane / 32);
+    f32x16_t s = {0.f};
+#pragma unroll
+    for (int n = 0; n < DP / 8; ++n) {
+      const float4 y = *reinterpret_cast<const float4*>(p + 32 * n);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(y.x, own.v[n].x, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(y.y, own.v[n].y, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(y.z, own.v[n].z, s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(y.w, own.v[n].w, s, 0, 0, 0);
+    }
+    return s;
+  }
+  template <int N>
+  static __device__ __forceinline__ void add(f32x16_t (&acc)[N], const char* tile, const float (&p)[16]) {
+    const int lane = threadIdx.x & 63;
+    const char* y = tile + 4 * (lane / 32) * Shape::kStride + 4 * (lane % 32);
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int t = 0; t < N; ++t)
+        acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(y + result_row(r, 0) * Shape::kStride + 128 * t), p[r], acc[t], 0, 0, 0);
+  }
+};
+
+// acc^T += Y^T P one streamed row after another (weights of rows that a column does not see are zero), for tiles that hold infinities or NaNs: a column takes the rows that it sees (bit r of `seen` for the row
+// of register r) and nothing else.  On the vector units, few registers at a time: this must not cost the loop around it any.
+template <class T, int DP>
+__device__ __forceinline__ void add_with_care(f32x16_t (&acc)[DP / 32], const char* tile, const float (&p)[16], uint32_t seen) {
+  const int lane = fresh(threadIdx.x & 63), half = lane / 32;
+#pragma unroll 1
+  for (int row = 0; row < kTile; ++row) {
+    const int from = row / 4 % 2, at = row / 8 * 4 + row % 4;  // the half and the register that hold the row's weights
+    float w = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w = r == at ? p[r] : w;
+    w = __shfl(w, lane % 32 + 32 * from);
+    const bool on = __shfl((int)seen, lane % 32 + 32 * from) >> at & 1;
+    // (a bit mask, not a choice: the compiler makes branches of choices here, with half of the registers inside them)
+    const uint32_t mask = on ? 0xffffffffu : 0u;
+    const T* y = reinterpret_cast<const T*>(tile + row * TileShape<T, DP>::kStride);
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = load_act(y, 32 * t + result_row(r, 0) + 4 * half + e);
+          acc[t][r + e] = __builtin_fmaf(w, __uint_as_float(__float_as_uint(v) & mask), acc[t][r + e]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  }
+}
+
+template <int N>
+__device__ __forceinline__ bool not_finite(const f32x16_t (&acc)[N]) {
+  bool bad = false;
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) bad |= !(__builtin_fabsf(acc[t][r]) < __builtin_inff());
+  return bad;
+}
+
+template <class T>
+__device__ __forceinline__ void store4(char* p, float a, float b, float c, float d) {
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+  else *reinterpret_cast<uint2*>(p) = make_uint2(pack2_bf16(a, b), pack2_bf16(c, d));
+}
+
+// 32 own rows out: through a place in LDS of the wavefront's own, so that rows are stored in runs of 16 bytes a lane.  acc^T holds an own row a lane.
+template <class T, int DP>
+__device__ __forceinline__ void store_rows(char* place, const f32x16_t (&acc)[DP / 32], float factor, bool zero, char* rows, int64_t step, int count, int dim) {
+  typedef TileShape<T, DP> Shape;
+  constexpr int E = 16 / sizeof(T);
+  const int lane = threadIdx.x & 63, h = lane / 32;
+  char* mine = place + (lane % 32) * Shape::kStride;
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      float o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = zero ? 0.f : acc[t][r + e] * factor;
+      store4<T>(mine + (int)sizeof(T) * (32 * t + result_row(r, h)), o[0], o[1], o[2], o[3]);
+    }
+  // (one wavefront's LDS accesses are done in order; the fence keeps the compiler from moving the reads up)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  if (dim % E == 0) {  // no unit ends inside
+#pragma unroll
+    for (int u = 0; u < kTile * Shape::kUnits / 64; ++u) {
+      const int at = lane + 64 * u, row = at / Shape::kUnits, c = at % Shape::kUnits * E;
+      const uint4 v = *reinterpret_cast<const uint4*>(place + row * Shape::kStride + (int)sizeof(T) * c);
+      if (row < count && c < dim) __builtin_memcpy(rows + row * step + (int)sizeof(T) * c, &v, 16);
+    }
+  } else {
+#pragma unroll 1
+    for (int at = lane; at < kTile * DP; at += 64) {
+      const int row = at / DP, c = at % DP;
+      if (row < count && c < dim) reinterpret_cast<T*>(rows + row * step)[c] = *reinterpret_cast<const T*>(place + row * Shape::kStride + (int)sizeof(T) * c);
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// ---- which tiles a workgroup's rows see ------------------------------------------------------------------------------------------------
+// Tiles of cached slots first, then tiles of first steps, then the window's.
+enum { TILE_CACHE, TILE_SINK, TILE_WINDOW, TILE_NONE };
+struct Tile {
+  int kind, at;
+};
+struct Tiles {
+  // of the workgroup's rows (up to 128, two a lane)
+  Row r0, r1;
+  int first_window, last_window;  // tiles
+  int cached;                     // slots that hold a step
+  int newest_slot, newest;        // the slot of the cache's last step, and that step
+  int least;                      // the least position of a row whose episode began before step 0
+  bool any_sinks;
+
+  __device__ __forceinline__ void set(const WindowArgs& a, uint32_t env, int row0, int rows) {
+    const int lane = threadIdx.x & 63;
+    r0 = row_of(a, lane < rows ? row0 + lane : a.T, env);
+    r1 = row_of(a, 64 + lane < rows ? row0 + 64 + lane : a.T, env);
+    const int top = max(r0.valid() ? r0.i : -1, r1.valid() ? r1.i : -1);
+    first_window = max(wave_min(min(r0.lo, r1.lo)), 0) / kTile;
+    last_window = wave_max(top);
+    last_window = last_window < 0 ? -1 : last_window / kTile;
+    any_sinks = a.sinks > 0 && last_window >= 0;
+    cached = 0;
+    newest_slot = newest = 0;
+    least = 0x7fffffff;
+    if (a.cache_k != nullptr) {
+      const int n = __builtin_amdgcn_readfirstlane(position_of(a, 0, env));
+      least = wave_min(min(r0.valid() && r0.start < 0 ? r0.position : 0x7fffffff, r1.valid() && r1.start < 0 ? r1.position : 0x7fffffff));
+      if (n > 0 && least != 0x7fffffff) {
+        cached = min(n, a.sinks + a.window);
+        newest = n - 1;
+        newest_slot = newest < a.sinks ? newest : a.sinks + (newest - a.sinks) % a.window;
+      }
+    }
+  }
+  // the step that a slot below `cached` holds
+  __device__ __forceinline__ int step_of(const WindowArgs& a, int slot) const {
+    if (newest < a.sinks + a.window || slot < a.sinks) return slot;  // (not yet gone round)
+    return newest - newest_slot + slot - (slot <= newest_slot ? 0 : a.window);
+  }
+  __device__ __forceinline__ int sink_tile(const Row& r, int from) const {
+    if (r.n_sinks == 0) return 0x7fffffff;
+    const int last = r.start + (int)r.n_sinks - 1;
+    if (last < 0 || last / kTile < from) return 0x7fffffff;
+    return max(max(r.start, 0) / kTile, from);
+  }
+  // the one behind t
+  __device__ __forceinline__ Tile next(const WindowArgs& a, Tile t) const {
+    if (t.kind == TILE_CACHE) {
+      while (++t.at * kTile < cached) {
+        const int slot = t.at * kTile + (threadIdx.x & 31);
+        bool needed = false;
+        if (slot < cached) needed = slot < a.sinks || least - step_of(a, slot) < a.window;
+        if (__ballot(needed) != 0) return t;
+      }
+      t.kind = TILE_SINK;
+      t.at = -1;
+    }
+    if (t.kind == TILE_SINK) {
+      if (any_sinks) {
+        const int n = wave_min(min(sink_tile(r0, t.at + 1), sink_tile(r1, t.at + 1)));
+        if (n < first_window) return {TILE_SINK, n};
+      }
+      t.kind = TILE_WINDOW;
+      t.at = first_window - 1;
+    }
+    ++t.at;
+    if (t.at > last_window) t.kind = TILE_NONE;
+    return t;
+  }
+};
+
+// Wavefronts a SIMD that the registers are shared out for: two where that spills none
+template <class T, int DP, bool GRADIENT>
+constexpr int rows_waves() { return sizeof(T) == 4 && DP > 64 ? 1 : 2; }
+template <class T, int DP>
+constexpr int columns_waves() { return DP > (sizeof(T) == 4 ? 32 : 64) ? 1 : 2; }
+
+// ---- output, and dq ------------------------------------------------------------------------------------------------------------------
+// A workgroup: `heads_each` query heads of one key head, WAVES / heads_each tiles of 32 rows each.
+template <class T, int DP, int WAVES, bool GRADIENT>
+__global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) window_rows_kernel(const WindowArgs a) {
+  typedef Products<T, DP> P;
+  typedef TileShape<T, DP> Shape;
+  __shared__ __attribute__((aligned(16))) char lds[(WAVES > 4 ? WAVES : 4) * Shape::kBytes];
+  auto tile_at = [&](int buffer, int which) __attribute__((always_inline)) { return lds + (2 * buffer + which) * Shape::kBytes; };
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+  // neighbouring heads, then stretches of time, then sequences: next to each other on one XCD
+  const uint32_t teams = a.group / a.heads_each;
+  uint32_t at = xcd_remap(blockIdx.x, gridDim.x);
+  const uint32_t head_team = at % (a.Hk * teams);
+  at /= a.Hk * teams;
+  const uint32_t block_t = at % a.blocks_t, b = at / a.blocks_t;
+  const uint32_t hk = head_team / teams, env = b / a.seqs_per_flag;
+  const uint32_t h = hk * a.group + head_team % teams * a.heads_each + wave % a.heads_each;
+  const int tiles_each = WAVES / a.heads_each, row0 = (int)block_t * tiles_each * kTile, my0 = row0 + (int)(wave / a.heads_each) * kTile;
+  Tiles tiles;
+  tiles.set(a, env, row0, tiles_each * kTile);
+  const Row row = row_of(a, my0 + lane % 32, env);
+  if constexpr (GRADIENT) {  // for dk and dv: where the episodes of each tile's rows began
+    if (h == 0 && b % a.seqs_per_flag == 0 && my0 < a.T) {
+      const int lo = wave_min(row.valid() ? row.start : 0x7fffffff), hi = wave_max(row.valid() ? row.start : -0x7fffffff);
+      if (lane == 0) a.reach[(int64_t)env * ((a.T + kTile - 1) / kTile) + my0 / kTile] = make_int2(lo, hi);
+    }
+  }
+  const char *kp = a.k.data + b * a.k.seq + hk * a.k.head, *vp = a.v.data + b * a.v.seq + hk * a.v.head;
+  const int64_t cached_at = ((int64_t)b * a.Hk + hk) * (a.sinks + a.window);
+  const char *ck = a.cache_k + cached_at * a.dk_dim * (int)sizeof(T), *cv = a.cache_v + cached_at * a.dv_dim * (int)sizeof(T);
+  typename P::Own q, d;
+  P::load_own(q, a.q.data + row.i * a.q.step + b * a.q.seq + h * a.q.head, a.dk_dim, row.valid(), a.flip);
+  float lse2 = 0.f, delta = 0.f;
+  const int64_t stat = ((int64_t)b * a.H + h) * a.T + row.i;
+  if constexpr (GRADIENT) {
+    P::load_own(d, a.dout.data + row.i * a.dout.step + b * a.dout.seq + h * a.dout.head, a.dv_dim, row.valid(), 0);
+    typename P::Own o;
+    P::load_own(o, a.out.data + row.i * a.out.step + b * a.out.seq + h * a.out.head, a.dv_dim, row.valid(), 0);
+    delta = P::dot(d, o);
+    delta += __shfl_xor(delta, 32);
+    if (half == 0 && row.i < a.T) a.delta[stat] = delta;
+    if (row.valid()) lse2 = a.lse[stat] * 1.44269504088896341f;
+  }
+  Fetch<T, DP, WAVES> fk, fv;
+  auto request = [&](const Tile& t) __attribute__((always_inline)) {
+    if (t.kind == TILE_CACHE) {
+      const int n = tiles.cached - t.at * kTile;
+      fk.request(ck + (int64_t)t.at * kTile * a.dk_dim * (int)sizeof(T), a.dk_dim * (int)sizeof(T), n, a.dk_dim);
+      fv.request(cv + (int64_t)t.at * kTile * a.dv_dim * (int)sizeof(T), a.dv_dim * (int)sizeof(T), n, a.dv_dim);
+    } else {
+      const int n = a.T - t.at * kTile;
+      fk.request(kp + (int64_t)t.at * kTile * a.k.step, a.k.step, n, a.dk_dim);
+      fv.request(vp + (int64_t)t.at * kTile * a.v.step, a.v.step, n, a.dv_dim);
+    }
+  };
+  f32x16_t acc[DP / 32];
+  float top = 0.f, sum = 0.f;  // output: the largest exponent (of two) so far, the sum of this half's weights
+  auto pass = [&](auto careful) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) acc[t] = (f32x16_t){0.f};
+    top = -__builtin_inff();
+    sum = 0.f;
+    Tile cur = tiles.next(a, {TILE_CACHE, -1});
+    if (cur.kind != TILE_NONE) request(cur);
+    for (int buffer = 0; cur.kind != TILE_NONE; buffer ^= 1) {
+      fk.store(tile_at(buffer, 0));
+      fv.store(tile_at(buffer, 1));
+      const Tile now = cur;
+      cur = tiles.next(a, cur);
+      if (cur.kind != TILE_NONE) request(cur);
+      __syncthreads();
+      // which of the tile's rows each lane's row sees: bit r for register r
+      const int j0 = now.at * kTile;
+      uint32_t seen = 0xffffu;
+      if (now.kind == TILE_CACHE) {
+        const bool goes_on = row.valid() && row.start < 0;
+        if (__ballot(goes_on) == 0) continue;
+        seen = 0;
+        const int first = j0 + 4 * fresh(half);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int slot = first + result_row(r, 0), step = tiles.step_of(a, slot);
+          if (goes_on && slot < tiles.cached && (slot < a.sinks || row.position - step < a.window)) seen |= 1u << r;
+        }
+      } else {
+        const int j1 = j0 + kTile - 1;
+        const bool whole = j0 >= row.lo && j1 <= row.i;
+        const bool some = row.valid() && (whole || (j1 >= row.lo && j0 <= row.i) || (row.start <= j1 && row.start + (int)row.n_sinks > j0));
+        if (__ballot(some) == 0) continue;
+        if (__ballot(!whole && row.valid()) != 0) {
+          seen = 0;
+          const int first = j0 + 4 * fresh(half);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) seen |= row.sees(first + result_row(r, 0)) ? 1u << r : 0u;
+        }
+      }
+      const bool masked = __ballot(seen != 0xffffu) != 0;
+      const f32x16_t s = P::score(tile_at(buffer, 0), q);
+      float p[16];
+      if constexpr (!GRADIENT) {
+        float most = -__builtin_inff();
+        if (masked) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) most = fmaxf(most, seen >> r & 1u ? s[r] : -__builtin_inff());
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) most = fmaxf(most, s[r]);
+        }
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const float now_top = fmaxf(top, most == -__builtin_inff() ? most : most * a.c), base = now_top == -__builtin_inff() ? 0.f : now_top;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c, -base));
+        if (masked) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) p[r] = seen >> r & 1u ? p[r] : 0.f;
+        }
+        if (__ballot(now_top != top) != 0) {
+          const float shrink = __builtin_amdgcn_exp2f(top - base);
+          sum *= shrink;
+#pragma unroll
+          for (int t = 0; t < DP / 32; ++t) acc[t] *= shrink;
+        }
+        top = now_top;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += p[r];
+      } else {
+        const f32x16_t e = P::score(tile_at(buffer, 1), d);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c, -lse2)) * (e[r] - delta);
+        if (masked) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) p[r] = seen >> r & 1u ? p[r] : 0.f;
+        }
+      }
+      const char* y = tile_at(buffer, GRADIENT ? 0 : 1);
+      if constexpr (!decltype(careful)::value) {
+        P::add(acc, y, p);
+      } else {
+        add_with_care<T, DP>(acc, y, p, seen);
+      }
+    }
+  };
+  pass(std::false_type());
+  if (__syncthreads_or(row.valid() && not_finite(acc))) pass(std::true_type());
+  __syncthreads();
+  const int count = a.T - my0;
+  char* place = lds + wave * Shape::kBytes;
+  if constexpr (!GRADIENT) {
+    sum += __shfl_xor(sum, 32);
+    if (half == 0 && a.lse != nullptr && row.i < a.T) a.lse[stat] = row.valid() ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : -__builtin_inff();
+    store_rows<T, DP>(place, acc, 1.f / sum, !row.valid(), a.out.data + my0 * a.out.step + b * a.out.seq + h * a.out.head, a.out.step, count, a.dv_dim);
+  } else {
+    store_rows<T, DP>(place, acc, a.scale, !row.valid(), a.dq.data + my0 * a.dq.step + b * a.dq.seq + h * a.dq.head, a.dq.step, count, a.dk_dim);
+  }
+}
+
+// ---- dk, dv ----------------------------------------------------------------------------------------------------------------------------
+// A workgroup: WAVES tiles of 32 keys of one key head; queries and their gradients are streamed, head after head of those that share the key head.
+template <class T, int DP, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, (columns_waves<T, DP>())) window_columns_kernel(const WindowArgs a) {
+  typedef Products<T, DP> P;
+  typedef TileShape<T, DP> Shape;
+  __shared__ __attribute__((aligned(16))) char lds[4 * Shape::kBytes];
+  __shared__ __attribute__((aligned(16))) float stats[2][2][kTile];  // lse (exponent of two), delta
+  __shared__ int4 sight[2][kTile];                                   // lo, span, start, first steps
+  auto tile_at = [&](int buffer, int which) __attribute__((always_inline)) { return lds + (2 * buffer + which) * Shape::kBytes; };
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+  uint32_t at = xcd_remap(blockIdx.x, gridDim.x);
+  const uint32_t hk = at % a.Hk;
+  at /= a.Hk;
+  const uint32_t block_t = at % a.blocks_t, b = at / a.blocks_t, env = b / a.seqs_per_flag;
+  const int col0 = (int)block_t * WAVES * kTile, col1 = min(col0 + WAVES * kTile, a.T) - 1, my0 = col0 + wave * kTile, my1 = min(my0 + kTile, a.T) - 1, j = my0 + lane % 32;
+  const int n_tiles = (a.T + kTile - 1) / kTile;
+  const int2* reach = a.reach + (int64_t)env * n_tiles;
+  typename P::Own k, v;
+  P::load_own(k, a.k.data + j * a.k.step + b * a.k.seq + hk * a.k.head, a.dk_dim, j < a.T, a.flip);
+  P::load_own(v, a.v.data + j * a.v.step + b * a.v.seq + hk * a.v.head, a.dv_dim, j < a.T, 0);
+  // The tiles of rows that see any of the workgroup's columns, 64 looked at at a time
+  struct Cursor {
+    int base;
+    uint64_t left;
+    int tile;
+    uint32_t g;
+  };
+  auto look = [&](int base) __attribute__((always_inline)) {
+    const int t = base + lane;
+    bool needed = false;
+    if (t < n_tiles) {
+      const int2 r = reach[t];
+      const int64_t last = (int64_t)col1 + a.window - 1;
+      needed = r.x <= col1 && ((int64_t)t * kTile <= last || (a.sinks > 0 && (int64_t)r.y + a.sinks > col0));
+    }
+    return (uint64_t)__ballot(needed);
+  };
+  auto next = [&](Cursor c) __attribute__((always_inline)) {
+    if (c.tile >= 0 && ++c.g < a.group) return c;
+    c.g = 0;
+    while (c.left == 0) {
+      c.base += 64;
+      if (c.base >= n_tiles) {
+        c.tile = -2;
+        return c;
+      }
+      c.left = look(c.base);
+    }
+    const int bit = __builtin_ctzll(c.left);
+    c.left &= c.left - 1;
+    c.tile = c.base + bit;
+    return c;
+  };
+  Fetch<T, DP, WAVES> fq, fd;
+  float lse2 = 0.f, delta = 0.f;
+  Row seer{};
+  auto request = [&](const Cursor& c) __attribute__((always_inline)) {
+    const uint32_t h = hk * a.group + c.g;
+    const int i0 = c.tile * kTile, n = a.T - i0;
+    fq.request(a.q.data + i0 * a.q.step + b * a.q.seq + h * a.q.head, a.q.step, n, a.dk_dim);
+    fd.request(a.dout.data + i0 * a.dout.step + b * a.dout.seq + h * a.dout.head, a.dout.step, n, a.dv_dim);
+    if (threadIdx.x < kTile) {
+      seer = row_of(a, i0 + threadIdx.x, env);
+      lse2 = delta = 0.f;
+      if (seer.valid()) {
+        const int64_t stat = ((int64_t)b * a.H + h) * a.T + seer.i;
+        lse2 = a.lse[stat] * 1.44269504088896341f;
+        delta = a.delta[stat];
+      }
+    }
+  };
+  f32x16_t dk[DP / 32], dv[DP / 32];
+  auto pass = [&](auto careful) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) dk[t] = dv[t] = (f32x16_t){0.f};
+    const int base = col0 / kTile;
+    Cursor cur = next({base, look(base), -1, 0});
+    if (cur.tile >= 0) request(cur);
+    for (int buffer = 0; cur.tile >= 0; buffer ^= 1) {
+      fq.store(tile_at(buffer, 0));
+      fd.store(tile_at(buffer, 1));
+      if (threadIdx.x < kTile) {
+        stats[buffer][0][threadIdx.x] = lse2;
+        stats[buffer][1][threadIdx.x] = delta;
+        sight[buffer][threadIdx.x] = make_int4(seer.lo, (int)seer.span, seer.start, (int)seer.n_sinks);
+      }
+      cur = next(cur);
+      if (cur.tile >= 0) request(cur);
+      __syncthreads();
+      auto sees = [&](const int4& w, int col) __attribute__((always_inline)) { return (uint32_t)(col - w.x) <= (uint32_t)w.y || (uint32_t)(col - w.z) < (uint32_t)w.w; };
+      uint32_t seen = 0xffffu;
+      {
+        // a row's last step is lo + span; rows that hold no step see nothing (lo above every column)
+        const int4 w = sight[buffer][lane % 32];
+        const int i = w.x == 0x7fffffff ? -1 : w.x + w.y;
+        const bool whole = w.x <= my0 && my1 <= i;
+        const bool some = whole || (w.x <= my1 && my0 <= i) || ((int64_t)w.z + w.w > my0 && w.z <= my1);
+        if (my0 >= a.T || __ballot(some) == 0) continue;
+        if (__ballot(!whole) != 0) {
+          seen = 0;
+          const int4* from = sight[buffer] + 4 * fresh(half);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            seen |= sees(from[result_row(r, 0)], j) ? 1u << r : 0u;
+            if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+      const bool masked = __ballot(seen != 0xffffu) != 0;
+      const f32x16_t s = P::score(tile_at(buffer, 0), k), e = P::score(tile_at(buffer, 1), v);
+      float p[16], ds[16];
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const float4 l = *reinterpret_cast<const float4*>(&stats[buffer][0][result_row(r, half)]);
+        const float4 m = *reinterpret_cast<const float4*>(&stats[buffer][1][result_row(r, half)]);
+        const float ls[4] = {l.x, l.y, l.z, l.w}, ms[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          p[r + u] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + u], a.c, -ls[u]));
+          ds[r + u] = p[r + u] * (e[r + u] - ms[u]);
+        }
+      }
+      if (masked) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          p[r] = seen >> r & 1u ? p[r] : 0.f;
+          ds[r] = seen >> r & 1u ? ds[r] : 0.f;
+        }
+      }
+      if constexpr (!decltype(careful)::value) {
+        P::add(dv, tile_at(buffer, 1), p);
+        P::add(dk, tile_at(buffer, 0), ds);
+      } else {
+        add_with_care<T, DP>(dv, tile_at(buffer, 1), p, seen);
+        add_with_care<T, DP>(dk, tile_at(buffer, 0), ds, seen);
+      }
+    }
+  };
+  pass(std::false_type());
+  if (__syncthreads_or(j < a.T && (not_finite(dk) || not_finite(dv)))) pass(std::true_type());
+  __syncthreads();
+  char* place = lds + wave * Shape::kBytes;
+  if (my0 < a.T) {
+    store_rows<T, DP>(place, dk, a.scale, false, a.dk.data + my0 * a.dk.step + b * a.dk.seq + hk * a.dk.head, a.dk.step, a.T - my0, a.dk_dim);
+    store_rows<T, DP>(place, dv, 1.f, false, a.dv.data + my0 * a.dv.step + b * a.dv.seq + hk * a.dv.head, a.dv.step, a.T - my0, a.dv_dim);
+  }
+}
+
+// The wavefronts that fetch a tile, at the least: a wavefront that fetches one of wide fp32 heads alone holds 128 registers of it and spills.
+constexpr int least_waves(size_t elem, int dim) { return elem == 4 && dim > 64 ? 4 : 1; }
+
+// ---- launches --------------------------------------------------------------------------------------------------------------------------
+enum { WINDOW_OUTPUT, WINDOW_DQ, WINDOW_DKV };
+
+template <class T, int DP, int WAVES>
+void launch_window(const WindowArgs& a, int pass, unsigned blocks, hipStream_t s) {
+  if (pass == WINDOW_OUTPUT) hipLaunchKernelGGL((window_rows_kernel<T, DP, WAVES, false>), dim3(blocks), dim3(64 * WAVES), 0, s, a);
+  if (pass == WINDOW_DQ) hipLaunchKernelGGL((window_rows_kernel<T, DP, WAVES, true>), dim3(blocks), dim3(64 * WAVES), 0, s, a);
+  if (pass == WINDOW_DKV) hipLaunchKernelGGL((window_columns_kernel<T, DP, WAVES>), dim3(blocks), dim3(64 * WAVES), 0, s, a);
+}
+template <class T, int DP>
+void launch_window(const WindowArgs& a, int pass, int waves, unsigned blocks, hipStream_t s) {
+  if constexpr (least_waves(sizeof(T), DP) <= 1) {
+    if (waves == 1) return launch_window<T, DP, 1>(a, pass, blocks, s);
+  }
+  if constexpr (least_waves(sizeof(T), DP) <= 2) {
+    if (waves == 2) return launch_window<T, DP, 2>(a, pass, blocks, s);
+  }
+  launch_window<T, DP, 4>(a, pass, blocks, s);
+}
+// Heads as wide as the wider of keys and values, in steps of 32
+template <class T>
+void launch_window(const WindowArgs& a, int pass, int waves, unsigned blocks, hipStream_t s) {
+  const int d = a.dk_dim > a.dv_dim ? a.dk_dim : a.dv_dim;
+  if (d <= 32) launch_window<T, 32>(a, pass, waves, blocks, s);
+  else if (d <= 64) launch_window<T, 64>(a, pass, waves, blocks, s);
+  else if (d <= 96) launch_window<T, 96>(a, pass, waves, blocks, s);
+  else launch_window<T, 128>(a, pass, waves, blocks, s);
+}
+void launch_window_f32(const WindowArgs& a, int pass, int waves, unsigned blocks, hipStream_t s);
+void launch_window_bf16(const WindowArgs& a, int pass, int waves, unsigned blocks, hipStream_t s);
+
+}  // namespace marl

@@ -1,0 +1,631 @@
+// Window attention: the calls, the cache behind a call, the single step on a cache.
+#include <type_traits>
+
+#include "attention_checks.h"
+#include "window_attention.h"
+
+namespace marl {
+namespace {
+
+// ---- how a call is laid out ----------------------------------------------------------------------------------------------------
+struct Plan {
+  int tiles;                  // of 32 steps
+  int heads_each, rows_waves; // query heads of a workgroup, its wavefronts
+  int cols_waves;
+  int64_t rows_t, cols_t;     // workgroups along time
+  int64_t rows, cols;         // workgroups
+  int64_t delta, reach, bytes;
+};
+// A workgroup's wavefronts share the streamed tiles: query heads of one key head first, then tiles next to each other in time.
+Plan plan_of(const marl_attention_dims& d) {
+  Plan p{};
+  p.tiles = (int)(((int64_t)d.n_steps + kTile - 1) / kTile);
+  const int group = d.n_heads / d.n_kv_heads;
+  p.heads_each = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
+  p.cols_waves = p.tiles < 2 ? 1 : p.tiles == 2 ? 2 : 4;
+  const int least = least_waves(d.precision == 0 ? 4 : 2, d.dim_k > d.dim_v ? d.dim_k : d.dim_v);
+  if (p.cols_waves < least) p.cols_waves = least;
+  p.rows_waves = p.heads_each * p.cols_waves < 4 ? p.heads_each * p.cols_waves : 4;
+  const int each = p.rows_waves / p.heads_each;
+  p.rows_t = (p.tiles + each - 1) / each;
+  p.cols_t = (p.tiles + p.cols_waves - 1) / p.cols_waves;
+  p.rows = (int64_t)d.n_seqs * (d.n_heads / p.heads_each) * p.rows_t;
+  p.cols = (int64_t)d.n_seqs * d.n_kv_heads * p.cols_t;
+  auto take = [&](int64_t bytes) {
+    const int64_t here = p.bytes;
+    p.bytes += (bytes + 255) / 256 * 256;
+    return here;
+  };
+  p.delta = take((int64_t)d.n_seqs * d.n_heads * d.n_steps * 4);
+  p.reach = take((int64_t)(d.n_seqs / d.seqs_per_flag) * p.tiles * 8);
+  return p;
+}
+
+// ---- the cache behind a call ---------------------------------------------------------------------------------------------------------
+// A row of the next cache comes from the call's steps or, where its step is older, from the cache before.  Bound by memory.
+struct CacheArgs {
+  WindowArray in[2];  // k, v
+  const char* old[2];
+  char* next[2];
+  const int32_t* positions;
+  int32_t first;
+  uint32_t n_flags, seqs_per_flag, Hk;
+  int32_t T, dim[2], window, sinks;
+  uint32_t chunks;  // of kCacheRows slots
+  int32_t in_place;
+};
+constexpr int kCacheRows = 64;
+
+template <class T>
+__device__ __forceinline__ void put_unit(T* p, const uint4& u, int left) {  // `left` elements, at most 16 bytes
+  constexpr int E = 16 / sizeof(T);
+  if (left >= E) {
+    __builtin_memcpy(p, &u, 16);
+  } else {
+    T e[E];
+    __builtin_memcpy(e, &u, 16);
+#pragma unroll
+    for (int x = 0; x < E; ++x)
+      if (x < left) p[x] = e[x];
+  }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) window_cache_kernel(const CacheArgs a) {
+  constexpr int E = 16 / sizeof(T);
+  uint32_t at = xcd_remap(blockIdx.x, gridDim.x);
+  const uint32_t chunk = at % a.chunks;
+  at /= a.chunks;
+  const uint32_t hk = at % a.Hk, b = at / a.Hk, env = b / a.seqs_per_flag;
+  // the last row that holds a step
+  int last = -1, newest = -1;
+  for (int t0 = a.T - 1; t0 >= 0 && last < 0; t0 -= 64) {
+    const int t = t0 - (int)(threadIdx.x & 63);
+    const int p = t < 0 ? -1 : a.positions != nullptr ? a.positions[(int64_t)t * a.n_flags + env] : a.first + t;
+    const uint64_t on = __ballot(p >= 0);
+    if (on != 0) {
+      const int lane = __builtin_ctzll(on);
+      last = t0 - lane;
+      newest = __shfl(p, lane);
+    }
+  }
+  const int slots = a.sinks + a.window;
+  const int newest_slot = newest < a.sinks ? newest : a.sinks + (newest - a.sinks) % a.window;
+  const int units[2] = {(a.dim[0] + E - 1) / E, (a.dim[1] + E - 1) / E}, per = units[0] + units[1];
+  const int64_t base = ((int64_t)b * a.Hk + hk) * slots;
+  const int slot0 = (int)chunk * kCacheRows, n = min(kCacheRows, slots - slot0);
+  for (int u = threadIdx.x; u < n * per; u += 256) {
+    const int slot = slot0 + u / per, x = u % per, which = x >= units[0], c = (which ? x - units[0] : x) * E;
+    bool fresh_row = false;
+    int64_t t = -1;
+    if (last >= 0) {
+      if (slot > newest && newest < slots) continue;  // holds no step
+      const int step = newest < slots || slot < a.sinks ? slot : newest - newest_slot + slot - (slot <= newest_slot ? 0 : a.window);
+      t = (int64_t)last - ((int64_t)newest - step);
+      fresh_row = t >= 0;
+    }
+    const int dim = which ? a.dim[1] : a.dim[0];
+    const WindowArray& in = which ? a.in[1] : a.in[0];
+    const char* old = which ? a.old[1] : a.old[0];
+    const int64_t place = (base + slot) * dim;
+    uint4 v;
+    if (fresh_row) {
+      v = load_unit<T>(in.data + t * in.step + b * in.seq + hk * in.head, c, dim);
+    } else {
+      if (old == nullptr || a.in_place) continue;
+      v = load_unit<T>(old + place * (int)sizeof(T), c, dim);
+    }
+    put_unit(reinterpret_cast<T*>(which ? a.next[1] : a.next[0]) + place + c, v, dim - c);
+  }
+}
+
+// ---- one step ------------------------------------------------------------------------------------------------------------------------
+// A wavefront takes up to G query heads of one key head of one sequence, over a part of the cache's slots: L lanes hold a row of keys and the
+// same row of values, 64 / L rows at a time, and a softmax of their own, joined at the end.  All slots that hold a step are seen, so nothing is masked.  Bound by
+// memory: the cache is read once for all heads that share it.
+struct StepArgs {
+  const char *q, *k, *v;
+  char* out;
+  int64_t q_seq, q_head, k_seq, k_head, v_seq, v_head, out_seq, out_head;  // bytes
+  char *cache_k, *cache_v;
+  const int32_t* positions;
+  uint32_t seqs_per_flag, H, Hk, group, chunks, splits;
+  int64_t units;  // wavefronts
+  int32_t dk, dv, window, sinks;
+  float c;  // scale log2(e)
+  float* part;   // [B][H][splits][dv]
+  float2* stat;  // [B][H][splits]: largest exponent of two, sum
+};
+
+// Sum over L lanes next to each other, in all of them
+template <int L>
+__device__ __forceinline__ float sum_lanes(float v) {
+  auto add = [&](auto control) { v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(control)::value, 0xf, 0xf, true)); };
+  if constexpr (L >= 2) add(std::integral_constant<int, 0xB1>());   // the neighbour
+  if constexpr (L >= 4) add(std::integral_constant<int, 0x4E>());   // the other pair
+  if constexpr (L >= 8) add(std::integral_constant<int, 0x141>());  // mirrored in eight
+  if constexpr (L >= 16) add(std::integral_constant<int, 0x140>()); // mirrored in sixteen
+  if constexpr (L >= 32) v += __shfl_xor(v, 16);
+  return v;
+}
+template <class T>
+__device__ __forceinline__ void widen(const uint4& u, float (&f)[16 / sizeof(T)]) {
+  if constexpr (sizeof(T) == 4) {
+    f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
+  } else {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+}
+template <class T>
+__device__ __forceinline__ uint4 narrow(const float (&f)[16 / sizeof(T)]) {
+  if constexpr (sizeof(T) == 4) return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  else return make_uint4(pack2_bf16(f[0], f[1]), pack2_bf16(f[2], f[3]), pack2_bf16(f[4], f[5]), pack2_bf16(f[6], f[7]));
+}
+
+constexpr int kStepRows = 4;  // rows of a lane on their way together
+
+template <class T, int L, int G>
+__global__ void __launch_bounds__(256) window_step_kernel(const StepArgs a) {
+  constexpr int E = 16 / sizeof(T), R = 64 / L;
+  const int64_t unit = (int64_t)xcd_remap(blockIdx.x, gridDim.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  if (unit >= a.units) return;
+  const int lane = threadIdx.x & 63, r = lane / L, c = lane % L * E;
+  const uint32_t split = (uint32_t)(unit % a.splits);
+  const int64_t rest = unit / a.splits;
+  const uint32_t chunk = (uint32_t)(rest % a.chunks);
+  const int64_t pair = rest / a.chunks;  // sequence and key head
+  const uint32_t b = (uint32_t)(pair / a.Hk), hk = (uint32_t)(pair % a.Hk);
+  const uint32_t h0 = hk * a.group + chunk * G, heads = min((uint32_t)G, a.group - chunk * G);
+  const int position = a.positions[b / a.seqs_per_flag];
+  const int slots = a.sinks + a.window;
+  float q[G][E], acc[G][E], top[G], sum[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const uint4 u = load_unit<T>(a.q + b * a.q_seq + (h0 + min((uint32_t)g, heads - 1)) * a.q_head, c, a.dk);
+    widen<T>(u, q[g]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      q[g][e] *= a.c;
+      acc[g][e] = 0.f;
+    }
+    top[g] = -__builtin_inff();
+    sum[g] = 0.f;
+  }
+  if (position >= 0) {
+    const int n = min(position, slots - 1) + 1, per = ((n - 1) / (int)a.splits / R + 1) * R;  // (a multiple of R that is no less than n / splits)
+    const int64_t begin = (int64_t)split * per;
+    const int end = (int)min((int64_t)n, begin + per);
+    const int here = position < a.sinks ? position : a.sinks + (position - a.sinks) % a.window;  // this step's slot
+    char *ck = a.cache_k + pair * slots * a.dk * (int64_t)sizeof(T), *cv = a.cache_v + pair * slots * a.dv * (int64_t)sizeof(T);
+    const char *kp = a.k + b * a.k_seq + hk * a.k_head, *vp = a.v + b * a.v_seq + hk * a.v_head;
+    for (int64_t base = begin; base < end; base += R * kStepRows) {
+      uint4 k[kStepRows], v[kStepRows];
+#pragma unroll
+      for (int u = 0; u < kStepRows; ++u) {
+        const int64_t slot = base + u * R + r;
+        k[u] = v[u] = make_uint4(0, 0, 0, 0);
+        if (slot < end) {
+          k[u] = load_unit<T>(slot == here ? kp : ck + slot * a.dk * (int)sizeof(T), c, a.dk);
+          v[u] = load_unit<T>(slot == here ? vp : cv + slot * a.dv * (int)sizeof(T), c, a.dv);
+        }
+      }
+      float s[G][kStepRows];
+#pragma unroll
+      for (int u = 0; u < kStepRows; ++u) {
+        const int64_t slot = base + u * R + r;
+        if (slot == here && slot < end && chunk == 0) {
+          if (c < a.dk) put_unit(reinterpret_cast<T*>(ck) + slot * a.dk + c, k[u], a.dk - c);
+          if (c < a.dv) put_unit(reinterpret_cast<T*>(cv) + slot * a.dv + c, v[u], a.dv - c);
+        }
+        float f[E];
+        widen<T>(k[u], f);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          float x = 0.f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) x = __builtin_fmaf(q[g][e], f[e], x);
+          x = sum_lanes<L>(x);
+          s[g][u] = slot < end ? x : -__builtin_inff();
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        float now = top[g];
+#pragma unroll
+        for (int u = 0; u < kStepRows; ++u) now = fmaxf(now, s[g][u]);
+        const float from = now == -__builtin_inff() ? 0.f : now, shrink = __builtin_amdgcn_exp2f(top[g] - from);
+        top[g] = now;
+        sum[g] *= shrink;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[g][e] *= shrink;
+#pragma unroll
+        for (int u = 0; u < kStepRows; ++u) {
+          s[g][u] = base + u * R + r < end ? __builtin_amdgcn_exp2f(s[g][u] - from) : 0.f;
+          sum[g] += s[g][u];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kStepRows; ++u) {
+        float f[E];
+        widen<T>(v[u], f);
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[g][e] = __builtin_fmaf(s[g][u], f[e], acc[g][e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    float most = top[g];
+#pragma unroll
+    for (int m = L; m < 64; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+    const float factor = __builtin_amdgcn_exp2f(top[g] - (most == -__builtin_inff() ? 0.f : most));
+    sum[g] *= factor;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[g][e] *= factor;
+#pragma unroll
+    for (int m = L; m < 64; m *= 2) {
+      sum[g] += __shfl_xor(sum[g], m);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[g][e] += __shfl_xor(acc[g][e], m);
+    }
+    if (r != 0 || (uint32_t)g >= heads) continue;
+    const uint32_t h = h0 + g;
+    if (a.splits == 1) {
+      if (c >= a.dv) continue;
+      float o[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = position < 0 ? 0.f : acc[g][e] / sum[g];
+      put_unit(reinterpret_cast<T*>(a.out + b * a.out_seq + h * a.out_head) + c, narrow<T>(o), a.dv - c);
+    } else {
+      const int64_t at = ((int64_t)b * a.H + h) * a.splits + split;
+      if (lane == 0) a.stat[at] = make_float2(most, sum[g]);
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (c + e < a.dv) a.part[at * a.dv + c + e] = acc[g][e];
+    }
+  }
+}
+
+// The parts of a cut step, one workgroup a query head, in a fixed order
+template <class T>
+__global__ void __launch_bounds__(128) window_step_join_kernel(const StepArgs a) {
+  const int64_t pair = blockIdx.x;
+  const uint32_t b = (uint32_t)(pair / a.H), h = (uint32_t)(pair % a.H);
+  const int d = threadIdx.x;
+  const int position = a.positions[b / a.seqs_per_flag];
+  const float2* stat = a.stat + pair * a.splits;
+  float top = -__builtin_inff();
+  for (uint32_t s = 0; s < a.splits; ++s) top = fmaxf(top, stat[s].x);
+  const float from = top == -__builtin_inff() ? 0.f : top;
+  if (d >= a.dv) return;
+  float sum = 0.f, acc = 0.f;
+#pragma unroll 8
+  for (uint32_t s = 0; s < a.splits; ++s) {
+    const float2 x = stat[s];
+    const float factor = __builtin_amdgcn_exp2f(x.x - from);
+    sum += factor * x.y;
+    acc += factor * a.part[(pair * a.splits + s) * a.dv + d];
+  }
+  const float o = position < 0 ? 0.f : acc / sum;
+  T* out = reinterpret_cast<T*>(a.out + b * a.out_seq + h * a.out_head) + d;
+  if constexpr (sizeof(T) == 4) *out = o;
+  else *out = to_bf16(o);
+}
+
+struct StepPlan {
+  int lanes, heads;  // of a row; of a wavefront
+  uint32_t chunks, splits;
+  int64_t units, part, stat, bytes;
+};
+// The slots are cut into parts while the wavefronts would not fill the chip, each of them two rounds of loads at least.
+StepPlan step_plan(const marl_attention_dims& d, int window, int sinks) {
+  constexpr int64_t kWaves = 2048;
+  StepPlan p{};
+  const int elements = d.precision == 0 ? 4 : 8, dim = d.dim_k > d.dim_v ? d.dim_k : d.dim_v, group = d.n_heads / d.n_kv_heads;
+  p.lanes = 4;
+  while (p.lanes * elements < dim) p.lanes *= 2;
+  p.heads = group == 1 ? 1 : group == 2 ? 2 : 4;
+  p.chunks = (uint32_t)((group + p.heads - 1) / p.heads);
+  const int64_t whole = (int64_t)d.n_seqs * d.n_kv_heads * p.chunks, slots = (int64_t)window + sinks, least = 64 / p.lanes * kStepRows * 2;
+  int64_t n = whole > 0 ? kWaves / whole : 1;
+  n = n < slots / least ? n : slots / least;
+  p.splits = (uint32_t)(n < 2 ? 1 : n);
+  p.units = whole * p.splits;
+  auto take = [&](int64_t bytes) {
+    const int64_t here = p.bytes;
+    p.bytes += (bytes + 255) / 256 * 256;
+    return here;
+  };
+  if (p.splits > 1) {
+    const int64_t parts = (int64_t)d.n_seqs * d.n_heads * p.splits;
+    p.part = take(parts * d.dim_v * 4);
+    p.stat = take(parts * 8);
+  }
+  return p;
+}
+
+template <class T>
+int32_t launch_step(const StepArgs& a, const StepPlan& p, int64_t pairs, hipStream_t s) {
+  const dim3 grid((unsigned)((p.units + 3) / 4)), block(256);
+#define MARL_STEP(L, G) hipLaunchKernelGGL((window_step_kernel<T, L, G>), grid, block, 0, s, a)
+#define MARL_STEP_HEADS(L)               \
+  do {                                   \
+    if (p.heads == 1) MARL_STEP(L, 1);   \
+    else if (p.heads == 2) MARL_STEP(L, 2); \
+    else MARL_STEP(L, 4);                \
+  } while (0)
+  if (p.lanes == 4) MARL_STEP_HEADS(4);
+  else if (p.lanes == 8) MARL_STEP_HEADS(8);
+  else if (p.lanes == 16) MARL_STEP_HEADS(16);
+  else if constexpr (sizeof(T) == 4) MARL_STEP_HEADS(32);
+#undef MARL_STEP_HEADS
+#undef MARL_STEP
+  if (p.splits > 1) hipLaunchKernelGGL((window_step_join_kernel<T>), dim3((unsigned)pairs), dim3(128), 0, s, a);
+  return launch_status();
+}
+
+// ---- checks ----------------------------------------------------------------------------------------------------------------------
+int32_t check_window(const marl_attention_dims* d, int32_t window, int32_t sinks) {
+  MARL_CHECK(check_dims(d));
+  if (window < 1 || sinks < 0 || (int64_t)window + sinks > ((int64_t)1 << 30)) return MARL_E_CONFIG;
+  if ((int64_t)d->n_seqs * d->n_kv_heads > ((int64_t)1 << 48) / (window + sinks)) return MARL_E_SIZE;  // (caches of 64-bit sizes)
+  return MARL_OK;
+}
+int32_t check_positions(const marl_attention_dims& d, const int32_t* positions, int32_t first) {
+  if ((reinterpret_cast<uintptr_t>(positions) & 3u) != 0) return MARL_E_ALIGN;
+  if (positions == nullptr && (int64_t)first + d.n_steps > 0x7fffffff) return MARL_E_SIZE;
+  return MARL_OK;
+}
+struct Extent {
+  uintptr_t from, bytes;
+  bool holds(const void* p) const { return bytes > 0 && reinterpret_cast<uintptr_t>(p) - from < bytes; }
+  bool meets(const Extent& o) const { return bytes > 0 && o.bytes > 0 && (from < o.from ? o.from - from < bytes : from - o.from < o.bytes); }
+};
+Extent cached(const marl_attention_dims& d, const void* p, int64_t slots, int dim) {
+  return {reinterpret_cast<uintptr_t>(p), p == nullptr ? 0 : (uintptr_t)((int64_t)d.n_seqs * d.n_kv_heads * slots * dim * (d.precision == 0 ? 4 : 2))};
+}
+// Both arrays or neither, aligned
+int32_t check_cache(const marl_window_cache& c, bool needed) {
+  if ((c.keys == nullptr) != (c.values == nullptr) || (needed && c.keys == nullptr)) return MARL_E_NULL;
+  return misaligned(c.keys) || misaligned(c.values) ? MARL_E_ALIGN : MARL_OK;
+}
+int32_t check_floats(const float* p, bool needed) {
+  if (p == nullptr) return needed ? MARL_E_NULL : MARL_OK;
+  return (reinterpret_cast<uintptr_t>(p) & 3u) != 0 ? MARL_E_ALIGN : MARL_OK;
+}
+
+WindowArray array_of(const marl_view& v, int elem) { return {static_cast<char*>(v.data), v.step * elem, v.seq * elem, v.head * elem}; }
+
+WindowArgs args_of(const marl_attention_dims& d, int32_t window, int32_t sinks, const int32_t* positions, int32_t first, const marl_window_cache& cache) {
+  WindowArgs a{};
+  a.cache_k = static_cast<const char*>(cache.keys);
+  a.cache_v = static_cast<const char*>(cache.values);
+  a.positions = positions;
+  a.first = first;
+  a.n_flags = (uint32_t)(d.n_seqs / d.seqs_per_flag);
+  a.seqs_per_flag = (uint32_t)d.seqs_per_flag;
+  a.T = d.n_steps;
+  a.B = (uint32_t)d.n_seqs;
+  a.H = (uint32_t)d.n_heads;
+  a.Hk = (uint32_t)d.n_kv_heads;
+  a.group = a.H / a.Hk;
+  a.dk_dim = d.dim_k;
+  a.dv_dim = d.dim_v;
+  a.window = window;
+  a.sinks = sinks;
+  a.scale = d.scale;
+  a.c = __builtin_fabsf(d.scale) * 1.44269504088896341f;
+  a.flip = d.scale < 0.f ? (d.precision == 0 ? 0x80000000u : 0x80008000u) : 0u;
+  return a;
+}
+int32_t launch(WindowArgs& a, const marl_attention_dims& d, const Plan& p, int pass, hipStream_t s) {
+  const bool cols = pass == WINDOW_DKV;
+  a.heads_each = (uint32_t)p.heads_each;
+  a.blocks_t = (uint32_t)(cols ? p.cols_t : p.rows_t);
+  (d.precision == 0 ? launch_window_f32 : launch_window_bf16)(a, pass, cols ? p.cols_waves : p.rows_waves, (unsigned)(cols ? p.cols : p.rows), s);
+  return launch_status();
+}
+int64_t cache_blocks(const marl_attention_dims& d, int64_t slots) { return (int64_t)d.n_seqs * d.n_kv_heads * ((slots + kCacheRows - 1) / kCacheRows); }
+
+enum { CALL_FORWARD, CALL_BACKWARD, CALL_STEP };
+// Every launch of a call within what a grid can be, before the first of them
+int32_t check_launches(const marl_attention_dims& d, int32_t window, int32_t sinks, int call, bool next_cache) {
+  bool fits = true;
+  if (call == CALL_STEP) {
+    const StepPlan p = step_plan(d, window, sinks);
+    fits = launchable((p.units + 3) / 4, 256) && (p.splits == 1 || launchable((int64_t)d.n_seqs * d.n_heads, 128));
+  } else {
+    const Plan p = plan_of(d);
+    fits = launchable(p.rows, 64 * p.rows_waves) && (call == CALL_FORWARD || launchable(p.cols, 64 * p.cols_waves));
+    if (next_cache) fits = fits && launchable(cache_blocks(d, (int64_t)window + sinks), 256);
+  }
+  return fits ? MARL_OK : MARL_E_SIZE;
+}
+
+}  // namespace
+}  // namespace marl
+
+using namespace marl;
+
+extern "C" {
+
+int32_t marl_window_attention_workspace(const marl_attention_dims* dims, int32_t window, int32_t sinks, int32_t call, int64_t* bytes) {
+  MARL_CHECK(check_window(dims, window, sinks));
+  if (call < CALL_FORWARD || call > CALL_STEP) return MARL_E_CONFIG;
+  if (bytes == nullptr) return MARL_E_NULL;
+  MARL_CHECK(check_launches(*dims, window, sinks, call, false));
+  *bytes = call == CALL_FORWARD ? 0 : call == CALL_BACKWARD ? plan_of(*dims).bytes : step_plan(*dims, window, sinks).bytes;
+  return MARL_OK;
+}
+
+int32_t marl_window_attention(const marl_attention_dims* dims, int32_t window, int32_t sinks, marl_view q, marl_view k, marl_view v,
+                              const int32_t* positions, int32_t first_position, marl_window_cache cache, marl_view out, float* lse,
+                              marl_window_cache next_cache, void* workspace, void* stream) {
+  (void)workspace;  // (of no bytes)
+  MARL_CHECK(check_window(dims, window, sinks));
+  const marl_attention_dims& d = *dims;
+  MARL_CHECK(check_launches(d, window, sinks, CALL_FORWARD, next_cache.keys != nullptr));
+  const bool used = d.n_steps > 0 && d.n_seqs > 0;
+  for (const marl_view& x : {q, k, v, out}) MARL_CHECK(check_view(x, d.precision, used));
+  MARL_CHECK(check_output(out, d, d.n_heads, used));
+  MARL_CHECK(check_positions(d, positions, first_position));
+  MARL_CHECK(check_floats(lse, false));
+  MARL_CHECK(check_cache(cache, false));
+  MARL_CHECK(check_cache(next_cache, false));
+  MARL_CHECK(check_places(out, {q, k, v}, used));
+  const int64_t slots = (int64_t)window + sinks;
+  const Extent ck = cached(d, cache.keys, slots, d.dim_k), cv = cached(d, cache.values, slots, d.dim_v), nk = cached(d, next_cache.keys, slots, d.dim_k),
+               nv = cached(d, next_cache.values, slots, d.dim_v);
+  const bool in_place = next_cache.keys != nullptr && next_cache.keys == cache.keys && next_cache.values == cache.values;
+  if (nk.meets(nv) || nk.meets(cv) || nv.meets(ck) || (!in_place && (nk.meets(ck) || nv.meets(cv)))) return MARL_E_CONFIG;
+  if (used) {
+    if (ck.holds(out.data) || cv.holds(out.data) || ck.holds(lse) || cv.holds(lse)) return MARL_E_CONFIG;
+    for (const void* x : {q.data, k.data, v.data, out.data, (void*)lse})
+      if (nk.holds(x) || nv.holds(x)) return MARL_E_CONFIG;
+    for (const void* x : {q.data, k.data, v.data, out.data, (void*)positions})
+      if (lse != nullptr && x == lse) return MARL_E_CONFIG;
+  }
+  if (d.n_seqs == 0) return MARL_OK;
+  hipStream_t s = (hipStream_t)stream;
+  const int elem = d.precision == 0 ? 4 : 2;
+  if (d.n_steps > 0) {
+    WindowArgs a = args_of(d, window, sinks, positions, first_position, cache);
+    a.q = array_of(q, elem);
+    a.k = array_of(k, elem);
+    a.v = array_of(v, elem);
+    a.out = array_of(out, elem);
+    a.lse = lse;
+    MARL_CHECK(launch(a, d, plan_of(d), WINDOW_OUTPUT, s));
+  }
+  if (next_cache.keys == nullptr) return MARL_OK;
+  CacheArgs c{};
+  c.in[0] = array_of(k, elem);
+  c.in[1] = array_of(v, elem);
+  c.old[0] = static_cast<const char*>(cache.keys);
+  c.old[1] = static_cast<const char*>(cache.values);
+  c.next[0] = static_cast<char*>(next_cache.keys);
+  c.next[1] = static_cast<char*>(next_cache.values);
+  c.positions = positions;
+  c.first = first_position;
+  c.n_flags = (uint32_t)(d.n_seqs / d.seqs_per_flag);
+  c.seqs_per_flag = (uint32_t)d.seqs_per_flag;
+  c.Hk = (uint32_t)d.n_kv_heads;
+  c.T = d.n_steps;
+  c.dim[0] = d.dim_k;
+  c.dim[1] = d.dim_v;
+  c.window = window;
+  c.sinks = sinks;
+  c.chunks = (uint32_t)((slots + kCacheRows - 1) / kCacheRows);
+  c.in_place = in_place;
+  const unsigned blocks = (unsigned)cache_blocks(d, slots);
+  if (d.precision == 0) hipLaunchKernelGGL((window_cache_kernel<float>), dim3(blocks), dim3(256), 0, s, c);
+  else hipLaunchKernelGGL((window_cache_kernel<bf16_t>), dim3(blocks), dim3(256), 0, s, c);
+  return launch_status();
+}
+
+int32_t marl_window_attention_backward(const marl_attention_dims* dims, int32_t window, int32_t sinks, marl_view q, marl_view k, marl_view v,
+                                       const int32_t* positions, int32_t first_position, marl_window_cache cache, marl_view out,
+                                       const float* lse, marl_view dout, marl_view dq, marl_view dk, marl_view dv, void* workspace,
+                                       void* stream) {
+  MARL_CHECK(check_window(dims, window, sinks));
+  const marl_attention_dims& d = *dims;
+  MARL_CHECK(check_launches(d, window, sinks, CALL_BACKWARD, false));
+  const bool used = d.n_steps > 0 && d.n_seqs > 0;
+  for (const marl_view& x : {q, k, v, out, dout, dq, dk, dv}) MARL_CHECK(check_view(x, d.precision, used));
+  MARL_CHECK(check_output(dq, d, d.n_heads, used));
+  MARL_CHECK(check_output(dk, d, d.n_kv_heads, used));
+  MARL_CHECK(check_output(dv, d, d.n_kv_heads, used));
+  MARL_CHECK(check_positions(d, positions, first_position));
+  MARL_CHECK(check_floats(lse, used));
+  MARL_CHECK(check_cache(cache, false));
+  if (used) MARL_REQUIRE_PTR(workspace);
+  MARL_CHECK(check_places(dq, {q, k, v, out, dout, dk, dv}, used));
+  MARL_CHECK(check_places(dk, {q, k, v, out, dout, dv}, used));
+  MARL_CHECK(check_places(dv, {q, k, v, out, dout}, used));
+  if (!used) return MARL_OK;
+  const int64_t slots = (int64_t)window + sinks;
+  const Extent ck = cached(d, cache.keys, slots, d.dim_k), cv = cached(d, cache.values, slots, d.dim_v);
+  for (const void* x : {dq.data, dk.data, dv.data})
+    if (ck.holds(x) || cv.holds(x) || x == lse || x == positions) return MARL_E_CONFIG;
+  hipStream_t s = (hipStream_t)stream;
+  const int elem = d.precision == 0 ? 4 : 2;
+  const Plan p = plan_of(d);
+  WindowArgs a = args_of(d, window, sinks, positions, first_position, cache);
+  a.q = array_of(q, elem);
+  a.k = array_of(k, elem);
+  a.v = array_of(v, elem);
+  a.out = array_of(out, elem);
+  a.dout = array_of(dout, elem);
+  a.dq = array_of(dq, elem);
+  a.dk = array_of(dk, elem);
+  a.dv = array_of(dv, elem);
+  a.lse = const_cast<float*>(lse);
+  a.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.delta);
+  a.reach = reinterpret_cast<int2*>(static_cast<char*>(workspace) + p.reach);
+  MARL_CHECK(launch(a, d, p, WINDOW_DQ, s));
+  return launch(a, d, p, WINDOW_DKV, s);
+}
+
+int32_t marl_window_attention_step(const marl_attention_dims* dims, int32_t window, int32_t sinks, marl_view q, marl_view k, marl_view v,
+                                   const int32_t* positions, marl_window_cache cache, marl_view out, void* workspace, void* stream) {
+  MARL_CHECK(check_window(dims, window, sinks));
+  const marl_attention_dims& d = *dims;
+  if (d.n_steps != 1) return MARL_E_SIZE;
+  MARL_CHECK(check_launches(d, window, sinks, CALL_STEP, false));
+  if (d.n_seqs == 0) return MARL_OK;
+  for (const marl_view& x : {q, k, v, out}) MARL_CHECK(check_view(x, d.precision, true));
+  MARL_CHECK(check_output(out, d, d.n_heads, true));
+  MARL_CHECK(check_cache(cache, true));
+  if (positions == nullptr) return MARL_E_NULL;
+  MARL_CHECK(check_positions(d, positions, 0));
+  const StepPlan p = step_plan(d, window, sinks);
+  if (p.bytes > 0) MARL_REQUIRE_PTR(workspace);
+  MARL_CHECK(check_places(out, {q, k, v}, true));
+  const int64_t slots = (int64_t)window + sinks;
+  const Extent ck = cached(d, cache.keys, slots, d.dim_k), cv = cached(d, cache.values, slots, d.dim_v);
+  if (ck.meets(cv)) return MARL_E_CONFIG;
+  for (const void* x : {(const void*)q.data, (const void*)k.data, (const void*)v.data, (const void*)out.data, (const void*)positions})
+    if (ck.holds(x) || cv.holds(x)) return MARL_E_CONFIG;
+  const int elem = d.precision == 0 ? 4 : 2;
+  StepArgs a{};
+  a.q = static_cast<const char*>(q.data);
+  a.k = static_cast<const char*>(k.data);
+  a.v = static_cast<const char*>(v.data);
+  a.out = static_cast<char*>(out.data);
+  a.q_seq = q.seq * elem;
+  a.q_head = q.head * elem;
+  a.k_seq = k.seq * elem;
+  a.k_head = k.head * elem;
+  a.v_seq = v.seq * elem;
+  a.v_head = v.head * elem;
+  a.out_seq = out.seq * elem;
+  a.out_head = out.head * elem;
+  a.cache_k = static_cast<char*>(cache.keys);
+  a.cache_v = static_cast<char*>(cache.values);
+  a.positions = positions;
+  a.seqs_per_flag = (uint32_t)d.seqs_per_flag;
+  a.H = (uint32_t)d.n_heads;
+  a.Hk = (uint32_t)d.n_kv_heads;
+  a.group = a.H / a.Hk;
+  a.chunks = p.chunks;
+  a.splits = p.splits;
+  a.units = p.units;
+  a.dk = d.dim_k;
+  a.dv = d.dim_v;
+  a.window = window;
+  a.sinks = sinks;
+  a.c = d.scale * 1.44269504088896341f;
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part);
+  a.stat = reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.stat);
+  const int64_t pairs = (int64_t)d.n_seqs * d.n_heads;
+  return d.precision == 0 ? launch_step<float>(a, p, pairs, (hipStream_t)stream) : launch_step<bf16_t>(a, p, pairs, (hipStream_t)stream);
+}
+
+}  // extern "C"
