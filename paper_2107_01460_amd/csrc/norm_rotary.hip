@@ -158,7 +158,7 @@ struct Columns {
 
 constexpr int kNormRows = 2;  // rows of a lane on their way together
 
-// L lanes take a row.  A workgroup takes one array's rows: forward one run of them, gradient every so many.
+// L lanes take a row, a workgroup every so many runs of one array's rows.
 template <class T, int L, bool INTER, bool WHOLE, bool GRADIENT>
 __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormArgs args) {
   constexpr int E = 16 / sizeof(T), kAtOnce = 256 / L;
@@ -304,11 +304,11 @@ int lanes_of(int precision, int dim) {
   while (L < units) L *= 2;
   return L;
 }
-// Workgroups of an array: a run of rows each, in the gradient as many as fill the chip
-constexpr int64_t kGradientBlocks = 2048;
-int64_t blocks_of(int64_t rows, int L, bool gradient) {
+// Workgroups of an array: as many as fill the chip, each with every so many runs of rows, so that weights are read once
+constexpr int64_t kMaxBlocks = 2048;
+int64_t blocks_of(int64_t rows, int L) {
   const int64_t run = 256 / L * kNormRows, n = (rows + run - 1) / run;
-  return gradient && n > kGradientBlocks ? kGradientBlocks : n;
+  return n > kMaxBlocks ? kMaxBlocks : n;
 }
 
 template <class T, int L, bool GRADIENT>
@@ -338,9 +338,7 @@ int32_t check_norm(const marl_attention_dims* dims, bool k) {
   if (d.seqs_per_flag < 1 || d.n_seqs % d.seqs_per_flag != 0) return MARL_E_CONFIG;
   const int64_t tokens = (int64_t)d.n_steps * d.n_seqs;
   if (tokens > ((int64_t)1 << 48) / (1 << 15)) return MARL_E_SIZE;
-  const int L = lanes_of(d.precision, d.dim_k);
-  const int64_t blocks = blocks_of(tokens * d.n_heads, L, false) + (k ? blocks_of(tokens * d.n_kv_heads, L, false) : 0);
-  return launchable(blocks, 256) ? MARL_OK : MARL_E_SIZE;
+  return MARL_OK;
 }
 int32_t check_turn(const marl_attention_dims& d, float eps, const float* table, int32_t n_positions, int32_t rotary_dim, const int32_t* positions,
                    int32_t first, int32_t interleaved) {
@@ -398,8 +396,8 @@ NormArgs args_of(const marl_attention_dims& d, float eps, const float* table, in
 int32_t run(NormArgs& a, const marl_attention_dims& d, bool gradient, bool k, hipStream_t s) {
   const int L = lanes_of(d.precision, d.dim_k), E = d.precision == 0 ? 4 : 8;
   const bool whole = d.dim_k % E == 0 && (a.inter || a.rotary / 2 % E == 0);
-  a.blocks_q = (uint32_t)blocks_of(a.a[0].rows, L, gradient);
-  const unsigned blocks = a.blocks_q + (k ? (unsigned)blocks_of(a.a[1].rows, L, gradient) : 0);
+  a.blocks_q = (uint32_t)blocks_of(a.a[0].rows, L);
+  const unsigned blocks = a.blocks_q + (k ? (unsigned)blocks_of(a.a[1].rows, L) : 0);
   if (d.precision == 0) (gradient ? launch_norm<float, true> : launch_norm<float, false>)(a, L, blocks, a.inter != 0, whole, s);
   else (gradient ? launch_norm<bf16_t, true> : launch_norm<bf16_t, false>)(a, L, blocks, a.inter != 0, whole, s);
   return launch_status();
@@ -441,7 +439,7 @@ int32_t marl_norm_rotary(const marl_attention_dims* dims, marl_view q, marl_view
 int32_t marl_norm_rotary_workspace(const marl_attention_dims* dims, int64_t* bytes) {
   MARL_CHECK(check_norm(dims, true));
   if (bytes == nullptr) return MARL_E_NULL;
-  *bytes = 2 * ((kGradientBlocks * dims->dim_k * 4 + 255) / 256 * 256);
+  *bytes = 2 * ((kMaxBlocks * dims->dim_k * 4 + 255) / 256 * 256);
   return MARL_OK;
 }
 
@@ -479,7 +477,7 @@ int32_t marl_norm_rotary_backward(const marl_attention_dims* dims, marl_view dq_
   }
   hipStream_t s = (hipStream_t)stream;
   NormArgs a = args_of(d, eps, table, n_positions, rotary_dim, positions, first_position, interleaved);
-  const int64_t half = (kGradientBlocks * d.dim_k * 4 + 255) / 256 * 256;
+  const int64_t half = (kMaxBlocks * d.dim_k * 4 + 255) / 256 * 256;
   WeightArgs w{};
   w.dim = d.dim_k;
   if (used) {
@@ -491,8 +489,8 @@ int32_t marl_norm_rotary_backward(const marl_attention_dims* dims, marl_view dq_
     const int L = lanes_of(d.precision, d.dim_k);
     w.part[0] = a.a[0].part;
     w.part[1] = a.a[1].part;
-    w.n[0] = (int32_t)blocks_of(a.a[0].rows, L, true);
-    w.n[1] = two ? (int32_t)blocks_of(a.a[1].rows, L, true) : 0;
+    w.n[0] = (int32_t)blocks_of(a.a[0].rows, L);
+    w.n[1] = two ? (int32_t)blocks_of(a.a[1].rows, L) : 0;
   }
   if (!weights) return MARL_OK;
   w.out[0] = dq_weight;

@@ -48,7 +48,25 @@ struct WindowArgs {
   uint32_t flip;       // the sign of a negative scale, for the elements of an own array (two of bf16, one of fp32)
   uint32_t heads_each; // query heads of a key head that a workgroup takes
   uint32_t blocks_t;   // workgroups along time
+  int32_t fast;        // rows as Fetch's FAST wants them
+  // first steps seen from beyond the window (far): chunks of far_tiles tiles of rows, far_slots tiles of columns each (none: 0), their numbers and sums
+  uint32_t far_chunks, far_slots;
+  int32_t far_tiles;
+  int* far_numbers;    // [B][Hk][chunk][slot], -1: none
+  float* far_parts;    // the same places, registers of dk and dv each
 };
+
+// Workgroups go round-robin to the eight XCDs.  Where there are many sequences, whole sequences go round: `run` workgroups next to each other in logical order
+// stay on one XCD, and all XCDs work on neighbouring sequences.  (Each XCD on an eighth of the sequences by itself, as in xcd_remap, has all of them at addresses
+// that differ by large powers of two, as a time-major array's steps do, so that they meet in a part of the memory's channels: 128 x 4096 steps of 8 heads of 64
+// in bf16, steps 4 MB apart: 753 us against MEASURED.)  With few sequences an XCD walks along time, its neighbours' keys in its L2.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t at, uint32_t total, uint32_t run, uint32_t sequences) {
+  if (sequences < 64) return xcd_remap(at, total);
+  const uint32_t turn = 8 * run, whole = total / turn * turn;
+  if (at >= whole) return at;
+  const uint32_t in = at / 8;
+  return in / run * turn + at % 8 * run + in % run;
+}
 
 __device__ __forceinline__ int position_of(const WindowArgs& a, int t, uint32_t env) {
   return a.positions != nullptr ? a.positions[(int64_t)t * a.n_flags + env] : a.first + t;
@@ -62,10 +80,10 @@ struct Row {
   __device__ __forceinline__ bool valid() const { return position >= 0; }
   __device__ __forceinline__ bool sees(int j) const { return (uint32_t)(j - lo) <= span || (uint32_t)(j - start) < n_sinks; }
 };
-__device__ __forceinline__ Row row_of(const WindowArgs& a, int i, uint32_t env) {
+__device__ __forceinline__ Row row_with(const WindowArgs& a, int i, int position) {
   Row r;
   r.i = i;
-  r.position = i < a.T ? position_of(a, i, env) : -1;
+  r.position = position;
   if (r.position < 0) {
     r.position = -1;
     r.start = r.lo = 0x7fffffff;
@@ -85,11 +103,27 @@ __device__ __forceinline__ int fresh(int v) {
   return v;
 }
 
+__device__ __forceinline__ Row row_of(const WindowArgs& a, int i, uint32_t env) { return row_with(a, i, i < a.T ? position_of(a, i, env) : -1); }
+
+template <int CONTROL>
+__device__ __forceinline__ int from_lane(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CONTROL, 0xf, 0xf, true);
+}
 template <class F>
 __device__ __forceinline__ int wave_reduce(int v, F f) {
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) v = f(v, __shfl_xor(v, m));
-  return __builtin_amdgcn_readfirstlane(v);
+  v = f(v, from_lane<0xB1>(v));   // the neighbour
+  v = f(v, from_lane<0x4E>(v));   // the other pair
+  v = f(v, from_lane<0x141>(v));  // mirrored in eight
+  v = f(v, from_lane<0x140>(v));  // mirrored in sixteen
+  return f(f(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)), f(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+// A value and the other half's, the same in both
+struct Halves {
+  float lo, hi;
+};
+__device__ __forceinline__ Halves halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return {__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
 __device__ __forceinline__ int wave_min(int v) { return wave_reduce(v, [](int a, int b) { return min(a, b); }); }
 __device__ __forceinline__ int wave_max(int v) { return wave_reduce(v, [](int a, int b) { return max(a, b); }); }
@@ -128,33 +162,80 @@ struct TileShape {
   static constexpr int kUnits = DP * (int)sizeof(T) / 16;  // of a row
 };
 
-// A workgroup's fetch of a tile, held in registers until the tile's place is free.
-template <class T, int DP, int WAVES>
+// Memory that a tile lies in, for loads that give zeros outside it.  (Workgroups hold the same: in scalar registers.)
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+struct Window {
+  __amdgpu_buffer_rsrc_t r;
+  __device__ __forceinline__ Window(const char* p, int64_t bytes) : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, (int)bytes, 0x00020000)) {}
+  __device__ __forceinline__ uint4 load(uint32_t at) const {
+    const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
+    return make_uint4(v[0], v[1], v[2], v[3]);
+  }
+};
+constexpr uint32_t kOutside = 0x80000000u;  // of any window
+
+// A fetch of a tile of 32 rows by WAVES wavefronts (one: each by itself), held in registers until the tile's place is free.  FAST: rows are whole 16-byte pieces, four-byte aligned, and 32 of them
+// span less than 2 GB; every load is then issued unconditionally, so that the wait for one tile leaves the next one's on their way.
+template <class T, int DP, int WAVES, bool FAST>
 struct Fetch {
-  static constexpr int kThreads = 64 * WAVES, kAll = kTile * TileShape<T, DP>::kUnits, kEach = (kAll + kThreads - 1) / kThreads;
-  uint4 v[kEach];
-  // rows from `rows` on, `step` bytes apart, `count` of them; the others zero
-  __device__ __forceinline__ void request(const char* rows, int64_t step, int count, int dim) {
-    constexpr int E = 16 / sizeof(T);
-    const bool whole = dim % E == 0;  // no unit ends inside
+  static constexpr int kUnits = TileShape<T, DP>::kUnits, kThreads = 64 * WAVES, kAll = kTile * kUnits, kEach = (kAll + kThreads - 1) / kThreads;
+  static constexpr bool kEven = kThreads % kUnits == 0;  // a thread's units lie in one column, the same number of rows apart
+  static constexpr int kPlaces = kEven ? 1 : kEach;
+  __device__ __forceinline__ static int tid() { return threadIdx.x % kThreads; }
+  // where a thread's units lie in a tile of rows `step` bytes apart
+  struct Places {
+    uint32_t at[FAST ? kPlaces : 1];
+    uint32_t more;
+    __device__ __forceinline__ void set(int64_t step, int dim) {
+      if constexpr (FAST) {
+        more = (uint32_t)(kThreads / kUnits) * (uint32_t)step;
 #pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-      const int at = threadIdx.x + u * kThreads, row = at / TileShape<T, DP>::kUnits, c = at % TileShape<T, DP>::kUnits;
-      v[u] = make_uint4(0, 0, 0, 0);
-      if (whole && row < count && c * E < dim) __builtin_memcpy(&v[u], rows + row * step + 16 * c, 16);  // (at any alignment)
+        for (int u = 0; u < kPlaces; ++u) at[u] = unit_at(tid(), u) * 16 < dim * (int)sizeof(T) && row_at(tid(), u) < kTile ? row_at(tid(), u) * (uint32_t)step + 16 * unit_at(tid(), u) : kOutside;
+      }
     }
-    if (whole) return;
+  };
+  uint4 v[kEach];
+  __device__ __forceinline__ static int row_at(int tid, int u) { return (tid + u * kThreads) / kUnits; }
+  __device__ __forceinline__ static int unit_at(int tid, int u) { return (tid + u * kThreads) % kUnits; }
+  // rows from `rows` on, `count` of them; the others zero (or, where rows share memory, any value of theirs)
+  __device__ __forceinline__ void request(const Places& p, const char* rows, int64_t step, int count, int dim) {
+    if constexpr (FAST) {
+      const int n = count < kTile ? count : kTile;
+      const Window w(rows, n > 0 ? (n - 1) * step + dim * (int)sizeof(T) : 0);
 #pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-      const int at = fresh(threadIdx.x) + u * kThreads, row = at / TileShape<T, DP>::kUnits, c = at % TileShape<T, DP>::kUnits;
-      if (row < count) v[u] = load_unit<T>(rows + row * step, c * E, dim);
+      for (int u = 0; u < kEach; ++u) v[u] = w.load(kEven ? p.at[0] + u * p.more : p.at[kEven ? 0 : u]);
+    } else {
+      const int tid = fresh(threadIdx.x % kThreads);
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        v[u] = make_uint4(0, 0, 0, 0);
+        if (row_at(tid, u) < count) v[u] = load_unit<T>(rows + row_at(tid, u) * step, unit_at(tid, u) * (16 / (int)sizeof(T)), dim);
+      }
     }
   }
   __device__ __forceinline__ void store(char* tile) const {
 #pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-      const int at = threadIdx.x + u * kThreads, row = at / TileShape<T, DP>::kUnits, c = at % TileShape<T, DP>::kUnits;
-      if (kAll % kThreads == 0 || at < kAll) *reinterpret_cast<uint4*>(tile + row * TileShape<T, DP>::kStride + 16 * c) = v[u];
+    for (int u = 0; u < kEach; ++u)
+      if (kAll % kThreads == 0 || tid() + u * kThreads < kAll)
+        *reinterpret_cast<uint4*>(tile + row_at(tid(), u) * TileShape<T, DP>::kStride + 16 * unit_at(tid(), u)) = v[u];
+  }
+};
+
+// A wavefront's own 32 rows: unit s of a lane's row, elements 2 E s + E half on
+template <class T, int DP, bool FAST>
+struct OwnRows {
+  const char* rows;
+  int64_t step;
+  int count, dim;
+  __device__ __forceinline__ uint4 unit(int s) const {
+    constexpr int E = 16 / sizeof(T);
+    const int lane = threadIdx.x & 63, col = 2 * E * s + E * (lane / 32);
+    if constexpr (FAST) {
+      const int n = count < kTile ? count : kTile;
+      const Window w(rows, n > 0 ? (n - 1) * step + dim * (int)sizeof(T) : 0);
+      return w.load(col < dim ? lane % 32 * (uint32_t)step + col * (int)sizeof(T) : kOutside);
+    } else {
+      return lane % 32 < count ? load_unit<T>(rows + lane % 32 * step, col, dim) : make_uint4(0, 0, 0, 0);
     }
   }
 };
@@ -172,12 +253,11 @@ struct Products<bf16_t, DP> {
   struct Own {
     bf16x8_t v[DP / 16];
   };
-  static __device__ __forceinline__ void load_own(Own& own, const char* row, int dim, bool on, uint32_t flip) {
-    const int h = (threadIdx.x & 63) / 32;
+  template <class Rows>
+  static __device__ __forceinline__ void load_own(Own& own, const Rows& rows, uint32_t flip) {
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) {
-      uint4 u = make_uint4(0, 0, 0, 0);
-      if (on) u = load_unit<bf16_t>(row, 16 * s + 8 * h, dim);
+      uint4 u = rows.unit(s);
       u.x ^= flip; u.y ^= flip; u.z ^= flip; u.w ^= flip;
       __builtin_memcpy(&own.v[s], &u, 16);
     }
@@ -230,12 +310,11 @@ struct Products<float, DP> {
   struct Own {
     float4 v[DP / 8];
   };
-  static __device__ __forceinline__ void load_own(Own& own, const char* row, int dim, bool on, uint32_t flip) {
-    const int h = (threadIdx.x & 63) / 32;
+  template <class Rows>
+  static __device__ __forceinline__ void load_own(Own& own, const Rows& rows, uint32_t flip) {
 #pragma unroll
     for (int s = 0; s < DP / 8; ++s) {
-      uint4 u = make_uint4(0, 0, 0, 0);
-      if (on) u = load_unit<float>(row, 8 * s + 4 * h, dim);
+      uint4 u = rows.unit(s);
       u.x ^= flip; u.y ^= flip; u.z ^= flip; u.w ^= flip;
       __builtin_memcpy(&own.v[s], &u, 16);
     }
@@ -304,12 +383,12 @@ __device__ __forceinline__ void add_with_care(f32x16_t (&acc)[DP / 32], const ch
 
 template <int N>
 __device__ __forceinline__ bool not_finite(const f32x16_t (&acc)[N]) {
-  bool bad = false;
+  float x = 0.f;  // zero times an infinity or a NaN stays a NaN
 #pragma unroll
   for (int t = 0; t < N; ++t)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) bad |= !(__builtin_fabsf(acc[t][r]) < __builtin_inff());
-  return bad;
+    for (int r = 0; r < 16; ++r) x = __builtin_fmaf(acc[t][r], 0.f, x);
+  return !(x == 0.f);
 }
 
 template <class T>
@@ -437,7 +516,7 @@ constexpr int columns_waves() { return DP > (sizeof(T) == 4 ? 32 : 64) ? 1 : 2; 
 
 // ---- output, and dq ------------------------------------------------------------------------------------------------------------------
 // A workgroup: `heads_each` query heads of one key head, WAVES / heads_each tiles of 32 rows each.
-template <class T, int DP, int WAVES, bool GRADIENT>
+template <class T, int DP, int WAVES, bool GRADIENT, bool FAST>
 __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) window_rows_kernel(const WindowArgs a) {
   typedef Products<T, DP> P;
   typedef TileShape<T, DP> Shape;
@@ -446,49 +525,57 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
   // neighbouring heads, then stretches of time, then sequences: next to each other on one XCD
   const uint32_t teams = a.group / a.heads_each;
-  uint32_t at = xcd_remap(blockIdx.x, gridDim.x);
+  uint32_t at = xcd_order(blockIdx.x, gridDim.x, a.Hk * teams * a.blocks_t, a.B);
   const uint32_t head_team = at % (a.Hk * teams);
   at /= a.Hk * teams;
   const uint32_t block_t = at % a.blocks_t, b = at / a.blocks_t;
   const uint32_t hk = head_team / teams, env = b / a.seqs_per_flag;
   const uint32_t h = hk * a.group + head_team % teams * a.heads_each + wave % a.heads_each;
   const int tiles_each = WAVES / a.heads_each, row0 = (int)block_t * tiles_each * kTile, my0 = row0 + (int)(wave / a.heads_each) * kTile;
+  const int i = my0 + lane % 32;
+  const char *kp = a.k.data + b * a.k.seq + hk * a.k.head, *vp = a.v.data + b * a.v.seq + hk * a.v.head;
+  const int64_t cached_at = ((int64_t)b * a.Hk + hk) * (a.sinks + a.window);
+  const char *ck = a.cache_k + cached_at * a.dk_dim * (int)sizeof(T), *cv = a.cache_v + cached_at * a.dv_dim * (int)sizeof(T);
+  typename P::Own q, d;
+  typedef OwnRows<T, DP, FAST> Rows;
+  const int count = a.T - my0;
+  P::load_own(q, Rows{a.q.data + my0 * a.q.step + b * a.q.seq + h * a.q.head, a.q.step, a.scale != 0.f ? count : 0, a.dk_dim}, a.flip);
+  float lse2 = 0.f, delta = 0.f;
+  const int64_t stat = ((int64_t)b * a.H + h) * a.T + i;
+  if constexpr (GRADIENT) {
+    P::load_own(d, Rows{a.dout.data + my0 * a.dout.step + b * a.dout.seq + h * a.dout.head, a.dout.step, count, a.dv_dim}, 0);
+    typename P::Own o;
+    P::load_own(o, Rows{a.out.data + my0 * a.out.step + b * a.out.seq + h * a.out.head, a.out.step, count, a.dv_dim}, 0);
+    delta = P::dot(d, o);
+    const Halves both = halves(delta);
+    delta = both.lo + both.hi;
+    if (half == 0 && i < a.T) a.delta[stat] = delta;
+    if (i < a.T) lse2 = a.lse[stat] * 1.44269504088896341f;
+  }
   Tiles tiles;
   tiles.set(a, env, row0, tiles_each * kTile);
-  const Row row = row_of(a, my0 + lane % 32, env);
+  const Row row = row_of(a, i, env);
   if constexpr (GRADIENT) {  // for dk and dv: where the episodes of each tile's rows began
     if (h == 0 && b % a.seqs_per_flag == 0 && my0 < a.T) {
       const int lo = wave_min(row.valid() ? row.start : 0x7fffffff), hi = wave_max(row.valid() ? row.start : -0x7fffffff);
       if (lane == 0) a.reach[(int64_t)env * ((a.T + kTile - 1) / kTile) + my0 / kTile] = make_int2(lo, hi);
     }
   }
-  const char *kp = a.k.data + b * a.k.seq + hk * a.k.head, *vp = a.v.data + b * a.v.seq + hk * a.v.head;
-  const int64_t cached_at = ((int64_t)b * a.Hk + hk) * (a.sinks + a.window);
-  const char *ck = a.cache_k + cached_at * a.dk_dim * (int)sizeof(T), *cv = a.cache_v + cached_at * a.dv_dim * (int)sizeof(T);
-  typename P::Own q, d;
-  P::load_own(q, a.q.data + row.i * a.q.step + b * a.q.seq + h * a.q.head, a.dk_dim, row.valid(), a.flip);
-  float lse2 = 0.f, delta = 0.f;
-  const int64_t stat = ((int64_t)b * a.H + h) * a.T + row.i;
-  if constexpr (GRADIENT) {
-    P::load_own(d, a.dout.data + row.i * a.dout.step + b * a.dout.seq + h * a.dout.head, a.dv_dim, row.valid(), 0);
-    typename P::Own o;
-    P::load_own(o, a.out.data + row.i * a.out.step + b * a.out.seq + h * a.out.head, a.dv_dim, row.valid(), 0);
-    delta = P::dot(d, o);
-    delta += __shfl_xor(delta, 32);
-    if (half == 0 && row.i < a.T) a.delta[stat] = delta;
-    if (row.valid()) lse2 = a.lse[stat] * 1.44269504088896341f;
-  }
-  Fetch<T, DP, WAVES> fk, fv;
-  auto request = [&](const Tile& t) __attribute__((always_inline)) {
-    if (t.kind == TILE_CACHE) {
-      const int n = tiles.cached - t.at * kTile;
-      fk.request(ck + (int64_t)t.at * kTile * a.dk_dim * (int)sizeof(T), a.dk_dim * (int)sizeof(T), n, a.dk_dim);
-      fv.request(cv + (int64_t)t.at * kTile * a.dv_dim * (int)sizeof(T), a.dv_dim * (int)sizeof(T), n, a.dv_dim);
-    } else {
-      const int n = a.T - t.at * kTile;
-      fk.request(kp + (int64_t)t.at * kTile * a.k.step, a.k.step, n, a.dk_dim);
-      fv.request(vp + (int64_t)t.at * kTile * a.v.step, a.v.step, n, a.dv_dim);
-    }
+  typedef Fetch<T, DP, WAVES, FAST> F;
+  const int64_t ck_step = a.dk_dim * (int)sizeof(T), cv_step = a.dv_dim * (int)sizeof(T);
+  typename F::Places pk, pv, pck, pcv;
+  pk.set(a.k.step, a.dk_dim);
+  pv.set(a.v.step, a.dv_dim);
+  pck.set(ck_step, a.dk_dim);
+  pcv.set(cv_step, a.dv_dim);
+  // two tiles on their way
+  F fk[2], fv[2];
+  auto request = [&](F& k, F& v, const Tile& t) __attribute__((always_inline)) {
+    const bool cache = t.kind == TILE_CACHE;
+    const int n = t.kind == TILE_NONE ? 0 : (cache ? tiles.cached : a.T) - t.at * kTile;
+    const int64_t first = t.kind == TILE_NONE ? 0 : (int64_t)t.at * kTile;
+    k.request(cache ? pck : pk, cache ? ck + first * ck_step : kp + first * a.k.step, cache ? ck_step : a.k.step, n, a.dk_dim);
+    v.request(cache ? pcv : pv, cache ? cv + first * cv_step : vp + first * a.v.step, cache ? cv_step : a.v.step, n, a.dv_dim);
   };
   f32x16_t acc[DP / 32];
   float top = 0.f, sum = 0.f;  // output: the largest exponent (of two) so far, the sum of this half's weights
@@ -497,60 +584,70 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
     for (int t = 0; t < DP / 32; ++t) acc[t] = (f32x16_t){0.f};
     top = -__builtin_inff();
     sum = 0.f;
-    Tile cur = tiles.next(a, {TILE_CACHE, -1});
-    if (cur.kind != TILE_NONE) request(cur);
-    for (int buffer = 0; cur.kind != TILE_NONE; buffer ^= 1) {
-      fk.store(tile_at(buffer, 0));
-      fv.store(tile_at(buffer, 1));
-      const Tile now = cur;
-      cur = tiles.next(a, cur);
-      if (cur.kind != TILE_NONE) request(cur);
+    Tile ahead[2];
+    ahead[0] = tiles.next(a, {TILE_CACHE, -1});
+    request(fk[0], fv[0], ahead[0]);
+    ahead[1] = tiles.next(a, ahead[0]);
+    request(fk[1], fv[1], ahead[1]);
+    // one tile: into LDS, the one after the next requested, the products; false behind the last
+    auto turn = [&](auto which) __attribute__((always_inline)) {
+      constexpr int buffer = decltype(which)::value;
+      const Tile now = ahead[buffer];
+      if (now.kind == TILE_NONE) return false;
+      fk[buffer].store(tile_at(buffer, 0));
+      fv[buffer].store(tile_at(buffer, 1));
+      ahead[buffer] = tiles.next(a, ahead[buffer ^ 1]);
+      request(fk[buffer], fv[buffer], ahead[buffer]);
       __syncthreads();
-      // which of the tile's rows each lane's row sees: bit r for register r
+      // What each lane's row sees of the tile, as simply as all rows allow: all of it, the steps from one on to another, or more
+      enum { SEE_ALL, SEE_BAND, SEE_MORE, SEE_CACHE };
       const int j0 = now.at * kTile;
-      uint32_t seen = 0xffffu;
+      int sight = SEE_CACHE;
       if (now.kind == TILE_CACHE) {
-        const bool goes_on = row.valid() && row.start < 0;
-        if (__ballot(goes_on) == 0) continue;
-        seen = 0;
-        const int first = j0 + 4 * fresh(half);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int slot = first + result_row(r, 0), step = tiles.step_of(a, slot);
-          if (goes_on && slot < tiles.cached && (slot < a.sinks || row.position - step < a.window)) seen |= 1u << r;
-        }
+        if (__ballot(row.valid() && row.start < 0) == 0) return true;
       } else {
         const int j1 = j0 + kTile - 1;
-        const bool whole = j0 >= row.lo && j1 <= row.i;
-        const bool some = row.valid() && (whole || (j1 >= row.lo && j0 <= row.i) || (row.start <= j1 && row.start + (int)row.n_sinks > j0));
-        if (__ballot(some) == 0) continue;
-        if (__ballot(!whole && row.valid()) != 0) {
-          seen = 0;
-          const int first = j0 + 4 * fresh(half);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) seen |= row.sees(first + result_row(r, 0)) ? 1u << r : 0u;
-        }
+        const bool band = j1 >= row.lo && j0 <= row.i, sinks = row.start <= j1 && row.start + (int)row.n_sinks > j0 && j0 < row.lo;
+        if (__ballot(row.valid() && (band || sinks)) == 0) return true;
+        sight = __ballot(row.valid() && sinks) != 0 ? SEE_MORE : __ballot(row.valid() && !(j0 >= row.lo && j1 <= row.i)) != 0 ? SEE_BAND : SEE_ALL;
       }
-      const bool masked = __ballot(seen != 0xffffu) != 0;
-      const f32x16_t s = P::score(tile_at(buffer, 0), q);
+      // (register r's column is result_row(r, half) behind the tile's first)
+      auto for_seen = [&](auto f) __attribute__((always_inline)) {  // f(register, whether it is seen)
+        const int first = j0 + 4 * fresh(half);
+        if (sight == SEE_BAND) {
+          const uint32_t from = (uint32_t)(first - row.lo);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) f(r, from + result_row(r, 0) <= row.span);
+        } else if (sight == SEE_MORE) {
+          const uint32_t from = (uint32_t)(first - row.lo), begun = (uint32_t)(first - row.start);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) f(r, from + result_row(r, 0) <= row.span || begun + result_row(r, 0) < row.n_sinks);
+        } else {
+          // slots of first steps; of the ring, whose steps from `from` on are seen, up to the newest step's slot, and from where it goes round
+          const bool goes_on = row.valid() && row.start < 0;
+          const int from = row.position - a.window + 1;
+          const bool round = tiles.newest >= a.sinks + a.window;
+          const int turned = tiles.newest - tiles.newest_slot;  // a slot's step, up to the newest; a window less behind it
+          const int x = round ? max(from - turned, a.sinks) : max(from, a.sinks), y = round ? max(from - turned + a.window, tiles.newest_slot + 1) : 0x7fffffff;
+          const int end = goes_on ? tiles.cached : 0, last = goes_on ? (round ? tiles.newest_slot : tiles.cached - 1) : -1, heads = goes_on ? min(a.sinks, tiles.cached) : 0;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int slot = first + result_row(r, 0);
+            f(r, (slot < heads) | ((slot >= x) & (slot <= last)) | ((slot >= y) & (slot < end)));
+          }
+        }
+      };
+      f32x16_t s = P::score(tile_at(buffer, 0), q);
       float p[16];
       if constexpr (!GRADIENT) {
-        float most = -__builtin_inff();
-        if (masked) {
+        if (sight != SEE_ALL) for_seen([&](int r, bool on) __attribute__((always_inline)) { s[r] = on ? s[r] : -__builtin_inff(); });
+        float most = s[0];
 #pragma unroll
-          for (int r = 0; r < 16; ++r) most = fmaxf(most, seen >> r & 1u ? s[r] : -__builtin_inff());
-        } else {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) most = fmaxf(most, s[r]);
-        }
-        most = fmaxf(most, __shfl_xor(most, 32));
-        const float now_top = fmaxf(top, most == -__builtin_inff() ? most : most * a.c), base = now_top == -__builtin_inff() ? 0.f : now_top;
+        for (int r = 1; r < 16; ++r) most = fmaxf(most, s[r]);
+        const Halves both = halves(most);
+        const float now_top = fmaxf(top, fmaxf(both.lo, both.hi) * a.c), base = now_top == -__builtin_inff() ? 0.f : now_top;
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c, -base));
-        if (masked) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) p[r] = seen >> r & 1u ? p[r] : 0.f;
-        }
         if (__ballot(now_top != top) != 0) {
           const float shrink = __builtin_amdgcn_exp2f(top - base);
           sum *= shrink;
@@ -564,26 +661,31 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
         const f32x16_t e = P::score(tile_at(buffer, 1), d);
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c, -lse2)) * (e[r] - delta);
-        if (masked) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) p[r] = seen >> r & 1u ? p[r] : 0.f;
-        }
+        if (sight != SEE_ALL) for_seen([&](int r, bool on) __attribute__((always_inline)) { p[r] = on ? p[r] : 0.f; });
       }
       const char* y = tile_at(buffer, GRADIENT ? 0 : 1);
       if constexpr (!decltype(careful)::value) {
         P::add(acc, y, p);
       } else {
+        uint32_t seen = 0xffffu;
+        if (sight != SEE_ALL) {
+          seen = 0;
+          for_seen([&](int r, bool on) __attribute__((always_inline)) { seen |= on ? 1u << r : 0u; });
+        }
         add_with_care<T, DP>(acc, y, p, seen);
       }
+      return true;
+    };
+    while (turn(std::integral_constant<int, 0>()) && turn(std::integral_constant<int, 1>())) {
     }
   };
   pass(std::false_type());
   if (__syncthreads_or(row.valid() && not_finite(acc))) pass(std::true_type());
   __syncthreads();
-  const int count = a.T - my0;
   char* place = lds + wave * Shape::kBytes;
   if constexpr (!GRADIENT) {
-    sum += __shfl_xor(sum, 32);
+    const Halves both = halves(sum);
+    sum = both.lo + both.hi;
     if (half == 0 && a.lse != nullptr && row.i < a.T) a.lse[stat] = row.valid() ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : -__builtin_inff();
     store_rows<T, DP>(place, acc, 1.f / sum, !row.valid(), a.out.data + my0 * a.out.step + b * a.out.seq + h * a.out.head, a.out.step, count, a.dv_dim);
   } else {
@@ -592,49 +694,92 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
 }
 
 // ---- dk, dv ----------------------------------------------------------------------------------------------------------------------------
-// A workgroup: WAVES tiles of 32 keys of one key head; queries and their gradients are streamed, head after head of those that share the key head.
-template <class T, int DP, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, (columns_waves<T, DP>())) window_columns_kernel(const WindowArgs a) {
+// A wavefront takes 32 columns of one key head and, of the query heads that share it, every `heads_each`-th; it streams the rows that see them through a place in LDS of
+// its own, so that wavefronts never wait for each other (four that share tiles of rows wait at every tile for the one that has work: 128 x 4096 steps of 4 heads
+// of 32 in fp32, window 32: MEASURED).  The heads_each wavefronts of the same columns add up their sums at the end, in order.
+//
+// First steps are seen by every later row of their episode: in a long sequence far more tiles of rows than any other column, one wavefront's work.  There the pairs
+// of tiles beyond the window are cut along the rows (far): every so many tiles of rows a wavefront takes the first `far_slots` tiles of first steps that they see, into
+// fp32 parts with the tile's number beside them; the columns' own wavefronts add the parts with their number, in order, and take what was beyond the slots themselves.
+template <class T, int DP>
+constexpr bool fetches_ahead() { return sizeof(T) == 2 || DP <= 64; }  // (wider ones spill)
+
+template <class T, int DP, bool FAST>
+__global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_kernel(const WindowArgs a, const int far) {
   typedef Products<T, DP> P;
   typedef TileShape<T, DP> Shape;
-  __shared__ __attribute__((aligned(16))) char lds[4 * Shape::kBytes];
-  __shared__ __attribute__((aligned(16))) float stats[2][2][kTile];  // lse (exponent of two), delta
-  __shared__ int4 sight[2][kTile];                                   // lo, span, start, first steps
-  auto tile_at = [&](int buffer, int which) __attribute__((always_inline)) { return lds + (2 * buffer + which) * Shape::kBytes; };
+  __shared__ __attribute__((aligned(16))) char lds[4][2 * Shape::kBytes];
+  __shared__ __attribute__((aligned(16))) float all_stats[4][2][kTile];  // lse (exponent of two), delta
+  __shared__ int4 all_sight[4][kTile];                                   // lo, span, start, first steps
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
-  uint32_t at = xcd_remap(blockIdx.x, gridDim.x);
-  const uint32_t hk = at % a.Hk;
-  at /= a.Hk;
-  const uint32_t block_t = at % a.blocks_t, b = at / a.blocks_t, env = b / a.seqs_per_flag;
-  const int col0 = (int)block_t * WAVES * kTile, col1 = min(col0 + WAVES * kTile, a.T) - 1, my0 = col0 + wave * kTile, my1 = min(my0 + kTile, a.T) - 1, j = my0 + lane % 32;
+  char *tile_q = lds[wave], *tile_d = lds[wave] + Shape::kBytes;
+  auto& stats = all_stats[wave];
+  int4* sight = all_sight[wave];
+  const uint32_t heads = a.heads_each, units_each = 4 / heads, team = wave % heads;
   const int n_tiles = (a.T + kTile - 1) / kTile;
+  const uint32_t per_head = far ? a.far_chunks * a.far_slots : (uint32_t)n_tiles;  // units of a key head
+  const int64_t unit = (int64_t)xcd_order(blockIdx.x, gridDim.x, (a.Hk * per_head + units_each - 1) / units_each, a.B) * units_each + wave / heads;
+  const bool on = unit < (int64_t)a.B * a.Hk * per_head;
+  const uint32_t hk = on ? (uint32_t)(unit % a.Hk) : 0, which = on ? (uint32_t)(unit / a.Hk % per_head) : 0, b = on ? (uint32_t)(unit / a.Hk / per_head) : 0;
+  const uint32_t env = b / a.seqs_per_flag;
   const int2* reach = a.reach + (int64_t)env * n_tiles;
+  const int64_t slots = (int64_t)a.far_chunks * a.far_slots, head_slots = ((int64_t)b * a.Hk + hk) * slots;
+  int* numbers = a.far_numbers + head_slots;
+  int col_tile = on ? (int)which : -1, first_tile = 0, end_tile = n_tiles;
+  if (far) {  // the columns: the chunk's slot-th tile of first steps that its rows see from beyond the window
+    const int chunk = which / a.far_slots;
+    first_tile = chunk * a.far_tiles;
+    end_tile = min(first_tile + a.far_tiles, n_tiles);
+    int from = 0;
+    col_tile = -1;
+    for (int n = (int)(which % a.far_slots); on && n >= 0; --n) {
+      int least = 0x7fffffff;
+      for (int i = first_tile * kTile + lane; i < end_tile * kTile; i += 64) {
+        const Row r = row_of(a, i, env);
+        const int t = i / kTile, most = t * kTile >= a.window + kTile - 1 ? (t * kTile - a.window - kTile + 1) / kTile : -1;
+        if (r.n_sinks == 0) continue;
+        const int last = r.start + (int)r.n_sinks - 1, c = max(max(r.start, 0) / kTile, from);
+        if (last >= 0 && c <= min(last / kTile, most)) least = min(least, c);
+      }
+      least = wave_min(least);
+      col_tile = least == 0x7fffffff ? -1 : least;
+      if (col_tile < 0) break;
+      from = col_tile + 1;
+    }
+    if (on && team == 0 && lane == 0) numbers[which] = col_tile;
+  }
+  const int my0 = max(col_tile, 0) * kTile, my1 = min(my0 + kTile, a.T) - 1, j = my0 + lane % 32;
   typename P::Own k, v;
-  P::load_own(k, a.k.data + j * a.k.step + b * a.k.seq + hk * a.k.head, a.dk_dim, j < a.T, a.flip);
-  P::load_own(v, a.v.data + j * a.v.step + b * a.v.seq + hk * a.v.head, a.dv_dim, j < a.T, 0);
-  // The tiles of rows that see any of the workgroup's columns, 64 looked at at a time
+  typedef OwnRows<T, DP, FAST> Rows;
+  P::load_own(k, Rows{a.k.data + my0 * a.k.step + b * a.k.seq + hk * a.k.head, a.k.step, a.scale != 0.f ? a.T - my0 : 0, a.dk_dim}, a.flip);
+  P::load_own(v, Rows{a.v.data + my0 * a.v.step + b * a.v.seq + hk * a.v.head, a.v.step, a.T - my0, a.dv_dim}, 0);
+  // The tiles of rows that see any of the columns, 64 looked at at a time
   struct Cursor {
     int base;
     uint64_t left;
-    int tile;
+    int tile;  // -1: none yet, -2: no more
     uint32_t g;
   };
   auto look = [&](int base) __attribute__((always_inline)) {
     const int t = base + lane;
     bool needed = false;
-    if (t < n_tiles) {
+    if (t < end_tile) {
       const int2 r = reach[t];
-      const int64_t last = (int64_t)col1 + a.window - 1;
-      needed = r.x <= col1 && ((int64_t)t * kTile <= last || (a.sinks > 0 && (int64_t)r.y + a.sinks > col0));
+      const bool beyond = t * kTile - my1 >= a.window;
+      needed = r.x <= my1 && (!beyond || (a.sinks > 0 && (int64_t)r.y + a.sinks > my0)) && (far ? beyond : t >= col_tile);
+      if (needed && beyond && !far && a.far_slots > 0)  // taken by a wavefront of its chunk?
+        for (uint32_t n = 0; n < a.far_slots; ++n)
+          if (numbers[t / a.far_tiles * a.far_slots + n] == col_tile) needed = false;
     }
     return (uint64_t)__ballot(needed);
   };
   auto next = [&](Cursor c) __attribute__((always_inline)) {
-    if (c.tile >= 0 && ++c.g < a.group) return c;
-    c.g = 0;
+    if (c.tile == -2) return c;
+    if (c.tile >= 0 && (c.g += heads) < a.group) return c;
+    c.g = team;
     while (c.left == 0) {
       c.base += 64;
-      if (c.base >= n_tiles) {
+      if (c.base >= end_tile) {
         c.tile = -2;
         return c;
       }
@@ -645,68 +790,71 @@ __global__ void __launch_bounds__(64 * WAVES, (columns_waves<T, DP>())) window_c
     c.tile = c.base + bit;
     return c;
   };
-  Fetch<T, DP, WAVES> fq, fd;
-  float lse2 = 0.f, delta = 0.f;
-  Row seer{};
+  typedef Fetch<T, DP, 1, FAST> F;
+  typename F::Places pq, pd;
+  pq.set(a.q.step, a.dk_dim);
+  pd.set(a.dout.step, a.dv_dim);
+  F fq, fd;
+  float lse, delta;
+  int position;
+  const int32_t* positions = a.positions != nullptr ? a.positions : reinterpret_cast<const int32_t*>(a.lse);
   auto request = [&](const Cursor& c) __attribute__((always_inline)) {
     const uint32_t h = hk * a.group + c.g;
-    const int i0 = c.tile * kTile, n = a.T - i0;
-    fq.request(a.q.data + i0 * a.q.step + b * a.q.seq + h * a.q.head, a.q.step, n, a.dk_dim);
-    fd.request(a.dout.data + i0 * a.dout.step + b * a.dout.seq + h * a.dout.head, a.dout.step, n, a.dv_dim);
-    if (threadIdx.x < kTile) {
-      seer = row_of(a, i0 + threadIdx.x, env);
-      lse2 = delta = 0.f;
-      if (seer.valid()) {
-        const int64_t stat = ((int64_t)b * a.H + h) * a.T + seer.i;
-        lse2 = a.lse[stat] * 1.44269504088896341f;
-        delta = a.delta[stat];
-      }
-    }
+    const int i0 = c.tile < 0 ? 0 : c.tile * kTile, n = c.tile < 0 ? 0 : a.T - i0;
+    fq.request(pq, a.q.data + i0 * a.q.step + b * a.q.seq + h * a.q.head, a.q.step, n, a.dk_dim);
+    fd.request(pd, a.dout.data + i0 * a.dout.step + b * a.dout.seq + h * a.dout.head, a.dout.step, n, a.dv_dim);
+    const int i = min(i0 + lane % kTile, a.T - 1);
+    const int64_t stat = ((int64_t)b * a.H + h) * a.T + i;
+    lse = a.lse[stat];
+    delta = a.delta[stat];
+    position = positions[a.positions != nullptr ? (int64_t)i * a.n_flags + env : 0];
   };
   f32x16_t dk[DP / 32], dv[DP / 32];
   auto pass = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) dk[t] = dv[t] = (f32x16_t){0.f};
-    const int base = col0 / kTile;
-    Cursor cur = next({base, look(base), -1, 0});
-    if (cur.tile >= 0) request(cur);
-    for (int buffer = 0; cur.tile >= 0; buffer ^= 1) {
-      fq.store(tile_at(buffer, 0));
-      fd.store(tile_at(buffer, 1));
-      if (threadIdx.x < kTile) {
-        stats[buffer][0][threadIdx.x] = lse2;
-        stats[buffer][1][threadIdx.x] = delta;
-        sight[buffer][threadIdx.x] = make_int4(seer.lo, (int)seer.span, seer.start, (int)seer.n_sinks);
+    if (col_tile < 0) return;
+    const int base = far ? first_tile : col_tile;
+    Cursor ahead = next({base, look(base), -1, team});
+    if (fetches_ahead<T, DP>()) request(ahead);
+    while (ahead.tile >= 0) {
+      const Cursor now = ahead;
+      if (!fetches_ahead<T, DP>()) request(now);
+      __builtin_amdgcn_wave_barrier();
+      fq.store(tile_q);
+      fd.store(tile_d);
+      if (lane < kTile) {
+        const int i = now.tile * kTile + lane;
+        const Row seer = row_with(a, i, i < a.T ? a.positions != nullptr ? position : a.first + i : -1);
+        stats[0][lane] = seer.valid() ? lse * 1.44269504088896341f : 0.f;
+        stats[1][lane] = seer.valid() ? delta : 0.f;
+        sight[lane] = make_int4(seer.lo, (int)seer.span, seer.start, (int)seer.n_sinks);
       }
-      cur = next(cur);
-      if (cur.tile >= 0) request(cur);
-      __syncthreads();
-      auto sees = [&](const int4& w, int col) __attribute__((always_inline)) { return (uint32_t)(col - w.x) <= (uint32_t)w.y || (uint32_t)(col - w.z) < (uint32_t)w.w; };
-      uint32_t seen = 0xffffu;
-      {
-        // a row's last step is lo + span; rows that hold no step see nothing (lo above every column)
-        const int4 w = sight[buffer][lane % 32];
-        const int i = w.x == 0x7fffffff ? -1 : w.x + w.y;
-        const bool whole = w.x <= my0 && my1 <= i;
-        const bool some = whole || (w.x <= my1 && my0 <= i) || ((int64_t)w.z + w.w > my0 && w.z <= my1);
-        if (my0 >= a.T || __ballot(some) == 0) continue;
-        if (__ballot(!whole) != 0) {
-          seen = 0;
-          const int4* from = sight[buffer] + 4 * fresh(half);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      ahead = next(ahead);
+      if (fetches_ahead<T, DP>()) request(ahead);
+      // (a row's last step is lo + span; rows that hold no step see nothing: lo above every column)
+      const int4 w = sight[lane % 32];
+      const int last = w.x == 0x7fffffff ? -1 : w.x + w.y;
+      const bool whole = w.x <= my0 && my1 <= last, band = w.x <= my1 && my0 <= last, sinks = (int64_t)w.z + w.w > my0 && w.z <= my1;
+      if (__ballot(band || sinks) == 0) continue;
+      const bool masked = __ballot(!whole) != 0, more = __ballot(sinks) != 0;
+      auto for_seen = [&](auto f) __attribute__((always_inline)) {  // f(register, whether its row sees the lane's column)
+        const int4* from = sight + 4 * fresh(half);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            seen |= sees(from[result_row(r, 0)], j) ? 1u << r : 0u;
-            if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-          }
+        for (int r = 0; r < 16; ++r) {
+          const int4 x = from[result_row(r, 0)];
+          f(r, (uint32_t)(j - x.x) <= (uint32_t)x.y || (more && (uint32_t)(j - x.z) < (uint32_t)x.w));
+          if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
-      }
-      const bool masked = __ballot(seen != 0xffffu) != 0;
-      const f32x16_t s = P::score(tile_at(buffer, 0), k), e = P::score(tile_at(buffer, 1), v);
+      };
+      const f32x16_t s = P::score(tile_q, k), e = P::score(tile_d, v);
       float p[16], ds[16];
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
-        const float4 l = *reinterpret_cast<const float4*>(&stats[buffer][0][result_row(r, half)]);
-        const float4 m = *reinterpret_cast<const float4*>(&stats[buffer][1][result_row(r, half)]);
+        const float4 l = *reinterpret_cast<const float4*>(&stats[0][result_row(r, half)]);
+        const float4 m = *reinterpret_cast<const float4*>(&stats[1][result_row(r, half)]);
         const float ls[4] = {l.x, l.y, l.z, l.w}, ms[4] = {m.x, m.y, m.z, m.w};
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -715,52 +863,112 @@ __global__ void __launch_bounds__(64 * WAVES, (columns_waves<T, DP>())) window_c
         }
       }
       if (masked) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          p[r] = seen >> r & 1u ? p[r] : 0.f;
-          ds[r] = seen >> r & 1u ? ds[r] : 0.f;
-        }
+        for_seen([&](int r, bool on) __attribute__((always_inline)) {
+          p[r] = on ? p[r] : 0.f;
+          ds[r] = on ? ds[r] : 0.f;
+        });
       }
       if constexpr (!decltype(careful)::value) {
-        P::add(dv, tile_at(buffer, 1), p);
-        P::add(dk, tile_at(buffer, 0), ds);
+        P::add(dv, tile_d, p);
+        P::add(dk, tile_q, ds);
       } else {
-        add_with_care<T, DP>(dv, tile_at(buffer, 1), p, seen);
-        add_with_care<T, DP>(dk, tile_at(buffer, 0), ds, seen);
+        uint32_t seen = 0xffffu;
+        if (masked) {
+          seen = 0;
+          for_seen([&](int r, bool on) __attribute__((always_inline)) { seen |= on ? 1u << r : 0u; });
+        }
+        add_with_care<T, DP>(dv, tile_d, p, seen);
+        add_with_care<T, DP>(dk, tile_q, ds, seen);
       }
     }
   };
   pass(std::false_type());
-  if (__syncthreads_or(j < a.T && (not_finite(dk) || not_finite(dv)))) pass(std::true_type());
-  __syncthreads();
-  char* place = lds + wave * Shape::kBytes;
-  if (my0 < a.T) {
-    store_rows<T, DP>(place, dk, a.scale, false, a.dk.data + my0 * a.dk.step + b * a.dk.seq + hk * a.dk.head, a.dk.step, a.T - my0, a.dk_dim);
-    store_rows<T, DP>(place, dv, 1.f, false, a.dv.data + my0 * a.dv.step + b * a.dv.seq + hk * a.dv.head, a.dv.step, a.T - my0, a.dv_dim);
+  if (__ballot(j < a.T && (not_finite(dk) || not_finite(dv))) != 0) pass(std::true_type());
+  // the heads' sums, in order
+  if (heads > 1) {
+    float* mine = reinterpret_cast<float*>(lds[wave]) + lane;
+    auto gather = [&](f32x16_t (&acc)[DP / 32]) __attribute__((always_inline)) {
+      __syncthreads();
+      if (team != 0) {
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) mine[64 * (16 * t + r)] = acc[t][r];
+      }
+      __syncthreads();
+      if (team == 0) {
+        for (uint32_t n = 1; n < heads; ++n) {
+          const float* other = reinterpret_cast<const float*>(lds[wave + n]) + lane;
+#pragma unroll
+          for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[t][r] += other[64 * (16 * t + r)];
+        }
+      }
+    };
+    gather(dk);
+    gather(dv);
+    __syncthreads();
   }
+  if (team != 0 || col_tile < 0) return;
+  // (a part: registers in order, lanes next to each other; dk, then dv)
+  constexpr int kPart = 64 * 16 * (DP / 32);
+  if (far) {
+    float* part = a.far_parts + (head_slots + which) * (2 * kPart) + lane;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        part[64 * (16 * t + r)] = dk[t][r];
+        part[kPart + 64 * (16 * t + r)] = dv[t][r];
+      }
+    return;
+  }
+  if (a.far_slots > 0) {
+    for (int64_t s0 = 0; s0 < slots; s0 += 64) {
+      uint64_t left = __ballot(s0 + lane < slots && numbers[s0 + lane] == col_tile);
+      for (; left != 0; left &= left - 1) {
+        const float* part = a.far_parts + (head_slots + s0 + __builtin_ctzll(left)) * (2 * kPart) + lane;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            dk[t][r] += part[64 * (16 * t + r)];
+            dv[t][r] += part[kPart + 64 * (16 * t + r)];
+          }
+      }
+    }
+  }
+  store_rows<T, DP>(lds[wave], dk, a.scale, false, a.dk.data + my0 * a.dk.step + b * a.dk.seq + hk * a.dk.head, a.dk.step, a.T - my0, a.dk_dim);
+  store_rows<T, DP>(lds[wave], dv, 1.f, false, a.dv.data + my0 * a.dv.step + b * a.dv.seq + hk * a.dv.head, a.dv.step, a.T - my0, a.dv_dim);
 }
 
 // The wavefronts that fetch a tile, at the least: a wavefront that fetches one of wide fp32 heads alone holds 128 registers of it and spills.
 constexpr int least_waves(size_t elem, int dim) { return elem == 4 && dim > 64 ? 4 : 1; }
 
 // ---- launches --------------------------------------------------------------------------------------------------------------------------
-enum { WINDOW_OUTPUT, WINDOW_DQ, WINDOW_DKV };
+enum { WINDOW_OUTPUT, WINDOW_DQ, WINDOW_DKV, WINDOW_FAR };
 
-template <class T, int DP, int WAVES>
+template <class T, int DP, int WAVES, bool FAST>
 void launch_window(const WindowArgs& a, int pass, unsigned blocks, hipStream_t s) {
-  if (pass == WINDOW_OUTPUT) hipLaunchKernelGGL((window_rows_kernel<T, DP, WAVES, false>), dim3(blocks), dim3(64 * WAVES), 0, s, a);
-  if (pass == WINDOW_DQ) hipLaunchKernelGGL((window_rows_kernel<T, DP, WAVES, true>), dim3(blocks), dim3(64 * WAVES), 0, s, a);
-  if (pass == WINDOW_DKV) hipLaunchKernelGGL((window_columns_kernel<T, DP, WAVES>), dim3(blocks), dim3(64 * WAVES), 0, s, a);
+  if (pass == WINDOW_OUTPUT) hipLaunchKernelGGL((window_rows_kernel<T, DP, WAVES, false, FAST>), dim3(blocks), dim3(64 * WAVES), 0, s, a);
+  if (pass == WINDOW_DQ) hipLaunchKernelGGL((window_rows_kernel<T, DP, WAVES, true, FAST>), dim3(blocks), dim3(64 * WAVES), 0, s, a);
 }
 template <class T, int DP>
 void launch_window(const WindowArgs& a, int pass, int waves, unsigned blocks, hipStream_t s) {
+  if (pass == WINDOW_DKV || pass == WINDOW_FAR) {
+    if (a.fast) hipLaunchKernelGGL((window_columns_kernel<T, DP, true>), dim3(blocks), dim3(256), 0, s, a, pass == WINDOW_FAR);
+    else hipLaunchKernelGGL((window_columns_kernel<T, DP, false>), dim3(blocks), dim3(256), 0, s, a, pass == WINDOW_FAR);
+    return;
+  }
+  if (!a.fast) return launch_window<T, DP, 4, false>(a, pass, blocks, s);
   if constexpr (least_waves(sizeof(T), DP) <= 1) {
-    if (waves == 1) return launch_window<T, DP, 1>(a, pass, blocks, s);
+    if (waves == 1) return launch_window<T, DP, 1, true>(a, pass, blocks, s);
   }
   if constexpr (least_waves(sizeof(T), DP) <= 2) {
-    if (waves == 2) return launch_window<T, DP, 2>(a, pass, blocks, s);
+    if (waves == 2) return launch_window<T, DP, 2, true>(a, pass, blocks, s);
   }
-  launch_window<T, DP, 4>(a, pass, blocks, s);
+  launch_window<T, DP, 4, true>(a, pass, blocks, s);
 }
 // Heads as wide as the wider of keys and values, in steps of 32
 template <class T>

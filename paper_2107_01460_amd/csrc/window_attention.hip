@@ -10,35 +10,55 @@ namespace {
 // ---- how a call is laid out ----------------------------------------------------------------------------------------------------
 struct Plan {
   int tiles;                  // of 32 steps
-  int heads_each, rows_waves; // query heads of a workgroup, its wavefronts
-  int cols_waves;
-  int64_t rows_t, cols_t;     // workgroups along time
-  int64_t rows, cols;         // workgroups
-  int64_t delta, reach, bytes;
+  int heads_each, rows_waves; // query heads of a workgroup; wavefronts of one that takes rows
+  int64_t rows_t;             // workgroups along time
+  int64_t rows, cols, far;    // workgroups
+  int far_tiles;
+  uint32_t far_chunks, far_slots;
+  int64_t delta, reach, numbers, parts, bytes;
 };
+int padded(const marl_attention_dims& d) { return ((d.dim_k > d.dim_v ? d.dim_k : d.dim_v) + 31) / 32 * 32; }
 // A workgroup's wavefronts share the streamed tiles: query heads of one key head first, then tiles next to each other in time.
-Plan plan_of(const marl_attention_dims& d) {
+Plan plan_of(const marl_attention_dims& d, int window, int sinks, bool fast) {
   Plan p{};
   p.tiles = (int)(((int64_t)d.n_steps + kTile - 1) / kTile);
-  const int group = d.n_heads / d.n_kv_heads;
+  const int group = d.n_heads / d.n_kv_heads, pairs = d.n_seqs * d.n_kv_heads;
   p.heads_each = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
-  p.cols_waves = p.tiles < 2 ? 1 : p.tiles == 2 ? 2 : 4;
-  const int least = least_waves(d.precision == 0 ? 4 : 2, d.dim_k > d.dim_v ? d.dim_k : d.dim_v);
-  if (p.cols_waves < least) p.cols_waves = least;
-  p.rows_waves = p.heads_each * p.cols_waves < 4 ? p.heads_each * p.cols_waves : 4;
+  int along = p.tiles < 2 ? 1 : p.tiles == 2 ? 2 : 4;
+  const int least = fast ? least_waves(d.precision == 0 ? 4 : 2, padded(d)) : 4;
+  if (along < least) along = least;
+  p.rows_waves = p.heads_each * along < 4 ? p.heads_each * along : 4;
   const int each = p.rows_waves / p.heads_each;
   p.rows_t = (p.tiles + each - 1) / each;
-  p.cols_t = (p.tiles + p.cols_waves - 1) / p.cols_waves;
   p.rows = (int64_t)d.n_seqs * (d.n_heads / p.heads_each) * p.rows_t;
-  p.cols = (int64_t)d.n_seqs * d.n_kv_heads * p.cols_t;
+  auto workgroups = [&](int64_t units) { return (units * p.heads_each + 3) / 4; };
+  p.cols = workgroups((int64_t)pairs * p.tiles);
+  // First steps seen from afar are cut along the rows where columns are few (else others keep the chip busy meanwhile) and eight tiles or more lie beyond the window
+  if (sinks > 0 && (int64_t)pairs * p.tiles <= 8192 && p.tiles > window / kTile + 10) {
+    p.far_tiles = p.tiles > 256 ? (p.tiles + 31) / 32 : 8;
+    p.far_chunks = (uint32_t)((p.tiles + p.far_tiles - 1) / p.far_tiles);
+    p.far_slots = (uint32_t)(sinks / kTile + 3 < 8 ? sinks / kTile + 3 : 8);
+    p.far = workgroups((int64_t)pairs * p.far_chunks * p.far_slots);
+  }
   auto take = [&](int64_t bytes) {
     const int64_t here = p.bytes;
     p.bytes += (bytes + 255) / 256 * 256;
     return here;
   };
+  const int64_t slots = (int64_t)pairs * p.far_chunks * p.far_slots;
   p.delta = take((int64_t)d.n_seqs * d.n_heads * d.n_steps * 4);
   p.reach = take((int64_t)(d.n_seqs / d.seqs_per_flag) * p.tiles * 8);
+  p.numbers = take(slots * 4);
+  p.parts = take(slots * 2 * kTile * padded(d) * 4);
   return p;
+}
+
+// Rows that Fetch takes with unconditional loads: whole 16-byte pieces, four-byte aligned, 32 of them within 2 GB
+bool fast_rows(const marl_attention_dims& d, const marl_view& v, int dim) {
+  const int elem = d.precision == 0 ? 4 : 2;
+  const int64_t step = v.step * elem;
+  return dim * elem % 16 == 0 && (reinterpret_cast<uintptr_t>(v.data) & 3u) == 0 && step % 4 == 0 && v.seq * elem % 4 == 0 && v.head * elem % 4 == 0 &&
+         step >= 0 && step < (1 << 26) - 16;
 }
 
 // ---- the cache behind a call ---------------------------------------------------------------------------------------------------------
@@ -73,7 +93,7 @@ __device__ __forceinline__ void put_unit(T* p, const uint4& u, int left) {  // `
 template <class T>
 __global__ void __launch_bounds__(256) window_cache_kernel(const CacheArgs a) {
   constexpr int E = 16 / sizeof(T);
-  uint32_t at = xcd_remap(blockIdx.x, gridDim.x);
+  uint32_t at = xcd_order(blockIdx.x, gridDim.x, a.Hk * a.chunks, a.n_flags * a.seqs_per_flag);
   const uint32_t chunk = at % a.chunks;
   at /= a.chunks;
   const uint32_t hk = at % a.Hk, b = at / a.Hk, env = b / a.seqs_per_flag;
@@ -203,17 +223,30 @@ __global__ void __launch_bounds__(256) window_step_kernel(const StepArgs a) {
     const int here = position < a.sinks ? position : a.sinks + (position - a.sinks) % a.window;  // this step's slot
     char *ck = a.cache_k + pair * slots * a.dk * (int64_t)sizeof(T), *cv = a.cache_v + pair * slots * a.dv * (int64_t)sizeof(T);
     const char *kp = a.k + b * a.k_seq + hk * a.k_head, *vp = a.v + b * a.v_seq + hk * a.v_head;
+    const bool whole_k = a.dk % E == 0, whole_v = a.dv % E == 0;  // no 16 bytes end inside
+    uint4 next_k[kStepRows], next_v[kStepRows];
+    auto request = [&](int64_t base) __attribute__((always_inline)) {  // a batch of rows, one batch ahead
+#pragma unroll
+      for (int u = 0; u < kStepRows; ++u) {
+        const int64_t slot = base + u * R + r;
+        next_k[u] = next_v[u] = make_uint4(0, 0, 0, 0);
+        if (slot >= end) continue;
+        const char *pk = slot == here ? kp : ck + slot * a.dk * (int)sizeof(T), *pv = slot == here ? vp : cv + slot * a.dv * (int)sizeof(T);
+        if (whole_k && c < a.dk) __builtin_memcpy(&next_k[u], pk + c * (int)sizeof(T), 16);
+        if (whole_v && c < a.dv) __builtin_memcpy(&next_v[u], pv + c * (int)sizeof(T), 16);
+        if (!whole_k) next_k[u] = load_unit<T>(pk, c, a.dk);
+        if (!whole_v) next_v[u] = load_unit<T>(pv, c, a.dv);
+      }
+    };
+    if (begin < end) request(begin);
     for (int64_t base = begin; base < end; base += R * kStepRows) {
       uint4 k[kStepRows], v[kStepRows];
 #pragma unroll
       for (int u = 0; u < kStepRows; ++u) {
-        const int64_t slot = base + u * R + r;
-        k[u] = v[u] = make_uint4(0, 0, 0, 0);
-        if (slot < end) {
-          k[u] = load_unit<T>(slot == here ? kp : ck + slot * a.dk * (int)sizeof(T), c, a.dk);
-          v[u] = load_unit<T>(slot == here ? vp : cv + slot * a.dv * (int)sizeof(T), c, a.dv);
-        }
+        k[u] = next_k[u];
+        v[u] = next_v[u];
       }
+      if (base + R * kStepRows < end) request(base + R * kStepRows);
       float s[G][kStepRows];
 #pragma unroll
       for (int u = 0; u < kStepRows; ++u) {
@@ -293,25 +326,42 @@ __global__ void __launch_bounds__(256) window_step_kernel(const StepArgs a) {
   }
 }
 
-// The parts of a cut step, one workgroup a query head, in a fixed order
+// The parts of a cut step, one workgroup a query head, in a fixed order: eight teams of 128 threads take every eighth part.
+constexpr int kMaxSplits = 512;
 template <class T>
-__global__ void __launch_bounds__(128) window_step_join_kernel(const StepArgs a) {
+__global__ void __launch_bounds__(1024) window_step_join_kernel(const StepArgs a) {
+  __shared__ float2 stats[kMaxSplits];
+  __shared__ float sums[8], accs[8][128];
   const int64_t pair = blockIdx.x;
   const uint32_t b = (uint32_t)(pair / a.H), h = (uint32_t)(pair % a.H);
-  const int d = threadIdx.x;
+  const int d = threadIdx.x % 128, team = threadIdx.x / 128;
   const int position = a.positions[b / a.seqs_per_flag];
-  const float2* stat = a.stat + pair * a.splits;
+  for (uint32_t s = threadIdx.x; s < a.splits; s += 1024) stats[s] = a.stat[pair * a.splits + s];
+  __syncthreads();
   float top = -__builtin_inff();
-  for (uint32_t s = 0; s < a.splits; ++s) top = fmaxf(top, stat[s].x);
+  for (uint32_t s = threadIdx.x & 63; s < a.splits; s += 64) top = fmaxf(top, stats[s].x);
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
   const float from = top == -__builtin_inff() ? 0.f : top;
-  if (d >= a.dv) return;
   float sum = 0.f, acc = 0.f;
+  const float* part = a.part + pair * a.splits * a.dv + d;
+  const bool on = d < a.dv;
 #pragma unroll 8
-  for (uint32_t s = 0; s < a.splits; ++s) {
-    const float2 x = stat[s];
+  for (uint32_t s = team; s < a.splits; s += 8) {
+    const float2 x = stats[s];
     const float factor = __builtin_amdgcn_exp2f(x.x - from);
-    sum += factor * x.y;
-    acc += factor * a.part[(pair * a.splits + s) * a.dv + d];
+    sum = __builtin_fmaf(factor, x.y, sum);
+    if (on) acc = __builtin_fmaf(factor, part[(int64_t)s * a.dv], acc);
+  }
+  if (d == 0) sums[team] = sum;
+  accs[team][d] = acc;
+  __syncthreads();
+  if (team != 0 || !on) return;
+  sum = acc = 0.f;
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    sum += sums[u];
+    acc += accs[u][d];
   }
   const float o = position < 0 ? 0.f : acc / sum;
   T* out = reinterpret_cast<T*>(a.out + b * a.out_seq + h * a.out_head) + d;
@@ -336,6 +386,7 @@ StepPlan step_plan(const marl_attention_dims& d, int window, int sinks) {
   const int64_t whole = (int64_t)d.n_seqs * d.n_kv_heads * p.chunks, slots = (int64_t)window + sinks, least = 64 / p.lanes * kStepRows * 2;
   int64_t n = whole > 0 ? kWaves / whole : 1;
   n = n < slots / least ? n : slots / least;
+  n = n < kMaxSplits ? n : kMaxSplits;
   p.splits = (uint32_t)(n < 2 ? 1 : n);
   p.units = whole * p.splits;
   auto take = [&](int64_t bytes) {
@@ -367,7 +418,7 @@ int32_t launch_step(const StepArgs& a, const StepPlan& p, int64_t pairs, hipStre
   else if constexpr (sizeof(T) == 4) MARL_STEP_HEADS(32);
 #undef MARL_STEP_HEADS
 #undef MARL_STEP
-  if (p.splits > 1) hipLaunchKernelGGL((window_step_join_kernel<T>), dim3((unsigned)pairs), dim3(128), 0, s, a);
+  if (p.splits > 1) hipLaunchKernelGGL((window_step_join_kernel<T>), dim3((unsigned)pairs), dim3(1024), 0, s, a);
   return launch_status();
 }
 
@@ -421,15 +472,15 @@ WindowArgs args_of(const marl_attention_dims& d, int32_t window, int32_t sinks, 
   a.window = window;
   a.sinks = sinks;
   a.scale = d.scale;
-  a.c = __builtin_fabsf(d.scale) * 1.44269504088896341f;
+  a.c = d.scale == 0.f ? 1.f : __builtin_fabsf(d.scale) * 1.44269504088896341f;  // (above zero, so that minus infinity stays that; the scores are zero then)
   a.flip = d.scale < 0.f ? (d.precision == 0 ? 0x80000000u : 0x80008000u) : 0u;
   return a;
 }
 int32_t launch(WindowArgs& a, const marl_attention_dims& d, const Plan& p, int pass, hipStream_t s) {
-  const bool cols = pass == WINDOW_DKV;
   a.heads_each = (uint32_t)p.heads_each;
-  a.blocks_t = (uint32_t)(cols ? p.cols_t : p.rows_t);
-  (d.precision == 0 ? launch_window_f32 : launch_window_bf16)(a, pass, cols ? p.cols_waves : p.rows_waves, (unsigned)(cols ? p.cols : p.rows), s);
+  a.blocks_t = (uint32_t)p.rows_t;
+  const int64_t blocks = pass == WINDOW_DKV ? p.cols : pass == WINDOW_FAR ? p.far : p.rows;
+  (d.precision == 0 ? launch_window_f32 : launch_window_bf16)(a, pass, p.rows_waves, (unsigned)blocks, s);
   return launch_status();
 }
 int64_t cache_blocks(const marl_attention_dims& d, int64_t slots) { return (int64_t)d.n_seqs * d.n_kv_heads * ((slots + kCacheRows - 1) / kCacheRows); }
@@ -440,10 +491,12 @@ int32_t check_launches(const marl_attention_dims& d, int32_t window, int32_t sin
   bool fits = true;
   if (call == CALL_STEP) {
     const StepPlan p = step_plan(d, window, sinks);
-    fits = launchable((p.units + 3) / 4, 256) && (p.splits == 1 || launchable((int64_t)d.n_seqs * d.n_heads, 128));
+    fits = launchable((p.units + 3) / 4, 256) && (p.splits == 1 || launchable((int64_t)d.n_seqs * d.n_heads, 1024));
   } else {
-    const Plan p = plan_of(d);
-    fits = launchable(p.rows, 64 * p.rows_waves) && (call == CALL_FORWARD || launchable(p.cols, 64 * p.cols_waves));
+    for (bool fast : {false, true}) {  // (whichever the arrays' strides lead to)
+      const Plan p = plan_of(d, window, sinks, fast);
+      fits = fits && launchable(p.rows, 64 * p.rows_waves) && (call == CALL_FORWARD || (launchable(p.cols, 256) && launchable(p.far, 256)));
+    }
     if (next_cache) fits = fits && launchable(cache_blocks(d, (int64_t)window + sinks), 256);
   }
   return fits ? MARL_OK : MARL_E_SIZE;
@@ -461,7 +514,7 @@ int32_t marl_window_attention_workspace(const marl_attention_dims* dims, int32_t
   if (call < CALL_FORWARD || call > CALL_STEP) return MARL_E_CONFIG;
   if (bytes == nullptr) return MARL_E_NULL;
   MARL_CHECK(check_launches(*dims, window, sinks, call, false));
-  *bytes = call == CALL_FORWARD ? 0 : call == CALL_BACKWARD ? plan_of(*dims).bytes : step_plan(*dims, window, sinks).bytes;
+  *bytes = call == CALL_FORWARD ? 0 : call == CALL_BACKWARD ? plan_of(*dims, window, sinks, true).bytes : step_plan(*dims, window, sinks).bytes;
   return MARL_OK;
 }
 
@@ -502,7 +555,8 @@ int32_t marl_window_attention(const marl_attention_dims* dims, int32_t window, i
     a.v = array_of(v, elem);
     a.out = array_of(out, elem);
     a.lse = lse;
-    MARL_CHECK(launch(a, d, plan_of(d), WINDOW_OUTPUT, s));
+    a.fast = fast_rows(d, q, d.dim_k) && fast_rows(d, k, d.dim_k) && fast_rows(d, v, d.dim_v);
+    MARL_CHECK(launch(a, d, plan_of(d, window, sinks, a.fast), WINDOW_OUTPUT, s));
   }
   if (next_cache.keys == nullptr) return MARL_OK;
   CacheArgs c{};
@@ -556,8 +610,10 @@ int32_t marl_window_attention_backward(const marl_attention_dims* dims, int32_t 
     if (ck.holds(x) || cv.holds(x) || x == lse || x == positions) return MARL_E_CONFIG;
   hipStream_t s = (hipStream_t)stream;
   const int elem = d.precision == 0 ? 4 : 2;
-  const Plan p = plan_of(d);
+  const bool fast = fast_rows(d, q, d.dim_k) && fast_rows(d, k, d.dim_k) && fast_rows(d, v, d.dim_v) && fast_rows(d, out, d.dim_v) && fast_rows(d, dout, d.dim_v);
+  const Plan p = plan_of(d, window, sinks, fast);
   WindowArgs a = args_of(d, window, sinks, positions, first_position, cache);
+  a.fast = fast;
   a.q = array_of(q, elem);
   a.k = array_of(k, elem);
   a.v = array_of(v, elem);
@@ -569,7 +625,13 @@ int32_t marl_window_attention_backward(const marl_attention_dims* dims, int32_t 
   a.lse = const_cast<float*>(lse);
   a.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.delta);
   a.reach = reinterpret_cast<int2*>(static_cast<char*>(workspace) + p.reach);
+  a.far_chunks = p.far_chunks;
+  a.far_slots = p.far_slots;
+  a.far_tiles = p.far_tiles;
+  a.far_numbers = reinterpret_cast<int*>(static_cast<char*>(workspace) + p.numbers);
+  a.far_parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.parts);
   MARL_CHECK(launch(a, d, p, WINDOW_DQ, s));
+  if (p.far > 0) MARL_CHECK(launch(a, d, p, WINDOW_FAR, s));
   return launch(a, d, p, WINDOW_DKV, s);
 }
 
