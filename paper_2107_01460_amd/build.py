@@ -19,10 +19,18 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I", INCLUDE, "
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]
 
+# Window attention's products with their sums in ordinary registers: the compiler otherwise copies 128 of them to the other half of the register file and back for
+# every tile where a wavefront has more than 256
+EXTRA_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for src in ("window_attention_f32.hip", "window_attention_bf16.hip")}
+
+
+def flags(src):
+    return [*FLAGS, *EXTRA_FLAGS.get(src, [])]
+
 
 def _compile(src):
     obj = os.path.join(CSRC, src.replace(".hip", ".o"))
-    subprocess.check_call(["hipcc", *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])
+    subprocess.check_call(["hipcc", *flags(src), "-c", os.path.join(CSRC, src), "-o", obj])
     return obj
 
 

@@ -154,12 +154,20 @@ __device__ __forceinline__ uint4 load_unit(const char* row, int col, int dim) {
 }
 
 // ---- tiles in LDS -------------------------------------------------------------------------------------------------------------------
-// Rows of DP elements and 16 bytes, so that eight consecutive rows' 16-byte pieces lie in different banks.
+// Read in two ways: 16 bytes of 16 rows at once (a product's first operand), and, in bf16, pieces of four rows' 64 bytes (the transposed reads).  bf16: a row's pieces
+// are exchanged by bits of the row's number, so that both touch every bank once (padded rows instead: 272 bytes, half of the time of the transposed reads went into
+// conflicts; a long sequence of 8 heads of 128 MEASURED).  fp32: padded by 16 bytes; its second reads are of single elements.
 template <class T, int DP>
 struct TileShape {
-  static constexpr int kStride = DP * (int)sizeof(T) + 16;
+  static constexpr bool kExchanged = sizeof(T) == 2;
+  static constexpr int kStride = kExchanged ? (DP <= 32 ? 64 : DP <= 64 ? 128 : 256) : DP * (int)sizeof(T) + 16;
   static constexpr int kBytes = kTile * kStride;
   static constexpr int kUnits = DP * (int)sizeof(T) / 16;  // of a row
+  // what a row's pieces are exchanged by: rows next to each other by the higher bits, which the transposed reads of four rows need
+  __device__ __forceinline__ static int mix(int row) {
+    return kStride == 64 ? row >> 2 & 3 : kStride == 128 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : (row & 3) << 2 | (row >> 2 & 3);
+  }
+  __device__ __forceinline__ static int at(int row, int unit) { return row * kStride + 16 * (kExchanged ? unit ^ mix(row) : unit); }
 };
 
 // Memory that a tile lies in, for loads that give zeros outside it.  (Workgroups hold the same: in scalar registers.)
@@ -217,7 +225,7 @@ struct Fetch {
 #pragma unroll
     for (int u = 0; u < kEach; ++u)
       if (kAll % kThreads == 0 || tid() + u * kThreads < kAll)
-        *reinterpret_cast<uint4*>(tile + row_at(tid(), u) * TileShape<T, DP>::kStride + 16 * unit_at(tid(), u)) = v[u];
+        *reinterpret_cast<uint4*>(tile + TileShape<T, DP>::at(row_at(tid(), u), unit_at(tid(), u))) = v[u];
   }
 };
 
@@ -270,21 +278,22 @@ struct Products<bf16_t, DP> {
       for (int e = 0; e < 8; ++e) s += (float)a.v[n][e] * (float)b.v[n][e];
     return s;
   }
+  // (a piece's place is the row's beginning and the exchanged number of the piece: one exclusive or from one piece to another)
   static __device__ __forceinline__ f32x16_t score(const char* tile, const Own& own) {
-    const int lane = threadIdx.x & 63;
-    const char* p = tile + (lane % 32) * Shape::kStride + 16 * (lane / 32);
+    const int lane = threadIdx.x & 63, first = Shape::at(lane % 32, lane / 32);
     f32x16_t s = {0.f};
 #pragma unroll
-    for (int n = 0; n < DP / 16; ++n) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8_t*>(p + 32 * n), own.v[n], s, 0, 0, 0);
+    for (int n = 0; n < DP / 16; ++n) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8_t*>(tile + (first ^ 32 * n)), own.v[n], s, 0, 0, 0);
     return s;
   }
   typedef short s16x8_t __attribute__((ext_vector_type(8)));
   // Four streamed rows of sixteen columns, transposed, for rows 16 g of columns 32 t
   static __device__ __forceinline__ s16x8_t turned(const char* tile, int t, int g) {
-    const int lane = threadIdx.x & 63;
-    const char* p = tile + (16 * g + 4 * (lane / 32) + lane % 16 / 4) * Shape::kStride + 2 * (32 * t + 16 * (lane / 16 % 2) + 4 * (lane % 4));
+    const int lane = threadIdx.x & 63, row = 4 * (lane / 32) + lane % 16 / 4, unit = 2 * (lane / 16 % 2) + lane % 4 / 2, in = 8 * (lane % 2);
+    const int first = (Shape::at(row, unit) + in) ^ 64 * t, second = (Shape::at(row + 8, unit) + in) ^ 64 * t;  // (rows 16 on are exchanged alike)
     typedef __attribute__((address_space(3))) i16x4_t* Lds;
-    const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 8 * Shape::kStride));
+    const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(tile + first + 16 * g * Shape::kStride));
+    const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(tile + second + 16 * g * Shape::kStride));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
   static __device__ __forceinline__ bf16x8_t pack(const float* p) {
@@ -351,6 +360,12 @@ struct Products<float, DP> {
   }
 };
 
+// Where a row's four elements 32 t + result_row(r, half) on lie
+template <class T, int DP>
+__device__ __forceinline__ int four_at(int row, int t, int r, int half) {
+  return sizeof(T) == 4 ? TileShape<T, DP>::at(row, 8 * t + r / 2 + half) : TileShape<T, DP>::at(row, 4 * t + r / 4) + 8 * half;
+}
+
 // acc^T += Y^T P one streamed row after another (weights of rows that a column does not see are zero), for tiles that hold infinities or NaNs: a column takes the rows that it sees (bit r of `seen` for the row
 // of register r) and nothing else.  On the vector units, few registers at a time: this must not cost the loop around it any.
 template <class T, int DP>
@@ -366,16 +381,13 @@ __device__ __forceinline__ void add_with_care(f32x16_t (&acc)[DP / 32], const ch
     const bool on = __shfl((int)seen, lane % 32 + 32 * from) >> at & 1;
     // (a bit mask, not a choice: the compiler makes branches of choices here, with half of the registers inside them)
     const uint32_t mask = on ? 0xffffffffu : 0u;
-    const T* y = reinterpret_cast<const T*>(tile + row * TileShape<T, DP>::kStride);
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
+        const T* y = reinterpret_cast<const T*>(tile + four_at<T, DP>(row, t, r, half));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float v = load_act(y, 32 * t + result_row(r, 0) + 4 * half + e);
-          acc[t][r + e] = __builtin_fmaf(w, __uint_as_float(__float_as_uint(v) & mask), acc[t][r + e]);
-        }
+        for (int e = 0; e < 4; ++e) acc[t][r + e] = __builtin_fmaf(w, __uint_as_float(__float_as_uint(load_act(y, e)) & mask), acc[t][r + e]);
         __builtin_amdgcn_sched_barrier(0);
       }
   }
@@ -403,7 +415,6 @@ __device__ __forceinline__ void store_rows(char* place, const f32x16_t (&acc)[DP
   typedef TileShape<T, DP> Shape;
   constexpr int E = 16 / sizeof(T);
   const int lane = threadIdx.x & 63, h = lane / 32;
-  char* mine = place + (lane % 32) * Shape::kStride;
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
@@ -411,7 +422,7 @@ __device__ __forceinline__ void store_rows(char* place, const f32x16_t (&acc)[DP
       float o[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = zero ? 0.f : acc[t][r + e] * factor;
-      store4<T>(mine + (int)sizeof(T) * (32 * t + result_row(r, h)), o[0], o[1], o[2], o[3]);
+      store4<T>(place + four_at<T, DP>(lane % 32, t, r, h), o[0], o[1], o[2], o[3]);
     }
   // (one wavefront's LDS accesses are done in order; the fence keeps the compiler from moving the reads up)
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -420,14 +431,14 @@ __device__ __forceinline__ void store_rows(char* place, const f32x16_t (&acc)[DP
 #pragma unroll
     for (int u = 0; u < kTile * Shape::kUnits / 64; ++u) {
       const int at = lane + 64 * u, row = at / Shape::kUnits, c = at % Shape::kUnits * E;
-      const uint4 v = *reinterpret_cast<const uint4*>(place + row * Shape::kStride + (int)sizeof(T) * c);
+      const uint4 v = *reinterpret_cast<const uint4*>(place + Shape::at(row, at % Shape::kUnits));
       if (row < count && c < dim) __builtin_memcpy(rows + row * step + (int)sizeof(T) * c, &v, 16);
     }
   } else {
 #pragma unroll 1
     for (int at = lane; at < kTile * DP; at += 64) {
       const int row = at / DP, c = at % DP;
-      if (row < count && c < dim) reinterpret_cast<T*>(rows + row * step)[c] = *reinterpret_cast<const T*>(place + row * Shape::kStride + (int)sizeof(T) * c);
+      if (row < count && c < dim) reinterpret_cast<T*>(rows + row * step)[c] = *reinterpret_cast<const T*>(place + Shape::at(row, c / E) + (int)sizeof(T) * (c % E));
     }
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -760,6 +771,12 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
     int tile;  // -1: none yet, -2: no more
     uint32_t g;
   };
+  uint64_t taken = 0;  // chunks (at most 64) whose rows beyond the window are in parts
+  if (!far && on) {
+    for (int s0 = 0; s0 < (int)slots; s0 += 64)
+      for (uint64_t left = __ballot(s0 + lane < (int)slots && numbers[min(s0 + lane, (int)slots - 1)] == col_tile); left != 0; left &= left - 1)
+        taken |= 1ull << ((s0 + __builtin_ctzll(left)) / a.far_slots);
+  }
   auto look = [&](int base) __attribute__((always_inline)) {
     const int t = base + lane;
     bool needed = false;
@@ -767,9 +784,7 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
       const int2 r = reach[t];
       const bool beyond = t * kTile - my1 >= a.window;
       needed = r.x <= my1 && (!beyond || (a.sinks > 0 && (int64_t)r.y + a.sinks > my0)) && (far ? beyond : t >= col_tile);
-      if (needed && beyond && !far && a.far_slots > 0)  // taken by a wavefront of its chunk?
-        for (uint32_t n = 0; n < a.far_slots; ++n)
-          if (numbers[t / a.far_tiles * a.far_slots + n] == col_tile) needed = false;
+      if (beyond && !far && taken != 0 && (taken >> (t / a.far_tiles) & 1)) needed = false;
     }
     return (uint64_t)__ballot(needed);
   };
@@ -884,25 +899,46 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
   };
   pass(std::false_type());
   if (__ballot(j < a.T && (not_finite(dk) || not_finite(dv))) != 0) pass(std::true_type());
+  // (a part: four registers a lane, lanes next to each other; dk, then dv)
+  constexpr int kPart = 64 * 16 * (DP / 32);
+  if (taken != 0) {  // the chunks' parts, every heads-th to a wavefront
+    uint32_t n = 0;
+    for (int s0 = 0; s0 < (int)slots; s0 += 64)
+      for (uint64_t left = __ballot(s0 + lane < (int)slots && numbers[min(s0 + lane, (int)slots - 1)] == col_tile); left != 0; left &= left - 1, ++n) {
+        if (n % heads != team) continue;
+        const float4* part = reinterpret_cast<const float4*>(a.far_parts + (head_slots + s0 + __builtin_ctzll(left)) * (2 * kPart)) + lane;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            const float4 x = part[64 * (4 * t + r / 4)], y = part[kPart / 4 + 64 * (4 * t + r / 4)];
+            dk[t][r] += x.x; dk[t][r + 1] += x.y; dk[t][r + 2] += x.z; dk[t][r + 3] += x.w;
+            dv[t][r] += y.x; dv[t][r + 1] += y.y; dv[t][r + 2] += y.z; dv[t][r + 3] += y.w;
+          }
+      }
+  }
   // the heads' sums, in order
   if (heads > 1) {
-    float* mine = reinterpret_cast<float*>(lds[wave]) + lane;
+    float4* mine = reinterpret_cast<float4*>(lds[wave]) + lane;
     auto gather = [&](f32x16_t (&acc)[DP / 32]) __attribute__((always_inline)) {
       __syncthreads();
       if (team != 0) {
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) mine[64 * (16 * t + r)] = acc[t][r];
+          for (int r = 0; r < 16; r += 4) mine[64 * (4 * t + r / 4)] = make_float4(acc[t][r], acc[t][r + 1], acc[t][r + 2], acc[t][r + 3]);
       }
       __syncthreads();
       if (team == 0) {
         for (uint32_t n = 1; n < heads; ++n) {
-          const float* other = reinterpret_cast<const float*>(lds[wave + n]) + lane;
+          const float4* other = reinterpret_cast<const float4*>(lds[wave + n]) + lane;
 #pragma unroll
           for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[t][r] += other[64 * (16 * t + r)];
+            for (int r = 0; r < 16; r += 4) {
+              const float4 x = other[64 * (4 * t + r / 4)];
+              acc[t][r] += x.x; acc[t][r + 1] += x.y; acc[t][r + 2] += x.z; acc[t][r + 3] += x.w;
+            }
         }
       }
     };
@@ -911,33 +947,16 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
     __syncthreads();
   }
   if (team != 0 || col_tile < 0) return;
-  // (a part: registers in order, lanes next to each other; dk, then dv)
-  constexpr int kPart = 64 * 16 * (DP / 32);
   if (far) {
-    float* part = a.far_parts + (head_slots + which) * (2 * kPart) + lane;
+    float4* part = reinterpret_cast<float4*>(a.far_parts + (head_slots + which) * (2 * kPart)) + lane;
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        part[64 * (16 * t + r)] = dk[t][r];
-        part[kPart + 64 * (16 * t + r)] = dv[t][r];
+      for (int r = 0; r < 16; r += 4) {
+        part[64 * (4 * t + r / 4)] = make_float4(dk[t][r], dk[t][r + 1], dk[t][r + 2], dk[t][r + 3]);
+        part[kPart / 4 + 64 * (4 * t + r / 4)] = make_float4(dv[t][r], dv[t][r + 1], dv[t][r + 2], dv[t][r + 3]);
       }
     return;
-  }
-  if (a.far_slots > 0) {
-    for (int64_t s0 = 0; s0 < slots; s0 += 64) {
-      uint64_t left = __ballot(s0 + lane < slots && numbers[s0 + lane] == col_tile);
-      for (; left != 0; left &= left - 1) {
-        const float* part = a.far_parts + (head_slots + s0 + __builtin_ctzll(left)) * (2 * kPart) + lane;
-#pragma unroll
-        for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            dk[t][r] += part[64 * (16 * t + r)];
-            dv[t][r] += part[kPart + 64 * (16 * t + r)];
-          }
-      }
-    }
   }
   store_rows<T, DP>(lds[wave], dk, a.scale, false, a.dk.data + my0 * a.dk.step + b * a.dk.seq + hk * a.dk.head, a.dk.step, a.T - my0, a.dk_dim);
   store_rows<T, DP>(lds[wave], dv, 1.f, false, a.dv.data + my0 * a.dv.step + b * a.dv.seq + hk * a.dv.head, a.dv.step, a.T - my0, a.dv_dim);

@@ -29,8 +29,8 @@ def positions_for(kind, T, envs, span, g):
     begun = -rand(0, 2 * span + 3, envs)[None].expand(T, envs)
     if kind == "whole":
         begun = torch.zeros_like(begun)
-    if kind in ("episodes", "ragged"):
-        ended = torch.rand((T, envs), generator=g, device="cuda") < 0.06
+    if kind in ("episodes", "ragged", "rare"):
+        ended = torch.rand((T, envs), generator=g, device="cuda") < (0.004 if kind == "rare" else 0.06)
         begun = torch.where(ended, t, begun).cummax(0).values
     p = t - begun
     if kind == "ragged":
@@ -93,7 +93,10 @@ CASES = [
     (100, 2, 2, 8, 2, 96, 96, 7, 1, "episodes", True), (128, 2, 2, 4, 4, 32, 32, 32, 2, "ragged", True), (200, 1, 2, 4, 2, 64, 64, 1000, 0, "none", False),
     (200, 2, 1, 8, 2, 128, 128, 50, 40, "going", True), (150, 2, 1, 6, 2, 40, 72, 20, 70, "episodes", True), (97, 2, 1, 5, 5, 127, 65, 11, 3, "any", True),
     (130, 2, 2, 3, 3, 5, 3, 100, 4, "any", False), (70, 1, 3, 2, 2, 100, 7, 66, 1, "ragged", False), (300, 1, 1, 4, 1, 128, 64, 64, 4, "going", False),
-    (260, 1, 1, 1, 1, 64, 128, 3, 33, "whole", False), (48, 2, 1, 7, 1, 24, 24, 16, 4, "going", True)]
+    (260, 1, 1, 1, 1, 64, 128, 3, 33, "whole", False), (48, 2, 1, 7, 1, 24, 24, 16, 4, "going", True),
+    # first steps that many tiles of rows see from beyond the window: of one episode, of several, more tiles of them than there are places, positions that do not count up
+    (900, 1, 1, 4, 1, 32, 32, 20, 4, "whole", False), (700, 2, 1, 2, 1, 64, 64, 33, 40, "rare", False), (1000, 1, 2, 6, 2, 128, 96, 50, 4, "rare", True),
+    (1500, 1, 1, 1, 1, 16, 16, 10, 400, "whole", False), (600, 1, 1, 2, 2, 32, 32, 7, 3, "any", True), (2500, 1, 1, 4, 2, 40, 40, 64, 2, "rare", False)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=NAMES.get)
