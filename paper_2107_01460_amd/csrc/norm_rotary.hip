@@ -1,8 +1,8 @@
 // The norm of each head of queries and keys with the rotation by position in the same pass, and its gradient.
 //   u = x r w,  r = 1 / sqrt(mean(x^2) + eps),  y = turn(u);   with du = turn back(dy) and g = du w:  dx = r g - x r^3 mean(g x),  dw = sum over rows of du x r
 // Bound by memory: every element in and out once; table rows, weights and the partners of a rotation come from caches.
-#include "common.h"
 #include "attention_checks.h"
+#include "lane_sums.h"
 
 namespace marl {
 namespace {
@@ -31,8 +31,9 @@ struct NormArray {
   int64_t x_step, x_seq, x_head, dy_step, dy_seq, dy_head, out_step, out_seq, out_head;  // bytes
   const float* weight;
   float* part;  // [workgroups][dim]: a workgroup's share of dw
-  Divisor heads;
-  int64_t rows;
+  uint32_t heads;
+  Divisor chunks;  // of kHeads heads: of a token
+  int64_t units;   // tokens times chunks
 };
 struct NormArgs {
   NormArray a[2];  // q, k
@@ -90,13 +91,6 @@ __device__ __forceinline__ void put(char* row, int col, int dim, const float (&f
       if (col + e < dim) p[e] = v[e];
   }
 }
-template <int L>
-__device__ __forceinline__ float sum_of(float v) {  // over L lanes next to each other, in all of them
-#pragma unroll
-  for (int m = 1; m < L; m *= 2) v += __shfl_xor(v, m);
-  return v;
-}
-
 // What a lane's E columns are to the rotation
 template <class T, bool INTER, bool WHOLE>
 struct Columns {
@@ -156,14 +150,14 @@ struct Columns {
   }
 };
 
-constexpr int kNormRows = 2;  // rows of a lane on their way together
+constexpr int kHeads = 4;  // of a token, one after another: position, table row and places are worked out once for them
 
-// L lanes take a row, a workgroup every so many runs of one array's rows.
+// L lanes take a token's heads, kHeads of them; a workgroup every so many of one array's units.
 template <class T, int L, bool INTER, bool WHOLE, bool GRADIENT>
 __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormArgs args) {
   constexpr int E = 16 / sizeof(T), kAtOnce = 256 / L;
   const bool second = blockIdx.x >= args.blocks_q;
-  const NormArray& a = args.a[second];
+  const NormArray a = second ? args.a[1] : args.a[0];
   const uint32_t block = second ? blockIdx.x - args.blocks_q : blockIdx.x, blocks = second ? gridDim.x - args.blocks_q : args.blocks_q;
   const int dim = args.dim, lane = threadIdx.x % L;
   Columns<T, INTER, WHOLE> cols{lane * E, args.rotary / 2, args.rotary};
@@ -184,79 +178,84 @@ __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormArgs args) {
   float dw[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) dw[e] = 0.f;
-  const int64_t run = (int64_t)kAtOnce * kNormRows;
-  for (int64_t first = block * run; first < a.rows; first += blocks * run) {
-    // (a run's first token and the rest by 32-bit division)
-    const int64_t token0 = first / a.heads.d;
-    const uint32_t in0 = (uint32_t)(first - token0 * a.heads.d) + threadIdx.x / L;
-    const int64_t t00 = token0 / args.B.d;
-    const uint32_t b0 = (uint32_t)(token0 - t00 * args.B.d);
-    struct Row {
-      float x[E], xp[E], dy[E], dyp[E];
-      char* out;
-      int position;
-      bool here;
-    } row[kNormRows];
+  const float each = 1.f / (float)dim;
+  const bool small = a.units < 0x7fffffff;
+  for (int64_t unit = (int64_t)block * kAtOnce + threadIdx.x / L; unit < a.units; unit += (int64_t)blocks * kAtOnce) {
+    uint32_t chunk, b;
+    int64_t t;
+    if (small) {
+      const uint32_t token = a.chunks((uint32_t)unit), row = args.B(token);
+      chunk = (uint32_t)unit - token * a.chunks.d;
+      t = row;
+      b = token - row * args.B.d;
+    } else {
+      const int64_t token = unit / a.chunks.d;
+      chunk = (uint32_t)(unit - token * a.chunks.d);
+      t = token / args.B.d;
+      b = (uint32_t)(token - t * args.B.d);
+    }
+    const int position = args.positions != nullptr ? args.positions[t * args.n_flags + args.seqs_per_flag(b)] : args.first + (int)t;
+    const uint32_t head0 = chunk * kHeads;
+    const int n = min((int)(a.heads - head0), kHeads);
+    const char* x = a.x + t * a.x_step + b * a.x_seq + head0 * a.x_head;
+    const char* dy = GRADIENT ? a.dy + t * a.dy_step + b * a.dy_seq + head0 * a.dy_head : nullptr;
+    char* out = a.out + t * a.out_step + b * a.out_seq + head0 * a.out_head;
+    float v[kHeads][E], z[kHeads][E], zp[kHeads][E];  // x; what is turned (x, or dy) and its partners
 #pragma unroll
-    for (int u = 0; u < kNormRows; ++u) {
-      Row& r = row[u];
-      const uint32_t at = in0 + u * kAtOnce, more = a.heads(at), head = at - more * a.heads.d;
-      const uint32_t bb = b0 + more, over = args.B(bb), b = bb - over * args.B.d;
-      const int64_t t = t00 + over;
-      r.here = first + u * kAtOnce + threadIdx.x / L < a.rows;
+    for (int u = 0; u < kHeads; ++u) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) r.x[e] = r.xp[e] = r.dy[e] = r.dyp[e] = 0.f;
-      r.position = -1;
-      r.out = nullptr;
-      if (!r.here) continue;
-      r.position = args.positions != nullptr ? args.positions[t * args.n_flags + args.seqs_per_flag(b)] : args.first + (int)t;
-      r.out = a.out + t * a.out_step + b * a.out_seq + head * a.out_head;
-      if (!on) continue;
-      const char* x = a.x + t * a.x_step + b * a.x_seq + head * a.x_head;
-      get<T, WHOLE>(r.x, x, col, dim);
+      for (int e = 0; e < E; ++e) v[u][e] = z[u][e] = zp[u][e] = 0.f;
+      if (u >= n || !on) continue;
+      get<T, WHOLE>(v[u], x + u * a.x_head, col, dim);
       if constexpr (!GRADIENT) {
-        cols.partners(r.x, r.xp, [&](float (&f)[E], int from) { get<T, WHOLE>(f, x, from, dim); });
+        cols.partners(v[u], zp[u], [&](float (&f)[E], int from) { get<T, WHOLE>(f, x + u * a.x_head, from, dim); });
       } else {
-        const char* dy = a.dy + t * a.dy_step + b * a.dy_seq + head * a.dy_head;
-        get<T, WHOLE>(r.dy, dy, col, dim);
-        cols.partners(r.dy, r.dyp, [&](float (&f)[E], int from) { get<T, WHOLE>(f, dy, from, dim); });
+        get<T, WHOLE>(z[u], dy + u * a.dy_head, col, dim);
+        cols.partners(z[u], zp[u], [&](float (&f)[E], int from) { get<T, WHOLE>(f, dy + u * a.dy_head, from, dim); });
+      }
+    }
+    const bool known = position < args.n_positions;
+    float c[E], s[E];
+    cols.angles(args.table + (int64_t)(known ? max(position, 0) : 0) * args.rotary, known, c, s);
+    if constexpr (!GRADIENT) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        c[e] *= w[e];
+        s[e] *= wp[e];
       }
     }
 #pragma unroll
-    for (int u = 0; u < kNormRows; ++u) {
-      Row& r = row[u];
-      float squares = 0.f;
+    for (int u = 0; u < kHeads; ++u) {
+      if (u >= n) break;
+      float squares = 0.f, y[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) squares = __builtin_fmaf(r.x[e], r.x[e], squares);
-      squares = sum_of<L>(squares);
-      const float power = squares / (float)dim + args.eps, rstd = 1.f / __builtin_sqrtf(power);
-      const bool known = r.position < args.n_positions;
-      float c[E], s[E], y[E];
-      cols.angles(args.table + (int64_t)(known ? max(r.position, 0) : 0) * args.rotary, known, c, s);
+      for (int e = 0; e < E; ++e) squares = __builtin_fmaf(v[u][e], v[u][e], squares);
+      squares = sum_lanes<L>(squares);
+      const float rstd = 1.f / __builtin_sqrtf(squares * each + args.eps);
       if constexpr (!GRADIENT) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = r.x[e] * rstd * w[e] * c[e] + r.xp[e] * rstd * wp[e] * s[e];
+        for (int e = 0; e < E; ++e) y[e] = rstd * (v[u][e] * c[e] + zp[u][e] * s[e]);
       } else {
         float g[E], du[E], dot = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          du[e] = r.dy[e] * c[e] - r.dyp[e] * s[e];
+          du[e] = z[u][e] * c[e] - zp[u][e] * s[e];
           g[e] = du[e] * w[e];
-          if (on) dot = __builtin_fmaf(g[e], r.x[e], dot);
+          if (on) dot = __builtin_fmaf(g[e], v[u][e], dot);
         }
-        dot = sum_of<L>(dot);
-        const float back = rstd * rstd * (dot / (float)dim);
+        dot = sum_lanes<L>(dot);
+        const float back = rstd * rstd * (dot * each);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          y[e] = rstd * (g[e] - r.x[e] * back);
-          if (r.position >= 0 && on) dw[e] = __builtin_fmaf(du[e], r.x[e] * rstd, dw[e]);
+          y[e] = rstd * (g[e] - v[u][e] * back);
+          if (position >= 0 && on) dw[e] = __builtin_fmaf(du[e], v[u][e] * rstd, dw[e]);
         }
       }
-      if (r.position < 0) {  // no step: zeros
+      if (position < 0) {  // no step: zeros
 #pragma unroll
         for (int e = 0; e < E; ++e) y[e] = 0.f;
       }
-      if (r.here && on) put<T, WHOLE>(r.out, col, dim, y);
+      if (on) put<T, WHOLE>(out + u * a.out_head, col, dim, y);
     }
   }
   if constexpr (GRADIENT) {
@@ -304,10 +303,10 @@ int lanes_of(int precision, int dim) {
   while (L < units) L *= 2;
   return L;
 }
-// Workgroups of an array: as many as fill the chip, each with every so many runs of rows, so that weights are read once
+// Workgroups of an array: as many as fill the chip, so that weights are read once
 constexpr int64_t kMaxBlocks = 2048;
-int64_t blocks_of(int64_t rows, int L) {
-  const int64_t run = 256 / L * kNormRows, n = (rows + run - 1) / run;
+int64_t blocks_of(int64_t units, int L) {
+  const int64_t run = 256 / L, n = (units + run - 1) / run;
   return n > kMaxBlocks ? kMaxBlocks : n;
 }
 
@@ -373,8 +372,9 @@ NormArray array_of(const marl_attention_dims& d, const marl_view& x, const marl_
   a.out_seq = out.seq * elem;
   a.out_head = out.head * elem;
   a.weight = weight;
-  a.heads = divisor((uint32_t)heads);
-  a.rows = (int64_t)d.n_steps * d.n_seqs * heads;
+  a.heads = (uint32_t)heads;
+  a.chunks = divisor((uint32_t)(heads + kHeads - 1) / kHeads);
+  a.units = (int64_t)d.n_steps * d.n_seqs * a.chunks.d;
   return a;
 }
 NormArgs args_of(const marl_attention_dims& d, float eps, const float* table, int32_t n_positions, int32_t rotary_dim, const int32_t* positions,
@@ -396,8 +396,8 @@ NormArgs args_of(const marl_attention_dims& d, float eps, const float* table, in
 int32_t run(NormArgs& a, const marl_attention_dims& d, bool gradient, bool k, hipStream_t s) {
   const int L = lanes_of(d.precision, d.dim_k), E = d.precision == 0 ? 4 : 8;
   const bool whole = d.dim_k % E == 0 && (a.inter || a.rotary / 2 % E == 0);
-  a.blocks_q = (uint32_t)blocks_of(a.a[0].rows, L);
-  const unsigned blocks = a.blocks_q + (k ? (unsigned)blocks_of(a.a[1].rows, L) : 0);
+  a.blocks_q = (uint32_t)blocks_of(a.a[0].units, L);
+  const unsigned blocks = a.blocks_q + (k ? (unsigned)blocks_of(a.a[1].units, L) : 0);
   if (d.precision == 0) (gradient ? launch_norm<float, true> : launch_norm<float, false>)(a, L, blocks, a.inter != 0, whole, s);
   else (gradient ? launch_norm<bf16_t, true> : launch_norm<bf16_t, false>)(a, L, blocks, a.inter != 0, whole, s);
   return launch_status();
@@ -489,8 +489,8 @@ int32_t marl_norm_rotary_backward(const marl_attention_dims* dims, marl_view dq_
     const int L = lanes_of(d.precision, d.dim_k);
     w.part[0] = a.a[0].part;
     w.part[1] = a.a[1].part;
-    w.n[0] = (int32_t)blocks_of(a.a[0].rows, L);
-    w.n[1] = two ? (int32_t)blocks_of(a.a[1].rows, L) : 0;
+    w.n[0] = (int32_t)blocks_of(a.a[0].units, L);
+    w.n[1] = two ? (int32_t)blocks_of(a.a[1].units, L) : 0;
   }
   if (!weights) return MARL_OK;
   w.out[0] = dq_weight;

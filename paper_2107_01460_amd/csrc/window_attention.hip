@@ -2,6 +2,7 @@
 #include <type_traits>
 
 #include "attention_checks.h"
+#include "lane_sums.h"
 #include "window_attention.h"
 
 namespace marl {
@@ -153,21 +154,11 @@ struct StepArgs {
   int64_t units;  // wavefronts
   int32_t dk, dv, window, sinks;
   float c;  // scale log2(e)
-  float* part;   // [B][H][splits][dv]
-  float2* stat;  // [B][H][splits]: largest exponent of two, sum
+  uint32_t parts;  // splits / 4: a workgroup's wavefronts take four next to each other and join them
+  float* part;     // [B][H][parts][dv]
+  float2* stat;    // [B][H][parts]: largest exponent of two, sum
 };
 
-// Sum over L lanes next to each other, in all of them
-template <int L>
-__device__ __forceinline__ float sum_lanes(float v) {
-  auto add = [&](auto control) { v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(control)::value, 0xf, 0xf, true)); };
-  if constexpr (L >= 2) add(std::integral_constant<int, 0xB1>());   // the neighbour
-  if constexpr (L >= 4) add(std::integral_constant<int, 0x4E>());   // the other pair
-  if constexpr (L >= 8) add(std::integral_constant<int, 0x141>());  // mirrored in eight
-  if constexpr (L >= 16) add(std::integral_constant<int, 0x140>()); // mirrored in sixteen
-  if constexpr (L >= 32) v += __shfl_xor(v, 16);
-  return v;
-}
 template <class T>
 __device__ __forceinline__ void widen(const uint4& u, float (&f)[16 / sizeof(T)]) {
   if constexpr (sizeof(T) == 4) {
@@ -192,6 +183,8 @@ constexpr int kStepRows = 4;  // rows of a lane on their way together
 template <class T, int L, int G>
 __global__ void __launch_bounds__(256) window_step_kernel(const StepArgs a) {
   constexpr int E = 16 / sizeof(T), R = 64 / L;
+  __shared__ float2 stats[4][G];
+  __shared__ float accs[4][G][L * E];
   const int64_t unit = (int64_t)xcd_remap(blockIdx.x, gridDim.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   if (unit >= a.units) return;
   const int lane = threadIdx.x & 63, r = lane / L, c = lane % L * E;
@@ -308,46 +301,59 @@ __global__ void __launch_bounds__(256) window_step_kernel(const StepArgs a) {
 #pragma unroll
       for (int e = 0; e < E; ++e) acc[g][e] += __shfl_xor(acc[g][e], m);
     }
-    if (r != 0 || (uint32_t)g >= heads) continue;
-    const uint32_t h = h0 + g;
     if (a.splits == 1) {
-      if (c >= a.dv) continue;
+      if (r != 0 || (uint32_t)g >= heads || c >= a.dv) continue;
       float o[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] = position < 0 ? 0.f : acc[g][e] / sum[g];
-      put_unit(reinterpret_cast<T*>(a.out + b * a.out_seq + h * a.out_head) + c, narrow<T>(o), a.dv - c);
-    } else {
-      const int64_t at = ((int64_t)b * a.H + h) * a.splits + split;
-      if (lane == 0) a.stat[at] = make_float2(most, sum[g]);
+      put_unit(reinterpret_cast<T*>(a.out + b * a.out_seq + (h0 + g) * a.out_head) + c, narrow<T>(o), a.dv - c);
+    } else if (r == 0) {
+      const int wave = threadIdx.x / 64;
+      if (lane == 0) stats[wave][g] = make_float2(most, sum[g]);
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (c + e < a.dv) a.part[at * a.dv + c + e] = acc[g][e];
+      for (int e = 0; e < E; ++e) accs[wave][g][c + e] = acc[g][e];
     }
+  }
+  if (a.splits == 1) return;
+  __syncthreads();
+  for (int at = threadIdx.x; at < (int)heads * L * E; at += 256) {
+    const int g = at / (L * E), d = at % (L * E);
+    const float most = fmaxf(fmaxf(stats[0][g].x, stats[1][g].x), fmaxf(stats[2][g].x, stats[3][g].x)), from = most == -__builtin_inff() ? 0.f : most;
+    float all = 0.f, o = 0.f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float factor = __builtin_amdgcn_exp2f(stats[u][g].x - from);
+      all = __builtin_fmaf(factor, stats[u][g].y, all);
+      o = __builtin_fmaf(factor, accs[u][g][d], o);
+    }
+    const int64_t place = ((int64_t)b * a.H + h0 + g) * a.parts + split / 4;
+    if (d == 0) a.stat[place] = make_float2(most, all);
+    if (d < a.dv) a.part[place * a.dv + d] = o;
   }
 }
 
 // The parts of a cut step, one workgroup a query head, in a fixed order: eight teams of 128 threads take every eighth part.
-constexpr int kMaxSplits = 512;
+constexpr int kMaxParts = 128;
 template <class T>
 __global__ void __launch_bounds__(1024) window_step_join_kernel(const StepArgs a) {
-  __shared__ float2 stats[kMaxSplits];
+  __shared__ float2 stats[kMaxParts];
   __shared__ float sums[8], accs[8][128];
   const int64_t pair = blockIdx.x;
   const uint32_t b = (uint32_t)(pair / a.H), h = (uint32_t)(pair % a.H);
   const int d = threadIdx.x % 128, team = threadIdx.x / 128;
   const int position = a.positions[b / a.seqs_per_flag];
-  for (uint32_t s = threadIdx.x; s < a.splits; s += 1024) stats[s] = a.stat[pair * a.splits + s];
+  for (uint32_t s = threadIdx.x; s < a.parts; s += 1024) stats[s] = a.stat[pair * a.parts + s];
   __syncthreads();
   float top = -__builtin_inff();
-  for (uint32_t s = threadIdx.x & 63; s < a.splits; s += 64) top = fmaxf(top, stats[s].x);
+  for (uint32_t s = threadIdx.x & 63; s < a.parts; s += 64) top = fmaxf(top, stats[s].x);
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
   const float from = top == -__builtin_inff() ? 0.f : top;
   float sum = 0.f, acc = 0.f;
-  const float* part = a.part + pair * a.splits * a.dv + d;
+  const float* part = a.part + pair * a.parts * a.dv + d;
   const bool on = d < a.dv;
 #pragma unroll 8
-  for (uint32_t s = team; s < a.splits; s += 8) {
+  for (uint32_t s = team; s < a.parts; s += 8) {
     const float2 x = stats[s];
     const float factor = __builtin_amdgcn_exp2f(x.x - from);
     sum = __builtin_fmaf(factor, x.y, sum);
@@ -386,7 +392,7 @@ StepPlan step_plan(const marl_attention_dims& d, int window, int sinks) {
   const int64_t whole = (int64_t)d.n_seqs * d.n_kv_heads * p.chunks, slots = (int64_t)window + sinks, least = 64 / p.lanes * kStepRows * 2;
   int64_t n = whole > 0 ? kWaves / whole : 1;
   n = n < slots / least ? n : slots / least;
-  n = n < kMaxSplits ? n : kMaxSplits;
+  n = n < 4 * kMaxParts ? n / 4 * 4 : 4 * kMaxParts;
   p.splits = (uint32_t)(n < 2 ? 1 : n);
   p.units = whole * p.splits;
   auto take = [&](int64_t bytes) {
@@ -395,7 +401,7 @@ StepPlan step_plan(const marl_attention_dims& d, int window, int sinks) {
     return here;
   };
   if (p.splits > 1) {
-    const int64_t parts = (int64_t)d.n_seqs * d.n_heads * p.splits;
+    const int64_t parts = (int64_t)d.n_seqs * d.n_heads * (p.splits / 4);
     p.part = take(parts * d.dim_v * 4);
     p.stat = take(parts * 8);
   }
@@ -678,6 +684,7 @@ int32_t marl_window_attention_step(const marl_attention_dims* dims, int32_t wind
   a.group = a.H / a.Hk;
   a.chunks = p.chunks;
   a.splits = p.splits;
+  a.parts = p.splits / 4;
   a.units = p.units;
   a.dk = d.dim_k;
   a.dv = d.dim_v;
