@@ -446,34 +446,30 @@ __device__ __forceinline__ void store_rows(char* place, const f32x16_t (&acc)[DP
 }
 
 // ---- which tiles a workgroup's rows see ------------------------------------------------------------------------------------------------
-// Tiles of cached slots first, then tiles of first steps, then the window's.
-enum { TILE_CACHE, TILE_SINK, TILE_WINDOW, TILE_NONE };
+// The window's tiles first, backwards in time: the first of them is known before the rows' positions are.  Then tiles of cached slots, then of first steps.
+enum { TILE_WINDOW, TILE_CACHE, TILE_SINK, TILE_NONE };
 struct Tile {
   int kind, at;
 };
 struct Tiles {
   // of the workgroup's rows (up to 128, two a lane)
   Row r0, r1;
-  int first_window, last_window;  // tiles
+  int first_window;               // tile
   int cached;                     // slots that hold a step
   int newest_slot, newest;        // the slot of the cache's last step, and that step
   int least;                      // the least position of a row whose episode began before step 0
   bool any_sinks;
 
-  __device__ __forceinline__ void set(const WindowArgs& a, uint32_t env, int row0, int rows) {
-    const int lane = threadIdx.x & 63;
-    r0 = row_of(a, lane < rows ? row0 + lane : a.T, env);
-    r1 = row_of(a, 64 + lane < rows ? row0 + 64 + lane : a.T, env);
-    const int top = max(r0.valid() ? r0.i : -1, r1.valid() ? r1.i : -1);
-    first_window = max(wave_min(min(r0.lo, r1.lo)), 0) / kTile;
-    last_window = wave_max(top);
-    last_window = last_window < 0 ? -1 : last_window / kTile;
-    any_sinks = a.sinks > 0 && last_window >= 0;
+  __device__ __forceinline__ void set(const WindowArgs& a, const Row& x, const Row& y, int first_position) {
+    r0 = x;
+    r1 = y;
+    first_window = max(wave_min(min(r0.lo, r1.lo)), 0) / kTile;  // (of no row: behind every tile)
+    any_sinks = a.sinks > 0 && __ballot(r0.valid() || r1.valid()) != 0;
     cached = 0;
     newest_slot = newest = 0;
     least = 0x7fffffff;
     if (a.cache_k != nullptr) {
-      const int n = __builtin_amdgcn_readfirstlane(position_of(a, 0, env));
+      const int n = __builtin_amdgcn_readfirstlane(first_position);
       least = wave_min(min(r0.valid() && r0.start < 0 ? r0.position : 0x7fffffff, r1.valid() && r1.start < 0 ? r1.position : 0x7fffffff));
       if (n > 0 && least != 0x7fffffff) {
         cached = min(n, a.sinks + a.window);
@@ -495,6 +491,11 @@ struct Tiles {
   }
   // the one behind t
   __device__ __forceinline__ Tile next(const WindowArgs& a, Tile t) const {
+    if (t.kind == TILE_WINDOW) {
+      if (--t.at >= first_window) return t;
+      t.kind = TILE_CACHE;
+      t.at = -1;
+    }
     if (t.kind == TILE_CACHE) {
       while (++t.at * kTile < cached) {
         const int slot = t.at * kTile + (threadIdx.x & 31);
@@ -510,11 +511,8 @@ struct Tiles {
         const int n = wave_min(min(sink_tile(r0, t.at + 1), sink_tile(r1, t.at + 1)));
         if (n < first_window) return {TILE_SINK, n};
       }
-      t.kind = TILE_WINDOW;
-      t.at = first_window - 1;
+      t.kind = TILE_NONE;
     }
-    ++t.at;
-    if (t.at > last_window) t.kind = TILE_NONE;
     return t;
   }
 };
@@ -544,33 +542,30 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
   const uint32_t h = hk * a.group + head_team % teams * a.heads_each + wave % a.heads_each;
   const int tiles_each = WAVES / a.heads_each, row0 = (int)block_t * tiles_each * kTile, my0 = row0 + (int)(wave / a.heads_each) * kTile;
   const int i = my0 + lane % 32;
+  // positions first, then rows and the first tile: all on their way together
+  const int rows = tiles_each * kTile;
+  const int i0 = lane < rows ? row0 + lane : a.T, i1 = 64 + lane < rows ? row0 + 64 + lane : a.T;
+  int position = a.first + i, position0 = a.first + i0, position1 = a.first + i1, first_position = a.first;
+  if (a.positions != nullptr) {
+    const int32_t* p = a.positions + env;
+    position = p[(int64_t)min(i, a.T - 1) * a.n_flags];
+    position0 = p[(int64_t)min(i0, a.T - 1) * a.n_flags];
+    position1 = p[(int64_t)min(i1, a.T - 1) * a.n_flags];
+    first_position = p[0];
+  }
   const char *kp = a.k.data + b * a.k.seq + hk * a.k.head, *vp = a.v.data + b * a.v.seq + hk * a.v.head;
   const int64_t cached_at = ((int64_t)b * a.Hk + hk) * (a.sinks + a.window);
   const char *ck = a.cache_k + cached_at * a.dk_dim * (int)sizeof(T), *cv = a.cache_v + cached_at * a.dv_dim * (int)sizeof(T);
-  typename P::Own q, d;
   typedef OwnRows<T, DP, FAST> Rows;
   const int count = a.T - my0;
+  typename P::Own q, d, o;
   P::load_own(q, Rows{a.q.data + my0 * a.q.step + b * a.q.seq + h * a.q.head, a.q.step, a.scale != 0.f ? count : 0, a.dk_dim}, a.flip);
   float lse2 = 0.f, delta = 0.f;
   const int64_t stat = ((int64_t)b * a.H + h) * a.T + i;
   if constexpr (GRADIENT) {
+    lse2 = a.lse[stat - i + min(i, a.T - 1)] * 1.44269504088896341f;
     P::load_own(d, Rows{a.dout.data + my0 * a.dout.step + b * a.dout.seq + h * a.dout.head, a.dout.step, count, a.dv_dim}, 0);
-    typename P::Own o;
     P::load_own(o, Rows{a.out.data + my0 * a.out.step + b * a.out.seq + h * a.out.head, a.out.step, count, a.dv_dim}, 0);
-    delta = P::dot(d, o);
-    const Halves both = halves(delta);
-    delta = both.lo + both.hi;
-    if (half == 0 && i < a.T) a.delta[stat] = delta;
-    if (i < a.T) lse2 = a.lse[stat] * 1.44269504088896341f;
-  }
-  Tiles tiles;
-  tiles.set(a, env, row0, tiles_each * kTile);
-  const Row row = row_of(a, i, env);
-  if constexpr (GRADIENT) {  // for dk and dv: where the episodes of each tile's rows began
-    if (h == 0 && b % a.seqs_per_flag == 0 && my0 < a.T) {
-      const int lo = wave_min(row.valid() ? row.start : 0x7fffffff), hi = wave_max(row.valid() ? row.start : -0x7fffffff);
-      if (lane == 0) a.reach[(int64_t)env * ((a.T + kTile - 1) / kTile) + my0 / kTile] = make_int2(lo, hi);
-    }
   }
   typedef Fetch<T, DP, WAVES, FAST> F;
   const int64_t ck_step = a.dk_dim * (int)sizeof(T), cv_step = a.dv_dim * (int)sizeof(T);
@@ -581,6 +576,8 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
   pcv.set(cv_step, a.dv_dim);
   // two tiles on their way
   F fk[2], fv[2];
+  Tiles tiles;
+  tiles.cached = 0;
   auto request = [&](F& k, F& v, const Tile& t) __attribute__((always_inline)) {
     const bool cache = t.kind == TILE_CACHE;
     const int n = t.kind == TILE_NONE ? 0 : (cache ? tiles.cached : a.T) - t.at * kTile;
@@ -588,6 +585,22 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
     k.request(cache ? pck : pk, cache ? ck + first * ck_step : kp + first * a.k.step, cache ? ck_step : a.k.step, n, a.dk_dim);
     v.request(cache ? pcv : pv, cache ? cv + first * cv_step : vp + first * a.v.step, cache ? cv_step : a.v.step, n, a.dv_dim);
   };
+  const Tile first_tile = {TILE_WINDOW, min(row0 / kTile + tiles_each, (a.T + kTile - 1) / kTile) - 1};
+  request(fk[0], fv[0], first_tile);
+  tiles.set(a, row_with(a, i0, i0 < a.T ? position0 : -1), row_with(a, i1, i1 < a.T ? position1 : -1), first_position);
+  const Row row = row_with(a, i, i < a.T ? position : -1);
+  if constexpr (GRADIENT) {  // for dk and dv: where the episodes of each tile's rows began
+    if (h == 0 && b % a.seqs_per_flag == 0 && my0 < a.T) {
+      const int lo = wave_min(row.valid() ? row.start : 0x7fffffff), hi = wave_max(row.valid() ? row.start : -0x7fffffff);
+      if (lane == 0) a.reach[(int64_t)env * ((a.T + kTile - 1) / kTile) + my0 / kTile] = make_int2(lo, hi);
+    }
+  }
+  if constexpr (GRADIENT) {
+    delta = P::dot(d, o);
+    const Halves both = halves(delta);
+    delta = both.lo + both.hi;
+    if (half == 0 && i < a.T) a.delta[stat] = delta;
+  }
   f32x16_t acc[DP / 32];
   float top = 0.f, sum = 0.f;  // output: the largest exponent (of two) so far, the sum of this half's weights
   auto pass = [&](auto careful) __attribute__((always_inline)) {
@@ -596,8 +609,8 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
     top = -__builtin_inff();
     sum = 0.f;
     Tile ahead[2];
-    ahead[0] = tiles.next(a, {TILE_CACHE, -1});
-    request(fk[0], fv[0], ahead[0]);
+    ahead[0] = first_tile;
+    if constexpr (decltype(careful)::value) request(fk[0], fv[0], first_tile);
     ahead[1] = tiles.next(a, ahead[0]);
     request(fk[1], fv[1], ahead[1]);
     // one tile: into LDS, the one after the next requested, the products; false behind the last
@@ -772,11 +785,6 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
     uint32_t g;
   };
   uint64_t taken = 0;  // chunks (at most 64) whose rows beyond the window are in parts
-  if (!far && on) {
-    for (int s0 = 0; s0 < (int)slots; s0 += 64)
-      for (uint64_t left = __ballot(s0 + lane < (int)slots && numbers[min(s0 + lane, (int)slots - 1)] == col_tile); left != 0; left &= left - 1)
-        taken |= 1ull << ((s0 + __builtin_ctzll(left)) / a.far_slots);
-  }
   auto look = [&](int base) __attribute__((always_inline)) {
     const int t = base + lane;
     bool needed = false;
@@ -824,14 +832,24 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
     delta = a.delta[stat];
     position = positions[a.positions != nullptr ? (int64_t)i * a.n_flags + env : 0];
   };
+  // (the rows next to the columns are always looked at: on their way before anything else is known)
+  const bool near = !far && fetches_ahead<T, DP>();
+  const Cursor beside = {col_tile, 0, col_tile < 0 ? -2 : col_tile, team};
+  if (near) request(beside);
+  if (!far && on) {
+    for (int s0 = 0; s0 < (int)slots; s0 += 64)
+      for (uint64_t left = __ballot(s0 + lane < (int)slots && numbers[min(s0 + lane, (int)slots - 1)] == col_tile); left != 0; left &= left - 1)
+        taken |= 1ull << ((s0 + __builtin_ctzll(left)) / a.far_slots);
+  }
   f32x16_t dk[DP / 32], dv[DP / 32];
   auto pass = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) dk[t] = dv[t] = (f32x16_t){0.f};
     if (col_tile < 0) return;
-    const int base = far ? first_tile : col_tile;
-    Cursor ahead = next({base, look(base), -1, team});
-    if (fetches_ahead<T, DP>()) request(ahead);
+    Cursor ahead = beside;
+    if (far) ahead = next({first_tile, look(first_tile), -1, team});
+    else ahead.left = look(col_tile) & ~1ull;
+    if (fetches_ahead<T, DP>() && (!near || decltype(careful)::value)) request(ahead);
     while (ahead.tile >= 0) {
       const Cursor now = ahead;
       if (!fetches_ahead<T, DP>()) request(now);
