@@ -205,14 +205,16 @@ struct Fetch {
   uint4 v[kEach];
   __device__ __forceinline__ static int row_at(int tid, int u) { return (tid + u * kThreads) / kUnits; }
   __device__ __forceinline__ static int unit_at(int tid, int u) { return (tid + u * kThreads) % kUnits; }
-  // rows from `rows` on, `count` of them; the others zero (or, where rows share memory, any value of theirs)
-  __device__ __forceinline__ void request(const Places& p, const char* rows, int64_t step, int count, int dim) {
+  // Of rows `step` bytes apart: tile number `tile`, `count` rows of it; the others zero (or, where rows share memory, any value of theirs)
+  __device__ __forceinline__ void request(const Places& p, const char* array, int64_t step, int tile, int count, int dim) {
     if constexpr (FAST) {
-      const int n = count < kTile ? count : kTile;
-      const Window w(rows, n > 0 ? (n - 1) * step + dim * (int)sizeof(T) : 0);
+      const char* rows = array + (uint64_t)(uint32_t)tile * (uint32_t)(kTile * (uint32_t)step);
+      const uint32_t last = (uint32_t)(count < kTile ? count - 1 : kTile - 1);
+      const Window w(rows, count > 0 ? (int)(last * (uint32_t)step + dim * (uint32_t)sizeof(T)) : 0);
 #pragma unroll
       for (int u = 0; u < kEach; ++u) v[u] = w.load(kEven ? p.at[0] + u * p.more : p.at[kEven ? 0 : u]);
     } else {
+      const char* rows = array + tile * (kTile * step);
       const int tid = fresh(threadIdx.x % kThreads);
 #pragma unroll
       for (int u = 0; u < kEach; ++u) {
@@ -581,9 +583,9 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
   auto request = [&](F& k, F& v, const Tile& t) __attribute__((always_inline)) {
     const bool cache = t.kind == TILE_CACHE;
     const int n = t.kind == TILE_NONE ? 0 : (cache ? tiles.cached : a.T) - t.at * kTile;
-    const int64_t first = t.kind == TILE_NONE ? 0 : (int64_t)t.at * kTile;
-    k.request(cache ? pck : pk, cache ? ck + first * ck_step : kp + first * a.k.step, cache ? ck_step : a.k.step, n, a.dk_dim);
-    v.request(cache ? pcv : pv, cache ? cv + first * cv_step : vp + first * a.v.step, cache ? cv_step : a.v.step, n, a.dv_dim);
+    const int at = t.kind == TILE_NONE ? 0 : t.at;
+    k.request(cache ? pck : pk, cache ? ck : kp, cache ? ck_step : a.k.step, at, n, a.dk_dim);
+    v.request(cache ? pcv : pv, cache ? cv : vp, cache ? cv_step : a.v.step, at, n, a.dv_dim);
   };
   const Tile first_tile = {TILE_WINDOW, min(row0 / kTile + tiles_each, (a.T + kTile - 1) / kTile) - 1};
   request(fk[0], fv[0], first_tile);
@@ -613,11 +615,11 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
     if constexpr (decltype(careful)::value) request(fk[0], fv[0], first_tile);
     ahead[1] = tiles.next(a, ahead[0]);
     request(fk[1], fv[1], ahead[1]);
-    // one tile: into LDS, the one after the next requested, the products; false behind the last
+    // One tile: into LDS, the one after the next requested, the products.  (The loop ends between pairs of turns only, the last turn without a tile where their number is
+    // odd: with a way out between the two, or a request on some ways only, the compiler waits for both tiles at each.)
     auto turn = [&](auto which) __attribute__((always_inline)) {
       constexpr int buffer = decltype(which)::value;
       const Tile now = ahead[buffer];
-      if (now.kind == TILE_NONE) return false;
       fk[buffer].store(tile_at(buffer, 0));
       fv[buffer].store(tile_at(buffer, 1));
       ahead[buffer] = tiles.next(a, ahead[buffer ^ 1]);
@@ -628,11 +630,11 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
       const int j0 = now.at * kTile;
       int sight = SEE_CACHE;
       if (now.kind == TILE_CACHE) {
-        if (__ballot(row.valid() && row.start < 0) == 0) return true;
+        if (__ballot(row.valid() && row.start < 0) == 0) return;
       } else {
         const int j1 = j0 + kTile - 1;
         const bool band = j1 >= row.lo && j0 <= row.i, sinks = row.start <= j1 && row.start + (int)row.n_sinks > j0 && j0 < row.lo;
-        if (__ballot(row.valid() && (band || sinks)) == 0) return true;
+        if (now.kind == TILE_NONE || __ballot(row.valid() && (band || sinks)) == 0) return;
         sight = __ballot(row.valid() && sinks) != 0 ? SEE_MORE : __ballot(row.valid() && !(j0 >= row.lo && j1 <= row.i)) != 0 ? SEE_BAND : SEE_ALL;
       }
       // (register r's column is result_row(r, half) behind the tile's first)
@@ -669,16 +671,19 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
 #pragma unroll
         for (int r = 1; r < 16; ++r) most = fmaxf(most, s[r]);
         const Halves both = halves(most);
-        const float now_top = fmaxf(top, fmaxf(both.lo, both.hi) * a.c), base = now_top == -__builtin_inff() ? 0.f : now_top;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c, -base));
-        if (__ballot(now_top != top) != 0) {
-          const float shrink = __builtin_amdgcn_exp2f(top - base);
+        // The sums are kept relative to the largest exponent within a factor of 2^8: nearly every tile holds a new largest score of one of 32 rows, few a much larger one.
+        // (A long sequence of 8 heads of 128, window 1024: MEASURED.)
+        const float new_top = fmaxf(top, fmaxf(both.lo, both.hi) * a.c);
+        if (__ballot(new_top > top + 8.f) != 0) {
+          const float shrink = __builtin_amdgcn_exp2f(top - (new_top == -__builtin_inff() ? 0.f : new_top));
           sum *= shrink;
 #pragma unroll
           for (int t = 0; t < DP / 32; ++t) acc[t] *= shrink;
+          top = new_top;
         }
-        top = now_top;
+        const float base = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c, -base));
 #pragma unroll
         for (int r = 0; r < 16; ++r) sum += p[r];
       } else {
@@ -698,10 +703,11 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
         }
         add_with_care<T, DP>(acc, y, p, seen);
       }
-      return true;
     };
-    while (turn(std::integral_constant<int, 0>()) && turn(std::integral_constant<int, 1>())) {
-    }
+    do {
+      turn(std::integral_constant<int, 0>());
+      turn(std::integral_constant<int, 1>());
+    } while (ahead[0].kind != TILE_NONE);
   };
   pass(std::false_type());
   if (__syncthreads_or(row.valid() && not_finite(acc))) pass(std::true_type());
@@ -725,8 +731,10 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
 // First steps are seen by every later row of their episode: in a long sequence far more tiles of rows than any other column, one wavefront's work.  There the pairs
 // of tiles beyond the window are cut along the rows (far): every so many tiles of rows a wavefront takes the first `far_slots` tiles of first steps that they see, into
 // fp32 parts with the tile's number beside them; the columns' own wavefronts add the parts with their number, in order, and take what was beyond the slots themselves.
+// Tiles of rows on their way: two where a wavefront has a SIMD's registers to itself anyway (the gradient of a long sequence of 8 heads of 128, window 512: MEASURED), none
+// beside the one at work where that would spill.
 template <class T, int DP>
-constexpr bool fetches_ahead() { return sizeof(T) == 2 || DP <= 64; }  // (wider ones spill)
+constexpr int tiles_ahead() { return sizeof(T) == 2 ? (DP > 64 ? 2 : 1) : DP <= 64 ? 1 : 0; }
 
 template <class T, int DP, bool FAST>
 __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_kernel(const WindowArgs a, const int far) {
@@ -817,25 +825,29 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
   typename F::Places pq, pd;
   pq.set(a.q.step, a.dk_dim);
   pd.set(a.dout.step, a.dv_dim);
-  F fq, fd;
-  float lse, delta;
-  int position;
+  const char *qp = a.q.data + b * a.q.seq, *dp = a.dout.data + b * a.dout.seq;
+  constexpr int kSets = tiles_ahead<T, DP>() > 1 ? 2 : 1;
+  struct Set {
+    F q, d;
+    float lse, delta;
+    int position;
+  } sets[kSets];
   const int32_t* positions = a.positions != nullptr ? a.positions : reinterpret_cast<const int32_t*>(a.lse);
-  auto request = [&](const Cursor& c) __attribute__((always_inline)) {
+  auto request = [&](Set& set, const Cursor& c) __attribute__((always_inline)) {
     const uint32_t h = hk * a.group + c.g;
     const int i0 = c.tile < 0 ? 0 : c.tile * kTile, n = c.tile < 0 ? 0 : a.T - i0;
-    fq.request(pq, a.q.data + i0 * a.q.step + b * a.q.seq + h * a.q.head, a.q.step, n, a.dk_dim);
-    fd.request(pd, a.dout.data + i0 * a.dout.step + b * a.dout.seq + h * a.dout.head, a.dout.step, n, a.dv_dim);
+    set.q.request(pq, qp + h * a.q.head, a.q.step, i0 / kTile, n, a.dk_dim);
+    set.d.request(pd, dp + h * a.dout.head, a.dout.step, i0 / kTile, n, a.dv_dim);
     const int i = min(i0 + lane % kTile, a.T - 1);
     const int64_t stat = ((int64_t)b * a.H + h) * a.T + i;
-    lse = a.lse[stat];
-    delta = a.delta[stat];
-    position = positions[a.positions != nullptr ? (int64_t)i * a.n_flags + env : 0];
+    set.lse = a.lse[stat];
+    set.delta = a.delta[stat];
+    set.position = positions[a.positions != nullptr ? (int64_t)i * a.n_flags + env : 0];
   };
   // (the rows next to the columns are always looked at: on their way before anything else is known)
-  const bool near = !far && fetches_ahead<T, DP>();
+  const bool near = !far && tiles_ahead<T, DP>() > 0;
   const Cursor beside = {col_tile, 0, col_tile < 0 ? -2 : col_tile, team};
-  if (near) request(beside);
+  if (near) request(sets[0], beside);
   if (!far && on) {
     for (int s0 = 0; s0 < (int)slots; s0 += 64)
       for (uint64_t left = __ballot(s0 + lane < (int)slots && numbers[min(s0 + lane, (int)slots - 1)] == col_tile); left != 0; left &= left - 1)
@@ -846,32 +858,39 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) dk[t] = dv[t] = (f32x16_t){0.f};
     if (col_tile < 0) return;
-    Cursor ahead = beside;
-    if (far) ahead = next({first_tile, look(first_tile), -1, team});
-    else ahead.left = look(col_tile) & ~1ull;
-    if (fetches_ahead<T, DP>() && (!near || decltype(careful)::value)) request(ahead);
-    while (ahead.tile >= 0) {
-      const Cursor now = ahead;
-      if (!fetches_ahead<T, DP>()) request(now);
+    Cursor ahead[kSets];
+    ahead[0] = beside;
+    if (far) ahead[0] = next({first_tile, look(first_tile), -1, team});
+    else ahead[0].left = look(col_tile) & ~1ull;
+    if (tiles_ahead<T, DP>() > 0 && (!near || decltype(careful)::value)) request(sets[0], ahead[0]);
+    if constexpr (kSets > 1) {
+      ahead[1] = next(ahead[0]);
+      request(sets[1], ahead[1]);
+    }
+    auto turn = [&](auto which) __attribute__((always_inline)) {
+      constexpr int at = decltype(which)::value;
+      Set& set = sets[at];
+      const Cursor now = ahead[at];
+      if constexpr (tiles_ahead<T, DP>() == 0) request(set, now);
       __builtin_amdgcn_wave_barrier();
-      fq.store(tile_q);
-      fd.store(tile_d);
+      set.q.store(tile_q);
+      set.d.store(tile_d);
       if (lane < kTile) {
         const int i = now.tile * kTile + lane;
-        const Row seer = row_with(a, i, i < a.T ? a.positions != nullptr ? position : a.first + i : -1);
-        stats[0][lane] = seer.valid() ? lse * 1.44269504088896341f : 0.f;
-        stats[1][lane] = seer.valid() ? delta : 0.f;
+        const Row seer = row_with(a, i, now.tile >= 0 && i < a.T ? a.positions != nullptr ? set.position : a.first + i : -1);
+        stats[0][lane] = seer.valid() ? set.lse * 1.44269504088896341f : 0.f;
+        stats[1][lane] = seer.valid() ? set.delta : 0.f;
         sight[lane] = make_int4(seer.lo, (int)seer.span, seer.start, (int)seer.n_sinks);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      ahead = next(ahead);
-      if (fetches_ahead<T, DP>()) request(ahead);
+      ahead[at] = next(ahead[(at + kSets - 1) % kSets]);
+      if constexpr (tiles_ahead<T, DP>() > 0) request(set, ahead[at]);
       // (a row's last step is lo + span; rows that hold no step see nothing: lo above every column)
       const int4 w = sight[lane % 32];
       const int last = w.x == 0x7fffffff ? -1 : w.x + w.y;
       const bool whole = w.x <= my0 && my1 <= last, band = w.x <= my1 && my0 <= last, sinks = (int64_t)w.z + w.w > my0 && w.z <= my1;
-      if (__ballot(band || sinks) == 0) continue;
+      if (__ballot(band || sinks) == 0) return;
       const bool masked = __ballot(!whole) != 0, more = __ballot(sinks) != 0;
       auto for_seen = [&](auto f) __attribute__((always_inline)) {  // f(register, whether its row sees the lane's column)
         const int4* from = sight + 4 * fresh(half);
@@ -913,6 +932,10 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
         add_with_care<T, DP>(dv, tile_d, p, seen);
         add_with_care<T, DP>(dk, tile_q, ds, seen);
       }
+    };
+    while (ahead[0].tile >= 0) {
+      turn(std::integral_constant<int, 0>());
+      if constexpr (kSets > 1) turn(std::integral_constant<int, 1>());
     }
   };
   pass(std::false_type());

@@ -41,7 +41,7 @@ Plan plan_of(const marl_attention_dims& d, int window, int sinks, bool fast) {
   p.cols = workgroups((int64_t)pairs * p.tiles);
   // First steps seen from afar are cut along the rows where columns are few (else others keep the chip busy meanwhile) and eight tiles or more lie beyond the window
   if (sinks > 0 && (int64_t)pairs * p.tiles <= 8192 && p.tiles > window / kTile + 10) {
-    p.far_tiles = p.tiles > 256 ? (p.tiles + 31) / 32 : 8;
+    p.far_tiles = p.tiles > 256 ? (p.tiles + 63) / 64 : 4;
     p.far_chunks = (uint32_t)((p.tiles + p.far_tiles - 1) / p.far_tiles);
     p.far_slots = (uint32_t)(sinks / kTile + 3 < 8 ? sinks / kTile + 3 : 8);
     p.far = workgroups((int64_t)pairs * p.far_chunks * p.far_slots);
