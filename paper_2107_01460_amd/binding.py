@@ -468,6 +468,7 @@ def linear_attention_backward(q, k, v, decay, dout, dq, dk, dv, workspace=None, 
 def linear_attention_step(q, k, v, decay, state, out, next_state=None, done=None, scale=1.0, stream=None):
     """One step: q [B][Hq][Dk], k, v [B][Hk][D], out [B][Hq][Dv]; done [environments]: of the step before (the state is cleared).  The state is
     updated in place unless next_state is given."""
+    _here(q, k, v, *cache, positions, out, workspace)
     precision, dt = _PRECISION.get(q.dtype), q.dtype
     if precision is None or q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
         raise _refused("q, k, v: float32 or bfloat16 [B][heads][D]")
@@ -569,6 +570,18 @@ def _positions(t, lead, B):
     return t.data_ptr(), B // n if B else 1
 
 
+def _here(*tensors):
+    """Tensors (or None) that the current GPU's kernels can use: those of another are refused, whatever its memory is to this one."""
+    current = -1
+    for t in tensors:
+        if t is not None:
+            at = t.get_device()
+            if at != current or at < 0:
+                if at < 0 or current >= 0 or at != torch.cuda.current_device():
+                    raise _refused("tensors are on the GPU that is the current one")
+                current = at
+
+
 def _norm_dims(q, k, table, positions):
     """(dims, shapes of q and of k, table rows, rotated elements, positions' pointer) of arrays [T][B][heads][D]; k may be None"""
     precision = _PRECISION.get(q.dtype)
@@ -585,6 +598,7 @@ def _norm_dims(q, k, table, positions):
 def norm_rotary(q, k, q_weight, k_weight, table, q_out, k_out, eps=1e-6, positions=None, first_position=0, interleaved=False, stream=None):
     """Every head of q and k divided by the root of its mean square and weighted, then rotated as by rotary(); weights (and k, k_out) may be None.  Rows of
     negative positions: zeros.  The outputs may be the inputs."""
+    _here(q, k, q_weight, k_weight, table, q_out, k_out, positions)
     dims, qs, ks, P, R, at = _norm_dims(q, k, table, positions)
     dt, D, none = q.dtype, q.shape[3], View()
     _check(lib().marl_norm_rotary(
@@ -607,6 +621,7 @@ def norm_rotary_workspace(q, k):
 def norm_rotary_backward(dq_out, dk_out, q, k, q_weight, k_weight, table, dq, dk, dq_weight=None, dk_weight=None, workspace=None, eps=1e-6, positions=None,
                          first_position=0, interleaved=False, stream=None):
     """dq, dk and the weights' gradients dq_weight, dk_weight (may be None) of norm_rotary from those of its outputs."""
+    _here(dq_out, dk_out, q, k, q_weight, k_weight, table, dq, dk, dq_weight, dk_weight, workspace, positions)
     dims, qs, ks, P, R, at = _norm_dims(q, k, table, positions)
     dt, D, none, need, L = q.dtype, q.shape[3], View(), C.c_int64(), lib()
     if dq_weight is not None or dk_weight is not None:
@@ -650,6 +665,8 @@ def _window_dims(q, k, v, positions, scale):
 def window_attention_workspace(q, k, v, window, sinks=0, kind="forward"):
     """Bytes of workspace that window_attention ("forward"), its gradient ("backward") or a step ("step") needs for arrays of these shapes, [T][B][heads][D]
     (of a step [B][heads][D] or [1][B][heads][D])."""
+    if kind not in WINDOW_CALLS:
+        raise _refused(f"kind: one of {list(WINDOW_CALLS)}")
     if kind == "step" and q.dim() == 3:
         q, k, v = q[None], k[None], v[None]
     n = C.c_int64()
@@ -661,6 +678,7 @@ def window_attention(q, k, v, out, window, sinks=0, lse=None, positions=None, fi
                      stream=None):
     """out [T][B][Hq][Dv] (and lse [B][Hq][T]) of attention over the last `window` steps of an episode and its first `sinks`; positions [T][environments]: each
     row's step in its episode, negative for none.  cache, next_cache: (keys, values) before and behind the call, [B][Hk][sinks + window][D]."""
+    _here(q, k, v, out, lse, positions, workspace, *(cache or ()), *(next_cache or ()))
     dims, T, B, H, Hk, Dk, Dv, at = _window_dims(q, k, v, positions, scale)
     dt, shape = q.dtype, (B, Hk, sinks + window)
     before = _cache(cache, shape, Dk, Dv, dt, "cache")
@@ -674,6 +692,7 @@ def window_attention(q, k, v, out, window, sinks=0, lse=None, positions=None, fi
 def window_attention_backward(q, k, v, out, lse, dout, dq, dk, dv, window, sinks=0, positions=None, first_position=0, cache=None, scale=1.0, workspace=None,
                               stream=None):
     """Gradients dq, dk, dv of window_attention from dout and what it kept; the cache's steps are constants."""
+    _here(q, k, v, out, lse, dout, dq, dk, dv, positions, workspace, *(cache or ()))
     dims, T, B, H, Hk, Dk, Dv, at = _window_dims(q, k, v, positions, scale)
     dt, need, L = q.dtype, C.c_int64(), lib()
     qs, ks, vs, os = (T, B, H, Dk), (T, B, Hk, Dk), (T, B, Hk, Dv), (T, B, H, Dv)
@@ -687,6 +706,7 @@ def window_attention_backward(q, k, v, out, lse, dout, dq, dk, dv, window, sinks
 
 def window_attention_step(q, k, v, cache, positions, out, window, sinks=0, scale=1.0, workspace=None, stream=None):
     """One step: q [B][Hq][Dk], k, v [B][Hk][D], out [B][Hq][Dv], positions [environments].  k and v go into the cache, which is read with them."""
+    _here(q, k, v, *cache, positions, out, workspace)
     precision, dt = _PRECISION.get(q.dtype), q.dtype
     if precision is None or q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
         raise _refused("q, k, v: float32 or bfloat16 [B][heads][D]")

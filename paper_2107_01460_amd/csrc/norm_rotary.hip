@@ -456,7 +456,7 @@ int32_t marl_norm_rotary_backward(const marl_attention_dims* dims, marl_view dq_
   MARL_CHECK(check_vector(dq_weight));
   MARL_CHECK(check_vector(dk_weight));
   if (dq_weight != nullptr && dq_weight == dk_weight) return MARL_E_CONFIG;
-  const bool weights = dq_weight != nullptr || (two && dk_weight != nullptr);
+  const bool weights = dq_weight != nullptr || ((two || !used) && dk_weight != nullptr);
   const marl_view in[2] = {q, k}, grad[2] = {dq_out, dk_out}, out[2] = {dq, dk};
   if (used) {
     MARL_CHECK(check_turn(d, eps, table, n_positions, rotary_dim, positions, first_position, interleaved));
@@ -476,11 +476,11 @@ int32_t marl_norm_rotary_backward(const marl_attention_dims* dims, marl_view dq_
     }
   }
   hipStream_t s = (hipStream_t)stream;
-  NormArgs a = args_of(d, eps, table, n_positions, rotary_dim, positions, first_position, interleaved);
   const int64_t half = (kMaxBlocks * d.dim_k * 4 + 255) / 256 * 256;
   WeightArgs w{};
   w.dim = d.dim_k;
   if (used) {
+    NormArgs a = args_of(d, eps, table, n_positions, rotary_dim, positions, first_position, interleaved);
     a.a[0] = array_of(d, q, &dq_out, dq, d.n_heads, q_weight);
     if (two) a.a[1] = array_of(d, k, &dk_out, dk, d.n_kv_heads, k_weight);
     if (dq_weight != nullptr) a.a[0].part = static_cast<float*>(workspace);
@@ -494,7 +494,7 @@ int32_t marl_norm_rotary_backward(const marl_attention_dims* dims, marl_view dq_
   }
   if (!weights) return MARL_OK;
   w.out[0] = dq_weight;
-  w.out[1] = two ? dk_weight : nullptr;
+  w.out[1] = two || !used ? dk_weight : nullptr;  // (an array of no elements has no address)
   hipLaunchKernelGGL(norm_weight_kernel, dim3((d.dim_k + 31) / 32, 2), dim3(1024), 0, s, w);
   return launch_status();
 }

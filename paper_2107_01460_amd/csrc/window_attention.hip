@@ -559,8 +559,9 @@ int32_t marl_window_attention(const marl_attention_dims* dims, int32_t window, i
   if (nk.meets(nv) || nk.meets(cv) || nv.meets(ck) || (!in_place && (nk.meets(ck) || nv.meets(cv)))) return MARL_E_CONFIG;
   if (used) {
     if (ck.holds(out.data) || cv.holds(out.data) || ck.holds(lse) || cv.holds(lse)) return MARL_E_CONFIG;
-    for (const void* x : {q.data, k.data, v.data, out.data, (void*)lse})
+    for (const void* x : {q.data, k.data, v.data, out.data, (void*)lse, (void*)positions})
       if (nk.holds(x) || nv.holds(x)) return MARL_E_CONFIG;
+    if (out.data == positions) return MARL_E_CONFIG;
     for (const void* x : {q.data, k.data, v.data, out.data, (void*)positions})
       if (lse != nullptr && x == lse) return MARL_E_CONFIG;
   }
@@ -669,6 +670,7 @@ int32_t marl_window_attention_step(const marl_attention_dims* dims, int32_t wind
   const StepPlan p = step_plan(d, window, sinks);
   if (p.bytes > 0) MARL_REQUIRE_PTR(workspace);
   MARL_CHECK(check_places(out, {q, k, v}, true));
+  if (out.data == positions) return MARL_E_CONFIG;
   const int64_t slots = (int64_t)window + sinks;
   const Extent ck = cached(d, cache.keys, slots, d.dim_k), cv = cached(d, cache.values, slots, d.dim_v);
   if (ck.meets(cv)) return MARL_E_CONFIG;
