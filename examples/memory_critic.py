@@ -1,10 +1,10 @@
 """A critic with a memory, fitted to the returns of rollouts, then used step by step as an acting loop would.
 
-    python examples/memory_critic.py [--envs 256] [--steps 64] [--iterations 30] [--bf16]
+    python examples/memory_critic.py [--envs 256] [--steps 64] [--iterations 30] [--bf16] [--window 16 [--sinks 2]]
 
 Environments are rolled out by the library (random-initialised policy), advantages and returns come from marl_compute_gae; the critic learns the
 returns from whole rollouts (linear attention, rotary positions and layer norms with their gradients) and then values the same rollout one
-step at a time from its states.
+step at a time from its states.  With --window it looks at the last steps of the episode and its first ones in place of a state with decays.
 """
 import argparse
 import os
@@ -21,7 +21,7 @@ import workloads as W
 from paper_2107_01460_amd.trainer import init_params
 
 
-def run(envs=256, steps=64, iterations=30, dtype=torch.float32, seed=0, say=print):
+def run(envs=256, steps=64, iterations=30, dtype=torch.float32, seed=0, say=print, window=None, sinks=0):
     """(loss of the first iteration, of the last, largest difference between whole and stepwise values)"""
     cfg = W.scaled(W.CONFIGS[1], n_envs=envs, rollout_len=steps, n_minibatches=1)
     sizes = M.query_sizes(cfg)
@@ -29,7 +29,7 @@ def run(envs=256, steps=64, iterations=30, dtype=torch.float32, seed=0, say=prin
     params, ws = init_params(cfg, seed).cuda(), M.alloc_workspace(sizes.rollout_workspace_bytes)
     M.env_reset(cfg, state)
     torch.manual_seed(seed)
-    critic = M.MemoryCritic(sizes.obs_dim, width=128, heads=4, kv_heads=2, max_episode=cfg["episode_cap"], dtype=dtype)
+    critic = M.MemoryCritic(sizes.obs_dim, width=128, heads=4, kv_heads=2, max_episode=cfg["episode_cap"], dtype=dtype, window=window, sinks=sinks)
     optimiser = torch.optim.Adam(critic.parameters(), lr=1e-3)
     memory = critic.initial_state(envs * cfg["n_agents"])
     losses = []
@@ -65,5 +65,7 @@ if __name__ == "__main__":
     p.add_argument("--steps", type=int, default=64)
     p.add_argument("--iterations", type=int, default=30)
     p.add_argument("--bf16", action="store_true")
+    p.add_argument("--window", type=int)
+    p.add_argument("--sinks", type=int, default=0)
     a = p.parse_args()
-    run(a.envs, a.steps, a.iterations, torch.bfloat16 if a.bf16 else torch.float32)
+    run(a.envs, a.steps, a.iterations, torch.bfloat16 if a.bf16 else torch.float32, window=a.window, sinks=a.sinks)

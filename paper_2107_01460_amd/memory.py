@@ -1,7 +1,8 @@
 """A critic with a memory on top of the sequence operators: what an agent saw earlier in its episode counts for the value of a step.
 
 The memory is linear attention with a decay for each head, on queries and keys turned by rotary positions (the step in the episode), between
-layer norms.  It has two forms with the same parameters: ``forward`` takes whole rollouts, [T][B][D] observations with the done flags of a
+layer norms; or, with ``window``, attention over the last steps of the episode and its first ones, on queries and keys normed by head and turned.  It has two
+forms with the same parameters: ``forward`` takes whole rollouts, [T][B][D] observations with the done flags of a
 trajectory, and has gradients; ``step`` takes one step of every sequence and a state of constant size, as an acting loop does.  The norms, the
 rotation and the attention run in the library's kernels; the projections between them are plain products of torch.  The kernels have first derivatives;
 asking for a second raises.
@@ -90,6 +91,58 @@ class Rotate(torch.autograd.Function):
         return q_out, k_out, None, None
 
 
+class NormRotate(torch.autograd.Function):
+    """Each head of q and k [T][B][heads][D] normed by the root of its mean square, weighted, and turned by its position."""
+
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, table, positions, eps):
+        q, k = _rows(q), _rows(k)
+        q_out, k_out = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k))
+        B.norm_rotary(q, k, q_weight, k_weight, table, q_out, k_out, eps=eps, positions=positions)
+        ctx.save_for_backward(q, k, q_weight, k_weight, table, positions)
+        ctx.eps = eps
+        return q_out, k_out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq_out, dk_out):
+        q, k, q_weight, k_weight, table, positions = ctx.saved_tensors
+        dq, dk = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k))
+        dqw, dkw = torch.empty_like(q_weight), torch.empty_like(k_weight)
+        B.norm_rotary_backward(_rows(dq_out), _rows(dk_out), q, k, q_weight, k_weight, table, dq, dk, dqw, dkw, B.alloc_workspace(B.norm_rotary_workspace(q, k)),
+                               eps=ctx.eps, positions=positions)
+        return dq, dk, dqw, dkw, None, None, None
+
+
+class AttendWindow(torch.autograd.Function):
+    """(out, state behind it) of attention over the last `window` steps and the first `sinks` of an episode; gradients of q, k, v.  state
+    [2][B][kv heads][sinks + window][D]: the cache's keys and values, constants of the gradient, or None where every episode begins in the call."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, state, positions, window, sinks, scale):
+        q, k, v = _rows(q), _rows(k), _rows(v)
+        T, n, H, D = q.shape
+        out = torch.empty((T, n, H, D), dtype=q.dtype, device=q.device)
+        lse = torch.empty((n, H, T), dtype=torch.float32, device=q.device)
+        after = torch.zeros((2, n, k.shape[2], sinks + window, D), dtype=q.dtype, device=q.device)     # the call leaves slots that hold no step as they were
+        B.window_attention(q, k, v, out, window, sinks, lse=lse, positions=positions, cache=None if state is None else (state[0], state[1]),
+                           next_cache=(after[0], after[1]), scale=scale)
+        ctx.save_for_backward(q, k, v, out, lse, state, positions)
+        ctx.looks = window, sinks, scale
+        ctx.mark_non_differentiable(after)
+        return out, after
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout, _):
+        q, k, v, out, lse, state, positions = ctx.saved_tensors
+        window, sinks, scale = ctx.looks
+        dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
+        B.window_attention_backward(q, k, v, out, lse, _rows(dout), dq, dk, dv, window, sinks, positions=positions, cache=None if state is None else (state[0], state[1]),
+                                    scale=scale, workspace=B.alloc_workspace(B.window_attention_workspace(q, k, v, window, sinks, kind="backward")))
+        return dq, dk, dv, None, None, None, None, None
+
+
 def episode_positions(done, first):
     """[T][N] int32 step in its episode of every step of a rollout: `first` [N] at step 0, 0 behind a step whose done is nonzero."""
     T = done.shape[0]
@@ -105,19 +158,24 @@ def episode_positions(done, first):
 class MemoryCritic(torch.nn.Module):
     """Value of every step from the steps of its episode up to it.
 
-    width: of the residual stream (a multiple of heads).  horizon: the heads' decays are 1 - 1 / h with h from 4 to it, in equal ratios."""
+    width: of the residual stream (a multiple of heads).  horizon: the heads' decays are 1 - 1 / h with h from 4 to it, in equal ratios.
 
-    def __init__(self, obs_dim, width=64, heads=4, kv_heads=None, layers=2, max_episode=1024, horizon=256, dtype=torch.float32, device="cuda"):
+    window: attention over that many last steps, the present one among them, and the episode's first `sinks`, in place of a state with decays.  A state then holds
+    those steps' keys and values, and positions alone tell what it holds: the step in its episode, also of the first step of a call, and 0 where one begins."""
+
+    def __init__(self, obs_dim, width=64, heads=4, kv_heads=None, layers=2, max_episode=1024, horizon=256, dtype=torch.float32, device="cuda", window=None, sinks=0):
         super().__init__()
         kv_heads = heads if kv_heads is None else kv_heads
         if width % heads or heads % kv_heads:
             raise B.MarlError("width is a multiple of heads, heads of kv_heads")
         if not 2 <= width // heads <= 128:
             raise B.MarlError(f"heads of {width // heads}: 2 to 128")
+        if window is None and sinks or window is not None and (window < 1 or sinks < 0 or window + sinks > 1 << 30):
+            raise B.MarlError("window is 1 or more, sinks 0 or more (with a window), together 2^30 at most")
         device = torch.device(device)
         if device.type == "cuda" and device.index not in (None, torch.cuda.current_device()):
             raise B.MarlError(f"{device} is not the current GPU, where the kernels run (torch.cuda.set_device)")
-        self.heads, self.kv_heads, self.dim, self.dtype = heads, kv_heads, width // heads, dtype
+        self.heads, self.kv_heads, self.dim, self.dtype, self.window, self.sinks = heads, kv_heads, width // heads, dtype, window, sinks
         h = 4.0 * (horizon / 4.0) ** (torch.arange(heads, dtype=torch.float64) / max(heads - 1, 1))
         self.register_buffer("decay", (1 - 1 / h).float().to(device))
         self.register_buffer("table", B.rotary_table(max_episode + 1, self.dim // 2 * 2))
@@ -131,6 +189,8 @@ class MemoryCritic(torch.nn.Module):
             m.norm_w, m.norm_b, m.norm2_w, m.norm2_b = ones(), zeros(), ones(), zeros()
             m.qkv = lin(width, (heads + 2 * kv_heads) * self.dim)
             m.out, m.up, m.down = lin(width, width), lin(width, 2 * width), lin(2 * width, width)
+            if window is not None:
+                m.q_norm, m.k_norm = (torch.nn.Parameter(torch.ones(self.dim, device=device)) for _ in range(2))
             self.layers.append(m)
         self.norm_w, self.norm_b = ones(), zeros()
         self.value = lin(width, 1)
@@ -139,9 +199,11 @@ class MemoryCritic(torch.nn.Module):
         return torch.nn.functional.linear(x, layer.weight.to(self.dtype), layer.bias.to(self.dtype))
 
     def initial_state(self, sequences):
-        """One state per layer, all zero."""
-        shape = (sequences, self.heads, self.dim, self.dim)
-        return [torch.zeros(shape, dtype=torch.float32, device=self.decay.device) for _ in self.layers]
+        """One state per layer, all zero: [B][heads][D][D] fp32, or with a window [2][B][kv heads][sinks + window][D] keys and values."""
+        shape, dtype = (sequences, self.heads, self.dim, self.dim), torch.float32
+        if self.window is not None:
+            shape, dtype = (2, sequences, self.kv_heads, self.sinks + self.window, self.dim), self.dtype
+        return [torch.zeros(shape, dtype=dtype, device=self.decay.device) for _ in self.layers]
 
     def _heads(self, m, y):
         """q, k, v as views of one product's columns."""
@@ -150,20 +212,26 @@ class MemoryCritic(torch.nn.Module):
         return qkv.split([self.heads, self.kv_heads, self.kv_heads], dim=-2)
 
     def _rest(self, m, x, out):
-        """Behind the memory: each head normed by itself, then the layer's own two products."""
-        out = LayerNorm.apply(out, None, None, 1e-5).flatten(-2)
-        x = x + self._product(m.out, out)
+        """Behind the memory: each head normed by itself (a window's outputs are means of values already), then the layer's own two products."""
+        if self.window is None:
+            out = LayerNorm.apply(out, None, None, 1e-5)
+        x = x + self._product(m.out, out.flatten(-2))
         y = LayerNorm.apply(x, m.norm2_w, m.norm2_b, 1e-5)
         return x + self._product(m.down, torch.nn.functional.gelu(self._product(m.up, y)))
 
     def forward(self, obs, positions, done=None, state=None):
-        """Values [T][B] fp32 and the states behind the last step, from obs [T][B][D], positions and done [T][environments]."""
+        """Values [T][B] fp32 and the states behind the last step, from obs [T][B][D], positions and done [T][environments] (a window goes by positions alone: negative
+        ones, of rows behind a recording's end, take no part)."""
         x = self._product(self.embed, obs.to(self.dtype))
         after = []
         for n, m in enumerate(self.layers):
             q, k, v = self._heads(m, LayerNorm.apply(x, m.norm_w, m.norm_b, 1e-5))
-            q, k = Rotate.apply(q, k, self.table, positions)
-            out, s = Attend.apply(q, k, v, self.decay, None if state is None else state[n], done, 1 / math.sqrt(self.dim))
+            if self.window is None:
+                q, k = Rotate.apply(q, k, self.table, positions)
+                out, s = Attend.apply(q, k, v, self.decay, None if state is None else state[n], done, 1 / math.sqrt(self.dim))
+            else:
+                q, k = NormRotate.apply(q, k, m.q_norm, m.k_norm, self.table, positions, 1e-6)
+                out, s = AttendWindow.apply(q, k, v, None if state is None else state[n], positions, self.window, self.sinks, 1 / math.sqrt(self.dim))
             after.append(s)
             x = self._rest(m, x, out)
         return self._product(self.value, LayerNorm.apply(x, self.norm_w, self.norm_b, 1e-5)).squeeze(-1).float(), after
@@ -174,8 +242,14 @@ class MemoryCritic(torch.nn.Module):
         x = self._product(self.embed, obs.to(self.dtype))
         for n, m in enumerate(self.layers):
             q, k, v = self._heads(m, LayerNorm.apply(x, m.norm_w, m.norm_b, 1e-5))
-            q, k = Rotate.apply(q[None], k[None], self.table, positions[None])
-            out = torch.empty((*q.shape[1:3], self.dim), dtype=self.dtype, device=x.device)
-            B.linear_attention_step(q[0], k[0], v, self.decay, state[n], out, done=done, scale=1 / math.sqrt(self.dim))
+            out = torch.empty((*q.shape[:2], self.dim), dtype=self.dtype, device=x.device)
+            if self.window is None:
+                q, k = Rotate.apply(q[None], k[None], self.table, positions[None])
+                B.linear_attention_step(q[0], k[0], v, self.decay, state[n], out, done=done, scale=1 / math.sqrt(self.dim))
+            else:
+                q, k = NormRotate.apply(q[None], k[None], m.q_norm, m.k_norm, self.table, positions[None], 1e-6)
+                need = B.window_attention_workspace(q, k, v[None], self.window, self.sinks, kind="step")
+                B.window_attention_step(q[0], k[0], v, (state[n][0], state[n][1]), positions, out, self.window, self.sinks, scale=1 / math.sqrt(self.dim),
+                                        workspace=B.alloc_workspace(need) if need else None)
             x = self._rest(m, x, out)
         return self._product(self.value, LayerNorm.apply(x, self.norm_w, self.norm_b, 1e-5)).squeeze(-1).float()
