@@ -460,12 +460,16 @@ struct Tiles {
   int cached;                     // slots that hold a step
   int newest_slot, newest;        // the slot of the cache's last step, and that step
   int least;                      // the least position of a row whose episode began before step 0
+  int all_from, all_to;           // tiles that every row sees whole
   bool any_sinks;
 
   __device__ __forceinline__ void set(const WindowArgs& a, const Row& x, const Row& y, int first_position) {
     r0 = x;
     r1 = y;
     first_window = max(wave_min(min(r0.lo, r1.lo)), 0) / kTile;  // (of no row: behind every tile)
+    const int most = wave_max(max(r0.valid() ? r0.lo : -0x7fffffff, r1.valid() ? r1.lo : -0x7fffffff));
+    all_from = max(most, 0) / kTile + (max(most, 0) % kTile != 0);
+    all_to = (wave_min(min(r0.valid() ? r0.i : 0x7ffffffe, r1.valid() ? r1.i : 0x7ffffffe)) + 1) / kTile - 1;
     any_sinks = a.sinks > 0 && __ballot(r0.valid() || r1.valid()) != 0;
     cached = 0;
     newest_slot = newest = 0;
@@ -617,19 +621,29 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
     request(fk[1], fv[1], ahead[1]);
     // One tile: into LDS, the one after the next requested, the products.  (The loop ends between pairs of turns only, the last turn without a tile where their number is
     // odd: with a way out between the two, or a request on some ways only, the compiler waits for both tiles at each.)
-    auto turn = [&](auto which) __attribute__((always_inline)) {
+    // Within the window, where every row sees whole tiles, nothing is looked at on the way (inside).
+    auto turn = [&](auto which, auto within) __attribute__((always_inline)) {
       constexpr int buffer = decltype(which)::value;
+      constexpr bool inside = decltype(within)::value;
       const Tile now = ahead[buffer];
       fk[buffer].store(tile_at(buffer, 0));
       fv[buffer].store(tile_at(buffer, 1));
-      ahead[buffer] = tiles.next(a, ahead[buffer ^ 1]);
-      request(fk[buffer], fv[buffer], ahead[buffer]);
+      if constexpr (inside) {
+        ahead[buffer].at -= 2;
+        fk[buffer].request(pk, kp, a.k.step, ahead[buffer].at, kTile, a.dk_dim);
+        fv[buffer].request(pv, vp, a.v.step, ahead[buffer].at, kTile, a.dv_dim);
+      } else {
+        ahead[buffer] = tiles.next(a, ahead[buffer ^ 1]);
+        request(fk[buffer], fv[buffer], ahead[buffer]);
+      }
       __syncthreads();
       // What each lane's row sees of the tile, as simply as all rows allow: all of it, the steps from one on to another, or more
       enum { SEE_ALL, SEE_BAND, SEE_MORE, SEE_CACHE };
       const int j0 = now.at * kTile;
       int sight = SEE_CACHE;
-      if (now.kind == TILE_CACHE) {
+      if constexpr (inside) {
+        sight = SEE_ALL;
+      } else if (now.kind == TILE_CACHE) {
         if (__ballot(row.valid() && row.start < 0) == 0) return;
       } else {
         const int j1 = j0 + kTile - 1;
@@ -672,7 +686,7 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
         for (int r = 1; r < 16; ++r) most = fmaxf(most, s[r]);
         const Halves both = halves(most);
         // The sums are kept relative to the largest exponent within a factor of 2^8: nearly every tile holds a new largest score of one of 32 rows, few a much larger one.
-        // (A long sequence of 8 heads of 128, window 1024: MEASURED.)
+        // (A long sequence of 8 heads of 128, window 1024: 219 us against 243 with every new one.)
         const float new_top = fmaxf(top, fmaxf(both.lo, both.hi) * a.c);
         if (__ballot(new_top > top + 8.f) != 0) {
           const float shrink = __builtin_amdgcn_exp2f(top - (new_top == -__builtin_inff() ? 0.f : new_top));
@@ -704,9 +718,18 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
         add_with_care<T, DP>(acc, y, p, seen);
       }
     };
+    constexpr std::integral_constant<int, 0> even;
+    constexpr std::integral_constant<int, 1> odd;
     do {
-      turn(std::integral_constant<int, 0>());
-      turn(std::integral_constant<int, 1>());
+      if constexpr (!decltype(careful)::value && !GRADIENT) {
+        // (the two tiles on their way, and the two that follow them)
+        while (ahead[0].kind == TILE_WINDOW && ahead[0].at <= tiles.all_to && ahead[0].at - 1 >= tiles.all_from && ahead[0].at - 3 >= tiles.first_window) {
+          turn(even, std::true_type());
+          turn(odd, std::true_type());
+        }
+      }
+      turn(even, std::false_type());
+      turn(odd, std::false_type());
     } while (ahead[0].kind != TILE_NONE);
   };
   pass(std::false_type());
@@ -750,9 +773,15 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
   const uint32_t heads = a.heads_each, units_each = 4 / heads, team = wave % heads;
   const int n_tiles = (a.T + kTile - 1) / kTile;
   const uint32_t per_head = far ? a.far_chunks * a.far_slots : (uint32_t)n_tiles;  // units of a key head
-  const int64_t unit = (int64_t)xcd_order(blockIdx.x, gridDim.x, (a.Hk * per_head + units_each - 1) / units_each, a.B) * units_each + wave / heads;
+  // neighbouring heads, then sequences, 64 of them where there are as many, then tiles: wavefronts at work together read along a step's sequences more than along time
+  // (128 x 4096 steps of 4 heads of 32 in fp32, steps 2 MB apart: 692 us against 766 with a sequence's tiles next to each other)
+  const int64_t unit = (int64_t)xcd_order(blockIdx.x, gridDim.x, (a.Hk + units_each - 1) / units_each, a.B) * units_each + wave / heads;
   const bool on = unit < (int64_t)a.B * a.Hk * per_head;
-  const uint32_t hk = on ? (uint32_t)(unit % a.Hk) : 0, which = on ? (uint32_t)(unit / a.Hk % per_head) : 0, b = on ? (uint32_t)(unit / a.Hk / per_head) : 0;
+  const uint32_t hk = on ? (uint32_t)(unit % a.Hk) : 0;
+  const uint32_t together = a.B < 64 ? 1 : 64;
+  const int64_t pair = on ? unit / a.Hk : 0, turn_of = pair / ((int64_t)together * per_head);
+  const uint32_t in_turn = (uint32_t)(pair - turn_of * together * per_head), seqs = min(together, a.B - (uint32_t)turn_of * together);
+  const uint32_t which = in_turn / seqs, b = (uint32_t)turn_of * together + in_turn % seqs;
   const uint32_t env = b / a.seqs_per_flag;
   const int2* reach = a.reach + (int64_t)env * n_tiles;
   const int64_t slots = (int64_t)a.far_chunks * a.far_slots, head_slots = ((int64_t)b * a.Hk + hk) * slots;

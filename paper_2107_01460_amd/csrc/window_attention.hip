@@ -20,15 +20,15 @@ struct Plan {
 };
 int padded(const marl_attention_dims& d) { return ((d.dim_k > d.dim_v ? d.dim_k : d.dim_v) + 31) / 32 * 32; }
 // A workgroup's wavefronts share the streamed tiles: query heads of one key head first, then tiles next to each other in time.
-Plan plan_of(const marl_attention_dims& d, int window, int sinks, bool fast) {
+Plan plan_of(const marl_attention_dims& d, int window, int sinks, bool fast, bool gradient) {
   Plan p{};
   p.tiles = (int)(((int64_t)d.n_steps + kTile - 1) / kTile);
   const int group = d.n_heads / d.n_kv_heads, pairs = d.n_seqs * d.n_kv_heads;
   p.heads_each = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
-  // (Two tiles of one head up to 64 wide: four wait for each other more than they share, unless the window is long.  128 x 4096 steps of 8 heads of 64 in bf16, window 64:
-  // 696 against 747 us, gradient of 4 heads of 32 in fp32, window 32: 1409 against 1535; 1024 x 520 steps of 4 heads of 32 in fp32, window 1024: 1484 against 1413; 16 384
-  // steps of 8 heads of 128 in bf16, window 512: 100 against 83.)
-  const int most = p.heads_each == 1 && padded(d) <= 64 && window < 512 ? 2 : 4;
+  // (Two tiles of one head where the window is short: four wait for each other more than they share.  128 x 4096 steps of 8 heads of 64 in bf16, window 64: 696 against
+  // 747 us, gradient of 4 heads of 32 in fp32, window 32: 1409 against 1535; 1024 x 520 steps of 4 heads of 32 in fp32, window 1024: 1484 against 1413; 1024 x 64 steps of
+  // 4 heads of 128 in bf16, window 150: 82 against 88, window 511: 118 against 112, and its gradient, whose two wavefronts would spill: 481 against 395.)
+  const int most = p.heads_each == 1 && window < (padded(d) <= 64 ? 512 : gradient ? 0 : 256) ? 2 : 4;
   int along = p.tiles < 2 ? 1 : p.tiles == 2 ? 2 : 4;
   if (along > most) along = most;
   const int least = fast ? least_waves(d.precision == 0 ? 4 : 2, padded(d)) : 4;
@@ -513,7 +513,7 @@ int32_t check_launches(const marl_attention_dims& d, int32_t window, int32_t sin
     fits = launchable((p.units + 3) / 4, 256) && (p.splits == 1 || launchable((int64_t)d.n_seqs * d.n_heads, 1024));
   } else {
     for (bool fast : {false, true}) {  // (whichever the arrays' strides lead to)
-      const Plan p = plan_of(d, window, sinks, fast);
+      const Plan p = plan_of(d, window, sinks, fast, call == CALL_BACKWARD);
       fits = fits && launchable(p.rows, 64 * p.rows_waves) && (call == CALL_FORWARD || (launchable(p.cols, 256) && launchable(p.far, 256)));
     }
     if (next_cache) fits = fits && launchable(cache_blocks(d, (int64_t)window + sinks), 256);
@@ -533,7 +533,7 @@ int32_t marl_window_attention_workspace(const marl_attention_dims* dims, int32_t
   if (call < CALL_FORWARD || call > CALL_STEP) return MARL_E_CONFIG;
   if (bytes == nullptr) return MARL_E_NULL;
   MARL_CHECK(check_launches(*dims, window, sinks, call, false));
-  *bytes = call == CALL_FORWARD ? 0 : call == CALL_BACKWARD ? plan_of(*dims, window, sinks, true).bytes : step_plan(*dims, window, sinks).bytes;
+  *bytes = call == CALL_FORWARD ? 0 : call == CALL_BACKWARD ? plan_of(*dims, window, sinks, true, true).bytes : step_plan(*dims, window, sinks).bytes;
   return MARL_OK;
 }
 
@@ -576,7 +576,7 @@ int32_t marl_window_attention(const marl_attention_dims* dims, int32_t window, i
     a.out = array_of(out, elem);
     a.lse = lse;
     a.fast = fast_rows(d, q, d.dim_k) && fast_rows(d, k, d.dim_k) && fast_rows(d, v, d.dim_v);
-    MARL_CHECK(launch(a, d, plan_of(d, window, sinks, a.fast), WINDOW_OUTPUT, s));
+    MARL_CHECK(launch(a, d, plan_of(d, window, sinks, a.fast, false), WINDOW_OUTPUT, s));
   }
   if (next_cache.keys == nullptr) return MARL_OK;
   CacheArgs c{};
@@ -631,7 +631,7 @@ int32_t marl_window_attention_backward(const marl_attention_dims* dims, int32_t 
   hipStream_t s = (hipStream_t)stream;
   const int elem = d.precision == 0 ? 4 : 2;
   const bool fast = fast_rows(d, q, d.dim_k) && fast_rows(d, k, d.dim_k) && fast_rows(d, v, d.dim_v) && fast_rows(d, out, d.dim_v) && fast_rows(d, dout, d.dim_v);
-  const Plan p = plan_of(d, window, sinks, fast);
+  const Plan p = plan_of(d, window, sinks, fast, true);
   WindowArgs a = args_of(d, window, sinks, positions, first_position, cache);
   a.fast = fast;
   a.q = array_of(q, elem);
