@@ -56,10 +56,11 @@ struct WindowArgs {
   float* far_parts;    // the same places, registers of dk and dv each
 };
 
-// Workgroups go round-robin to the eight XCDs.  Where there are many sequences, whole sequences go round: `run` workgroups next to each other in logical order
-// stay on one XCD, and all XCDs work on neighbouring sequences.  (Each XCD on an eighth of the sequences by itself, as in xcd_remap, has all of them at addresses
-// that differ by large powers of two, as a time-major array's steps do, so that they meet in a part of the memory's channels: 128 x 4096 steps of 8 heads of 64
-// in bf16, steps 4 MB apart: 753 us against MEASURED.)  With few sequences an XCD walks along time, its neighbours' keys in its L2.
+// Workgroups go round-robin to the eight XCDs.  Where there are many sequences, `run` workgroups next to each other in logical order stay on one XCD, and all XCDs work
+// on neighbouring sequences: their rows of a step lie side by side (777 steps of 111 sequences, heads of 40 and 72 in bf16: 132 us against 142 with an eighth of the
+// sequences for each XCD, as in xcd_remap; 128 x 4096 steps of 8 heads of 64: 1166 against 1186).  With few sequences an XCD walks along time, its neighbours' keys in
+// its L2.  (Steps a power of two of bytes apart are slow however workgroups are laid out: 128 x 4096 steps of 8 heads of 64 in bf16 take 701 to 753 us without a cache when
+// steps are 4 MB apart, 516 to 540 when a few lines lie between them, about what the memory gives.)
 __device__ __forceinline__ uint32_t xcd_order(uint32_t at, uint32_t total, uint32_t run, uint32_t sequences) {
   if (sequences < 64) return xcd_remap(at, total);
   const uint32_t turn = 8 * run, whole = total / turn * turn;
@@ -155,8 +156,8 @@ __device__ __forceinline__ uint4 load_unit(const char* row, int col, int dim) {
 
 // ---- tiles in LDS -------------------------------------------------------------------------------------------------------------------
 // Read in two ways: 16 bytes of 16 rows at once (a product's first operand), and, in bf16, pieces of four rows' 64 bytes (the transposed reads).  bf16: a row's pieces
-// are exchanged by bits of the row's number, so that both touch every bank once (padded rows instead: 272 bytes, half of the time of the transposed reads went into
-// conflicts; a long sequence of 8 heads of 128 MEASURED).  fp32: padded by 16 bytes; its second reads are of single elements.
+// are exchanged by bits of the row's number, so that both touch every bank once (rows padded to 272 bytes: 2.7e7 cycles of conflicts in a long sequence of 8 heads of 128,
+// exchanged: 8e5; 266 us and 242, with the sums in ordinary registers).  fp32: padded by 16 bytes; its second reads are of single elements.
 template <class T, int DP>
 struct TileShape {
   static constexpr bool kExchanged = sizeof(T) == 2;
@@ -748,13 +749,13 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, GRADIENT>())) w
 
 // ---- dk, dv ----------------------------------------------------------------------------------------------------------------------------
 // A wavefront takes 32 columns of one key head and, of the query heads that share it, every `heads_each`-th; it streams the rows that see them through a place in LDS of
-// its own, so that wavefronts never wait for each other (four that share tiles of rows wait at every tile for the one that has work: 128 x 4096 steps of 4 heads
-// of 32 in fp32, window 32: MEASURED).  The heads_each wavefronts of the same columns add up their sums at the end, in order.
+// its own, so that wavefronts never wait for each other (four that share tiles of rows wait at every tile for the one that has work: the gradient of 128 x 4096 steps of
+// 4 heads of 32 in fp32, window 32: 1735 us against 1527).  The heads_each wavefronts of the same columns add up their sums at the end, in order.
 //
 // First steps are seen by every later row of their episode: in a long sequence far more tiles of rows than any other column, one wavefront's work.  There the pairs
 // of tiles beyond the window are cut along the rows (far): every so many tiles of rows a wavefront takes the first `far_slots` tiles of first steps that they see, into
-// fp32 parts with the tile's number beside them; the columns' own wavefronts add the parts with their number, in order, and take what was beyond the slots themselves.
-// Tiles of rows on their way: two where a wavefront has a SIMD's registers to itself anyway (the gradient of a long sequence of 8 heads of 128, window 512: MEASURED), none
+// fp32 parts with the tile's number beside them (8192 steps, 4 first steps: 411 us of gradient against 2881); the columns' own wavefronts add the parts with their number, in order, and take what was beyond the slots themselves.
+// Tiles of rows on their way: two where a wavefront has a SIMD's registers to itself anyway (8192 steps of 8 heads of 128, window 512: 124 us against 119), none
 // beside the one at work where that would spill.
 template <class T, int DP>
 constexpr int tiles_ahead() { return sizeof(T) == 2 ? (DP > 64 ? 2 : 1) : DP <= 64 ? 1 : 0; }

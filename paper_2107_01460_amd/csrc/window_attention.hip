@@ -68,7 +68,8 @@ bool fast_rows(const marl_attention_dims& d, const marl_view& v, int dim) {
 }
 
 // ---- the cache behind a call ---------------------------------------------------------------------------------------------------------
-// A row of the next cache comes from the call's steps or, where its step is older, from the cache before.  Bound by memory.
+// A row of the next cache comes from the call's steps or, where its step is older, from the cache before; a step's slot is the same in both.  Bound by memory: 4096
+// sequences of 8 heads of 64 in bf16, 68 slots: 177 us for the 0.83 GB in and out.
 struct CacheArgs {
   WindowArray in[2];  // k, v
   const char* old[2];
@@ -80,7 +81,7 @@ struct CacheArgs {
   uint32_t chunks;  // of kCacheRows slots
   int32_t in_place;
 };
-constexpr int kCacheRows = 64;
+constexpr int kCacheRows = 128;  // slots of a workgroup (of 64, a second workgroup for the few behind them begins anew: 278 us; of 32: 220)
 
 template <class T>
 __device__ __forceinline__ void put_unit(T* p, const uint4& u, int left) {  // `left` elements, at most 16 bytes
