@@ -40,6 +40,7 @@ struct WindowArgs {
   int32_t first;
   uint32_t n_flags, seqs_per_flag;
   float *lse, *delta;  // [B][H][T]
+  int* places;         // [n_flags][T]: the rows' positions, each environment's side by side
   int2* reach;         // [n_flags][tiles]: of a tile's rows, the earliest and the latest beginning of an episode
   int32_t T;
   uint32_t B, H, Hk, group;
@@ -69,17 +70,12 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t at, uint32_t total, uint3
   return in / run * turn + at % 8 * run + in % run;
 }
 
-__device__ __forceinline__ int position_of(const WindowArgs& a, int t, uint32_t env) {
-  return a.positions != nullptr ? a.positions[(int64_t)t * a.n_flags + env] : a.first + t;
-}
-
 // What a row sees.  Rows that hold no step see nothing.
 struct Row {
   int i, start, lo;       // steps from `lo` to i
   uint32_t span, n_sinks; // i - lo; first steps from `start` on
   int position;           // negative: no step
   __device__ __forceinline__ bool valid() const { return position >= 0; }
-  __device__ __forceinline__ bool sees(int j) const { return (uint32_t)(j - lo) <= span || (uint32_t)(j - start) < n_sinks; }
 };
 __device__ __forceinline__ Row row_with(const WindowArgs& a, int i, int position) {
   Row r;
@@ -104,7 +100,6 @@ __device__ __forceinline__ int fresh(int v) {
   return v;
 }
 
-__device__ __forceinline__ Row row_of(const WindowArgs& a, int i, uint32_t env) { return row_with(a, i, i < a.T ? position_of(a, i, env) : -1); }
 
 template <int CONTROL>
 __device__ __forceinline__ int from_lane(int v) {
@@ -602,8 +597,9 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, WAVES, GRADIENT
   request(fk[0], fv[0], first_tile);
   tiles.set(a, row_with(a, i0, i0 < a.T ? position0 : -1), row_with(a, i1, i1 < a.T ? position1 : -1), first_position);
   const Row row = row_with(a, i, i < a.T ? position : -1);
-  if constexpr (GRADIENT) {  // for dk and dv: where the episodes of each tile's rows began
+  if constexpr (GRADIENT) {  // for dk and dv: the positions (far apart in their own array), and where the episodes of each tile's rows began
     if (h == 0 && b % a.seqs_per_flag == 0 && my0 < a.T) {
+      if (half == 0 && i < a.T) a.places[(int64_t)env * a.T + i] = row.position;
       const int lo = wave_min(row.valid() ? row.start : 0x7fffffff), hi = wave_max(row.valid() ? row.start : -0x7fffffff);
       if (lane == 0) a.reach[(int64_t)env * ((a.T + kTile - 1) / kTile) + my0 / kTile] = make_int2(lo, hi);
     }
@@ -797,6 +793,7 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
   const uint32_t which = in_turn / seqs, b = (uint32_t)turn_of * together + in_turn % seqs;
   const uint32_t env = b / a.seqs_per_flag;
   const int2* reach = a.reach + (int64_t)env * n_tiles;
+  const int* places = a.places + (int64_t)env * a.T;
   const int64_t slots = (int64_t)a.far_chunks * a.far_slots, head_slots = ((int64_t)b * a.Hk + hk) * slots;
   int* numbers = a.far_numbers + head_slots;
   int col_tile = on ? (int)which : -1, first_tile = 0, end_tile = n_tiles;
@@ -809,7 +806,7 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
     for (int n = (int)(which % a.far_slots); on && n >= 0; --n) {
       int least = 0x7fffffff;
       for (int i = first_tile * kTile + lane; i < end_tile * kTile; i += 64) {
-        const Row r = row_of(a, i, env);
+        const Row r = row_with(a, i, i < a.T ? places[i] : -1);
         const int t = i / kTile, most = t * kTile >= a.window + kTile - 1 ? (t * kTile - a.window - kTile + 1) / kTile : -1;
         if (r.n_sinks == 0) continue;
         const int last = r.start + (int)r.n_sinks - 1, c = max(max(r.start, 0) / kTile, from);
@@ -873,7 +870,6 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
     float lse, delta;
     int position;
   } sets[kSets];
-  const int32_t* positions = a.positions != nullptr ? a.positions : reinterpret_cast<const int32_t*>(a.lse);
   auto request = [&](Set& set, const Cursor& c) __attribute__((always_inline)) {
     const uint32_t h = hk * a.group + c.g;
     const int i0 = c.tile < 0 ? 0 : c.tile * kTile, n = c.tile < 0 ? 0 : a.T - i0;
@@ -883,7 +879,7 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
     const int64_t stat = ((int64_t)b * a.H + h) * a.T + i;
     set.lse = a.lse[stat];
     set.delta = a.delta[stat];
-    set.position = positions[a.positions != nullptr ? (int64_t)i * a.n_flags + env : 0];
+    set.position = places[i];
   };
   // (the rows next to the columns are always looked at: on their way before anything else is known)
   const bool near = !far && tiles_ahead<T, DP>() > 0;
@@ -921,7 +917,7 @@ __global__ void __launch_bounds__(256, (columns_waves<T, DP>())) window_columns_
       set.d.store(tile_d);
       if (lane < kTile) {
         const int i = now.tile * kTile + lane;
-        const Row seer = row_with(a, i, now.tile >= 0 && i < a.T ? a.positions != nullptr ? set.position : a.first + i : -1);
+        const Row seer = row_with(a, i, now.tile >= 0 && i < a.T ? set.position : -1);
         stats[0][lane] = seer.valid() ? set.lse * 1.44269504088896341f : 0.f;
         stats[1][lane] = seer.valid() ? set.delta : 0.f;
         sight[lane] = make_int4(seer.lo, (int)seer.span, seer.start, (int)seer.n_sinks);

@@ -16,7 +16,7 @@ struct Plan {
   int64_t rows, cols, far;    // workgroups
   int far_tiles;
   uint32_t far_chunks, far_slots;
-  int64_t delta, reach, numbers, parts, bytes;
+  int64_t delta, places, reach, numbers, parts, bytes;
 };
 int padded(const marl_attention_dims& d) { return ((d.dim_k > d.dim_v ? d.dim_k : d.dim_v) + 31) / 32 * 32; }
 // A workgroup's wavefronts share the streamed tiles: query heads of one key head first, then tiles next to each other in time.
@@ -53,6 +53,7 @@ Plan plan_of(const marl_attention_dims& d, int window, int sinks, bool fast, boo
   };
   const int64_t slots = (int64_t)pairs * p.far_chunks * p.far_slots;
   p.delta = take((int64_t)d.n_seqs * d.n_heads * d.n_steps * 4);
+  p.places = take((int64_t)(d.n_seqs / d.seqs_per_flag) * d.n_steps * 4);
   p.reach = take((int64_t)(d.n_seqs / d.seqs_per_flag) * p.tiles * 8);
   p.numbers = take(slots * 4);
   p.parts = take(slots * 2 * kTile * padded(d) * 4);
@@ -645,6 +646,7 @@ int32_t marl_window_attention_backward(const marl_attention_dims* dims, int32_t 
   a.dv = array_of(dv, elem);
   a.lse = const_cast<float*>(lse);
   a.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.delta);
+  a.places = reinterpret_cast<int*>(static_cast<char*>(workspace) + p.places);
   a.reach = reinterpret_cast<int2*>(static_cast<char*>(workspace) + p.reach);
   a.far_chunks = p.far_chunks;
   a.far_slots = p.far_slots;
