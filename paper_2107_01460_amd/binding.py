@@ -468,7 +468,6 @@ def linear_attention_backward(q, k, v, decay, dout, dq, dk, dv, workspace=None, 
 def linear_attention_step(q, k, v, decay, state, out, next_state=None, done=None, scale=1.0, stream=None):
     """One step: q [B][Hq][Dk], k, v [B][Hk][D], out [B][Hq][Dv]; done [environments]: of the step before (the state is cleared).  The state is
     updated in place unless next_state is given."""
-    _here(q, k, v, *cache, positions, out, workspace)
     precision, dt = _PRECISION.get(q.dtype), q.dtype
     if precision is None or q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
         raise _refused("q, k, v: float32 or bfloat16 [B][heads][D]")

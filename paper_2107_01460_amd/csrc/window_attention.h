@@ -525,7 +525,7 @@ struct Tiles {
   }
 };
 
-// Wavefronts a SIMD that the registers are shared out for: as many as spill none
+// Wavefronts a SIMD that the registers are shared out for: as many as spill none, but for dq of bf16 heads wider than 64 (6 to 36 registers)
 template <class T, int DP, int WAVES, bool GRADIENT>
 constexpr int rows_waves() { return sizeof(T) == 4 ? (DP > 64 ? 1 : DP > 32 || WAVES == 1 ? 2 : 3) : DP <= 32 || (DP <= 64 && WAVES > 1 && !GRADIENT) ? 3 : 2; }
 template <class T, int DP>
