@@ -713,10 +713,16 @@ def window_attention_step(q, k, v, cache, positions, out, window, sinks=0, scale
     _, Hk, Dv = v.shape
     at, per = _positions(positions, (), B)
     dims, need, L = AttentionDims.from_buffer_copy(_DIMS.pack(precision, 1, B, H, Hk, Dk, Dv, per, scale)), C.c_int64(), lib()
-    _check(L.marl_window_attention_workspace(C.byref(dims), window, sinks, 2, C.byref(need)))
-    _check(L.marl_window_attention_step(
+    size = lambda: _check(L.marl_window_attention_workspace(C.byref(dims), window, sinks, 2, C.byref(need)))
+    if workspace is not None:
+        size()
+    code = L.marl_window_attention_step(
         C.byref(dims), window, sinks, _step_view(q, (B, H, Dk), dt, "q"), _step_view(k, (B, Hk, Dk), dt, "k"), _step_view(v, (B, Hk, Dv), dt, "v"), at,
-        _cache(cache, (B, Hk, sinks + window), Dk, Dv, dt, "cache"), _step_view(out, (B, H, Dv), dt, "out"), _workspace(workspace, need.value), _stream(stream)))
+        _cache(cache, (B, Hk, sinks + window), Dk, Dv, dt, "cache"), _step_view(out, (B, H, Dv), dt, "out"), _workspace(workspace, need.value), _stream(stream))
+    if code and workspace is None:   # (most steps need none: asked for where the call misses it)
+        size()
+        _workspace(None, need.value)
+    _check(code)
     _raise_versions((out, *cache))
 
 
