@@ -127,12 +127,16 @@ struct Columns {
       }
     }
   }
-  // each element's partner: inside the vector, or half the rotated part away
+  // each element's partner: inside the vector (taken from there where it is used), or half the rotated part away; zero behind the rotated part, since a neighbour's infinity
+  // times the sine of 0 is a NaN
+  __device__ __forceinline__ float partner(const float (&own)[E], const float (&p)[E], int e) const {
+    if constexpr (INTER) return col + (e & ~1) < rotary ? own[e ^ 1] : 0.f;
+    else return p[e];
+  }
   template <class F>
-  __device__ __forceinline__ void partners(const float (&own)[E], float (&p)[E], F load) const {
+  __device__ __forceinline__ void partners(float (&p)[E], F load) const {
     if constexpr (INTER) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) p[e] = own[e ^ 1];
+      (void)load;
     } else if constexpr (WHOLE) {
       if (col < rotary) load(p, col < half ? col + half : col - half);
       else {
@@ -174,7 +178,7 @@ __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormArgs args) {
     for (int e = 0; e < E; ++e) w[e] = wp[e] = 1.f;
   } else {
     weights(w, col);
-    if constexpr (!GRADIENT) cols.partners(w, wp, weights);
+    if constexpr (!GRADIENT) cols.partners(wp, weights);
   }
   float dw[E];
 #pragma unroll
@@ -209,10 +213,10 @@ __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormArgs args) {
       if (u >= n || !on) continue;
       get<T, WHOLE>(v[u], x + u * a.x_head, col, dim);
       if constexpr (!GRADIENT) {
-        cols.partners(v[u], zp[u], [&](float (&f)[E], int from) { get<T, WHOLE>(f, x + u * a.x_head, from, dim); });
+        cols.partners(zp[u], [&](float (&f)[E], int from) { get<T, WHOLE>(f, x + u * a.x_head, from, dim); });
       } else {
         get<T, WHOLE>(z[u], dy + u * a.dy_head, col, dim);
-        cols.partners(z[u], zp[u], [&](float (&f)[E], int from) { get<T, WHOLE>(f, dy + u * a.dy_head, from, dim); });
+        cols.partners(zp[u], [&](float (&f)[E], int from) { get<T, WHOLE>(f, dy + u * a.dy_head, from, dim); });
       }
     }
     const bool known = position < args.n_positions;
@@ -222,7 +226,7 @@ __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormArgs args) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         c[e] *= w[e];
-        s[e] *= wp[e];
+        s[e] *= cols.partner(w, wp, e);
       }
     }
 #pragma unroll
@@ -235,12 +239,12 @@ __global__ void __launch_bounds__(256) norm_rotary_kernel(const NormArgs args) {
       const float rstd = 1.f / __builtin_sqrtf(squares * each + args.eps);
       if constexpr (!GRADIENT) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = rstd * (v[u][e] * c[e] + zp[u][e] * s[e]);
+        for (int e = 0; e < E; ++e) y[e] = rstd * (v[u][e] * c[e] + cols.partner(v[u], zp[u], e) * s[e]);
       } else {
         float g[E], du[E], dot = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          du[e] = z[u][e] * c[e] - zp[u][e] * s[e];
+          du[e] = z[u][e] * c[e] - cols.partner(z[u], zp[u], e) * s[e];
           g[e] = du[e] * w[e];
           if (on) dot = __builtin_fmaf(g[e], v[u][e], dot);
         }
