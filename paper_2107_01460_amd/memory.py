@@ -114,6 +114,18 @@ class NormRotate(torch.autograd.Function):
         return dq, dk, dqw, dkw, None, None, None
 
 
+def _zero_state(shape, dtype, device):
+    """A window's state [2][B][kv heads][slots][D] of zeros: keys and values, each at the sixteen bytes that the library asks of a cache."""
+    strides = [math.prod(shape[n + 1:]) for n in range(len(shape))]
+    strides[0] += -strides[0] % (16 // dtype.itemsize)
+    return torch.empty_strided(shape, strides, dtype=dtype, device=device).zero_()
+
+
+def _halves(state):
+    """(keys, values) of a window's state as the library takes them: the state's own memory, or a copy where a caller's copy or slice of a state lies at other bytes."""
+    return tuple(x if x.is_contiguous() and x.data_ptr() % 16 == 0 else x.clone(memory_format=torch.contiguous_format) for x in (state[0], state[1]))
+
+
 class AttendWindow(torch.autograd.Function):
     """(out, state behind it) of attention over the last `window` steps and the first `sinks` of an episode; gradients of q, k, v.  state
     [2][B][kv heads][sinks + window][D]: the cache's keys and values, constants of the gradient, or None where every episode begins in the call."""
@@ -124,8 +136,8 @@ class AttendWindow(torch.autograd.Function):
         T, n, H, D = q.shape
         out = torch.empty((T, n, H, D), dtype=q.dtype, device=q.device)
         lse = torch.empty((n, H, T), dtype=torch.float32, device=q.device)
-        after = torch.zeros((2, n, k.shape[2], sinks + window, D), dtype=q.dtype, device=q.device)     # the call leaves slots that hold no step as they were
-        B.window_attention(q, k, v, out, window, sinks, lse=lse, positions=positions, cache=None if state is None else (state[0], state[1]),
+        after = _zero_state((2, n, k.shape[2], sinks + window, D), q.dtype, q.device)     # the call leaves slots that hold no step as they were
+        B.window_attention(q, k, v, out, window, sinks, lse=lse, positions=positions, cache=None if state is None else _halves(state),
                            next_cache=(after[0], after[1]), scale=scale)
         ctx.save_for_backward(q, k, v, out, lse, state, positions)
         ctx.looks = window, sinks, scale
@@ -138,7 +150,7 @@ class AttendWindow(torch.autograd.Function):
         q, k, v, out, lse, state, positions = ctx.saved_tensors
         window, sinks, scale = ctx.looks
         dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
-        B.window_attention_backward(q, k, v, out, lse, _rows(dout), dq, dk, dv, window, sinks, positions=positions, cache=None if state is None else (state[0], state[1]),
+        B.window_attention_backward(q, k, v, out, lse, _rows(dout), dq, dk, dv, window, sinks, positions=positions, cache=None if state is None else _halves(state),
                                     scale=scale, workspace=B.alloc_workspace(B.window_attention_workspace(q, k, v, window, sinks, kind="backward")))
         return dq, dk, dv, None, None, None, None, None
 
@@ -200,10 +212,10 @@ class MemoryCritic(torch.nn.Module):
 
     def initial_state(self, sequences):
         """One state per layer, all zero: [B][heads][D][D] fp32, or with a window [2][B][kv heads][sinks + window][D] keys and values."""
-        shape, dtype = (sequences, self.heads, self.dim, self.dim), torch.float32
+        device = self.decay.device
         if self.window is not None:
-            shape, dtype = (2, sequences, self.kv_heads, self.sinks + self.window, self.dim), self.dtype
-        return [torch.zeros(shape, dtype=dtype, device=self.decay.device) for _ in self.layers]
+            return [_zero_state((2, sequences, self.kv_heads, self.sinks + self.window, self.dim), self.dtype, device) for _ in self.layers]
+        return [torch.zeros((sequences, self.heads, self.dim, self.dim), dtype=torch.float32, device=device) for _ in self.layers]
 
     def _heads(self, m, y):
         """q, k, v as views of one product's columns."""
@@ -249,7 +261,11 @@ class MemoryCritic(torch.nn.Module):
             else:
                 q, k = NormRotate.apply(q[None], k[None], m.q_norm, m.k_norm, self.table, positions[None], 1e-6)
                 need = B.window_attention_workspace(q, k, v[None], self.window, self.sinks, kind="step")
-                B.window_attention_step(q[0], k[0], v, (state[n][0], state[n][1]), positions, out, self.window, self.sinks, scale=1 / math.sqrt(self.dim),
+                cache = _halves(state[n])
+                B.window_attention_step(q[0], k[0], v, cache, positions, out, self.window, self.sinks, scale=1 / math.sqrt(self.dim),
                                         workspace=B.alloc_workspace(need) if need else None)
+                for own, used in zip(state[n], cache):
+                    if own.data_ptr() != used.data_ptr():
+                        own.copy_(used)
             x = self._rest(m, x, out)
         return self._product(self.value, LayerNorm.apply(x, self.norm_w, self.norm_b, 1e-5)).squeeze(-1).float()
