@@ -360,6 +360,13 @@ def _refused(what):
 
 
 # (What follows runs in front of every call, which for a single step takes as long as the kernel: comparisons first, words only for a refusal.)
+def _int32(*numbers):
+    """Refuses what ctypes would take modulo 2^32."""
+    for n in numbers:
+        if not -0x80000000 <= n <= 0x7fffffff:
+            raise _refused(f"{n}: 32 bits")
+
+
 def _floats(t, shape, name):
     """Pointer of an optional contiguous fp32 tensor of this shape."""
     if t is None:
@@ -495,6 +502,7 @@ def layer_norm(x, weight, bias, out, mean=None, rstd=None, eps=1e-5, stream=None
     if precision is None or x.dim() != 2:
         raise _refused("x: float32 or bfloat16 [rows][width]")
     shape = n, width = x.shape
+    _int32(width)
     _check(lib().marl_layer_norm(precision, n, width, *_rows(x, shape, dt, "x"), _floats(weight, (width,), "weight"),
                                  _floats(bias, (width,), "bias"), eps, *_rows(out, shape, dt, "out"), _floats(mean, (n,), "mean"),
                                  _floats(rstd, (n,), "rstd"), _stream(stream)))
@@ -504,6 +512,7 @@ def layer_norm(x, weight, bias, out, mean=None, rstd=None, eps=1e-5, stream=None
 def layer_norm_workspace(rows, width):
     """Bytes of workspace that the gradient of layer_norm needs."""
     n = C.c_int64()
+    _int32(width)
     _check(lib().marl_layer_norm_workspace(rows, width, C.byref(n)))
     return n.value
 
@@ -514,6 +523,7 @@ def layer_norm_backward(dout, x, weight, mean, rstd, dx, dweight=None, dbias=Non
     if precision is None or x.dim() != 2:
         raise _refused("x: float32 or bfloat16 [rows][width]")
     shape = n, width = x.shape
+    _int32(width)
     need = 0 if dweight is None and dbias is None else layer_norm_workspace(n, width)
     _check(lib().marl_layer_norm_backward(
         precision, n, width, *_rows(dout, shape, dt, "dout"), *_rows(x, shape, dt, "x"), _floats(weight, (width,), "weight"),
@@ -527,6 +537,7 @@ ROTARY_SCALING = {None: 0, "linear": 1, "base": 2, "by_turns": 3}
 
 def rotary_table(n_positions, rotary_dim, base=10000.0, scaling=None, factor=1.0, trained_length=0.0, slow=1.0, fast=32.0, amplitude=1.0, stream=None):
     """[n_positions][rotary_dim] float32: cosines, then sines, of position times frequency, for contexts `factor` times the trained length."""
+    _int32(n_positions, rotary_dim)
     table = torch.empty((n_positions, rotary_dim), dtype=torch.float32, device="cuda")
     dims = RotaryDims(n_positions, rotary_dim, ROTARY_SCALING[scaling], base, factor, trained_length, slow, fast, amplitude)
     _check(lib().marl_rotary_table(C.byref(dims), _ptr(table), _stream(stream)))
@@ -545,6 +556,7 @@ def rotary(q, k, table, q_out, k_out, positions=None, first_position=0, interlea
     if table.dim() != 2:
         raise _refused("table: [positions][rotary_dim]")
     P, R = table.shape
+    _int32(P, R, first_position)
     at, per = None, 1
     if positions is not None:
         n = positions.shape[-1] if positions.dim() else 0
@@ -581,7 +593,7 @@ def _here(*tensors):
                 current = at
 
 
-def _norm_dims(q, k, table, positions):
+def _norm_dims(q, k, table, positions, first_position):
     """(dims, shapes of q and of k, table rows, rotated elements, positions' pointer) of arrays [T][B][heads][D]; k may be None"""
     precision = _PRECISION.get(q.dtype)
     if precision is None or q.dim() != 4 or k is not None and k.dim() != 4:
@@ -590,6 +602,7 @@ def _norm_dims(q, k, table, positions):
     Hk = 1 if k is None else k.shape[2]
     if table.dim() != 2:
         raise _refused("table: [positions][rotary_dim]")
+    _int32(*table.shape, first_position)
     at, per = _positions(positions, (T,), B)
     return AttentionDims.from_buffer_copy(_DIMS.pack(precision, T, B, H, Hk, D, D, per, 1.0)), (T, B, H, D), (T, B, Hk, D), *table.shape, at
 
@@ -598,7 +611,7 @@ def norm_rotary(q, k, q_weight, k_weight, table, q_out, k_out, eps=1e-6, positio
     """Every head of q and k divided by the root of its mean square and weighted, then rotated as by rotary(); weights (and k, k_out) may be None.  Rows of
     negative positions: zeros.  The outputs may be the inputs."""
     _here(q, k, q_weight, k_weight, table, q_out, k_out, positions)
-    dims, qs, ks, P, R, at = _norm_dims(q, k, table, positions)
+    dims, qs, ks, P, R, at = _norm_dims(q, k, table, positions, first_position)
     dt, D, none = q.dtype, q.shape[3], View()
     _check(lib().marl_norm_rotary(
         C.byref(dims), _view(q, qs, dt, "q"), none if k is None else _view(k, ks, dt, "k"), _floats(q_weight, (D,), "q_weight"),
@@ -621,7 +634,7 @@ def norm_rotary_backward(dq_out, dk_out, q, k, q_weight, k_weight, table, dq, dk
                          first_position=0, interleaved=False, stream=None):
     """dq, dk and the weights' gradients dq_weight, dk_weight (may be None) of norm_rotary from those of its outputs."""
     _here(dq_out, dk_out, q, k, q_weight, k_weight, table, dq, dk, dq_weight, dk_weight, workspace, positions)
-    dims, qs, ks, P, R, at = _norm_dims(q, k, table, positions)
+    dims, qs, ks, P, R, at = _norm_dims(q, k, table, positions, first_position)
     dt, D, none, need, L = q.dtype, q.shape[3], View(), C.c_int64(), lib()
     if dq_weight is not None or dk_weight is not None:
         _check(L.marl_norm_rotary_workspace(C.byref(dims), C.byref(need)))
@@ -666,6 +679,7 @@ def window_attention_workspace(q, k, v, window, sinks=0, kind="forward"):
     (of a step [B][heads][D] or [1][B][heads][D])."""
     if kind not in WINDOW_CALLS:
         raise _refused(f"kind: one of {list(WINDOW_CALLS)}")
+    _int32(window, sinks)
     if kind == "step" and q.dim() == 3:
         q, k, v = q[None], k[None], v[None]
     n = C.c_int64()
@@ -678,6 +692,7 @@ def window_attention(q, k, v, out, window, sinks=0, lse=None, positions=None, fi
     """out [T][B][Hq][Dv] (and lse [B][Hq][T]) of attention over the last `window` steps of an episode and its first `sinks`; positions [T][environments]: each
     row's step in its episode, negative for none.  cache, next_cache: (keys, values) before and behind the call, [B][Hk][sinks + window][D]."""
     _here(q, k, v, out, lse, positions, workspace, *(cache or ()), *(next_cache or ()))
+    _int32(window, sinks, first_position)
     dims, T, B, H, Hk, Dk, Dv, at = _window_dims(q, k, v, positions, scale)
     dt, shape = q.dtype, (B, Hk, sinks + window)
     before = _cache(cache, shape, Dk, Dv, dt, "cache")
@@ -692,6 +707,7 @@ def window_attention_backward(q, k, v, out, lse, dout, dq, dk, dv, window, sinks
                               stream=None):
     """Gradients dq, dk, dv of window_attention from dout and what it kept; the cache's steps are constants."""
     _here(q, k, v, out, lse, dout, dq, dk, dv, positions, workspace, *(cache or ()))
+    _int32(window, sinks, first_position)
     dims, T, B, H, Hk, Dk, Dv, at = _window_dims(q, k, v, positions, scale)
     dt, need, L = q.dtype, C.c_int64(), lib()
     qs, ks, vs, os = (T, B, H, Dk), (T, B, Hk, Dk), (T, B, Hk, Dv), (T, B, H, Dv)
@@ -706,6 +722,7 @@ def window_attention_backward(q, k, v, out, lse, dout, dq, dk, dv, window, sinks
 def window_attention_step(q, k, v, cache, positions, out, window, sinks=0, scale=1.0, workspace=None, stream=None):
     """One step: q [B][Hq][Dk], k, v [B][Hk][D], out [B][Hq][Dv], positions [environments].  k and v go into the cache, which is read with them."""
     _here(q, k, v, *cache, positions, out, workspace)
+    _int32(window, sinks)
     precision, dt = _PRECISION.get(q.dtype), q.dtype
     if precision is None or q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
         raise _refused("q, k, v: float32 or bfloat16 [B][heads][D]")
