@@ -404,15 +404,15 @@ int32_t marl_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, c
 /* Norm of each head of q [T][B][n_heads][dim] and, with the same positions, k [T][B][n_kv_heads][dim] (k.data NULL: q alone), then the rotation of marl_rotary, in
  * one pass: u = x * rstd * weight, rstd = 1 / sqrt(mean(x^2) + eps) over a head's dim (1..256) elements, weight [dim] for all heads of q, of k (fp32; NULL: 1); the
  * first rotary_dim elements of u are rotated, the others copied.  positions and first_position as in marl_rotary, but a row whose position is negative holds no
- * step: zeros.  A position behind the table gives NaNs in the rotated elements.  An output may be its input, with the same strides.  The values between norm and
- * rotation are not rounded.  dims: precision, n_steps, n_seqs, n_heads, n_kv_heads, dim_k, seqs_per_flag are read. */
+ * step: zeros.  A position behind the table gives NaNs in the rotated elements.  An output may be its input, with the same strides; otherwise it begins where no other
+ * array does, and no row of it lies in the table, the weights or the positions (MARL_E_CONFIG).  The values between norm and rotation are not rounded.  dims: precision, n_steps, n_seqs, n_heads, n_kv_heads, dim_k, seqs_per_flag are read. */
 int32_t marl_norm_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, const float* q_weight, const float* k_weight, float eps,
                          const float* table, int32_t n_positions, int32_t rotary_dim, const int32_t* positions, int32_t first_position,
                          int32_t interleaved, marl_view q_out, marl_view k_out, void* stream);
 
 /* Its gradient: dq, dk from the gradients dq_out, dk_out of its outputs, and the sums over all rows dq_weight, dk_weight [dim] (fp32, nullable, added in an order that
- * depends on the sizes only).  Rows that hold no step: zeros, and nothing of theirs enters the sums.  dq may be dq_out or q with the same strides, dk likewise.  workspace:
- * marl_norm_rotary_workspace bytes, where a sum is asked for. */
+ * depends on the sizes only).  Rows that hold no step: zeros, and nothing of theirs enters the sums.  dq may be dq_out or q with the same strides, dk likewise; the
+ * sums and the workspace share memory with nothing else (MARL_E_CONFIG).  workspace: marl_norm_rotary_workspace bytes, where a sum is asked for. */
 int32_t marl_norm_rotary_backward(const marl_attention_dims* dims, marl_view dq_out, marl_view dk_out, marl_view q, marl_view k, const float* q_weight,
                                   const float* k_weight, float eps, const float* table, int32_t n_positions, int32_t rotary_dim,
                                   const int32_t* positions, int32_t first_position, int32_t interleaved, marl_view dq, marl_view dk,
@@ -438,7 +438,10 @@ typedef struct marl_window_cache {
  * last row that holds a step; its slots that hold no step, and where there is no cache those of steps before row 0, are left as they were.  A sequence without a step:
  * the cache itself.
  * bf16: scores and statistics are fp32 sums of exact products; the weights, and in the gradient what multiplies keys and queries, are rounded to bf16 once (2^-9 of each
- * term); outputs are rounded once.  workspace: marl_window_attention_workspace bytes.  Errors as in marl_linear_attention; MARL_E_CONFIG for window or sinks
+ * term); outputs are rounded once.  workspace: marl_window_attention_workspace bytes.
+ * Memory shared (MARL_E_CONFIG, in the gradient and the step too): no row of q, k, v, out or their gradients lies in lse, a cache or the workspace where the call writes
+ * that, no row of an output in these or in positions where it reads them, and these overlap nowhere where one of them is written.  Rows of arrays with strides may lie
+ * between each other's: of such arrays an output begins where no other does.  Errors as in marl_linear_attention; MARL_E_CONFIG for window or sinks
  * out of range. */
 int32_t marl_window_attention(const marl_attention_dims* dims, int32_t window, int32_t sinks, marl_view q, marl_view k, marl_view v,
                               const int32_t* positions, int32_t first_position, marl_window_cache cache, marl_view out, float* lse,

@@ -314,6 +314,8 @@ int64_t blocks_of(int64_t units, int L) {
   const int64_t run = 256 / L, n = (units + run - 1) / run;
   return n > kMaxBlocks ? kMaxBlocks : n;
 }
+// Of the workspace: the shares of dw of one array's workgroups
+int64_t share_bytes(const marl_attention_dims& d) { return (kMaxBlocks * d.dim_k * 4 + 255) / 256 * 256; }
 
 template <class T, int L, bool GRADIENT>
 void launch_lanes(const NormArgs& a, unsigned blocks, bool inter, bool whole, hipStream_t s) {
@@ -435,6 +437,10 @@ int32_t marl_norm_rotary(const marl_attention_dims* dims, marl_view q, marl_view
     MARL_CHECK(check_in_place(out[u], in[u], d, heads));
   }
   if (two && (q_out.data == k_out.data || q_out.data == k.data || k_out.data == q.data)) return MARL_E_CONFIG;
+  for (int u = 0; u < (two ? 2 : 1); ++u)
+    if (touches(out[u], d, u == 0 ? d.n_heads : d.n_kv_heads, d.dim_k,
+                {extent(table, (int64_t)n_positions * rotary_dim * 4), places_of(d, positions), extent(q_weight, d.dim_k * 4), extent(k_weight, d.dim_k * 4)}))
+      return MARL_E_CONFIG;
   NormArgs a = args_of(d, eps, table, n_positions, rotary_dim, positions, first_position, interleaved);
   a.a[0] = array_of(d, q, nullptr, q_out, d.n_heads, q_weight);
   if (two) a.a[1] = array_of(d, k, nullptr, k_out, d.n_kv_heads, k_weight);
@@ -444,7 +450,7 @@ int32_t marl_norm_rotary(const marl_attention_dims* dims, marl_view q, marl_view
 int32_t marl_norm_rotary_workspace(const marl_attention_dims* dims, int64_t* bytes) {
   MARL_CHECK(check_norm(dims, true));
   if (bytes == nullptr) return MARL_E_NULL;
-  *bytes = 2 * ((kMaxBlocks * dims->dim_k * 4 + 255) / 256 * 256);
+  *bytes = 2 * share_bytes(*dims);
   return MARL_OK;
 }
 
@@ -460,7 +466,8 @@ int32_t marl_norm_rotary_backward(const marl_attention_dims* dims, marl_view dq_
   MARL_CHECK(check_vector(k_weight));
   MARL_CHECK(check_vector(dq_weight));
   MARL_CHECK(check_vector(dk_weight));
-  if (dq_weight != nullptr && dq_weight == dk_weight) return MARL_E_CONFIG;
+  const Extent wq = extent(q_weight, d.dim_k * 4), wk = extent(k_weight, d.dim_k * 4), gq = extent(dq_weight, d.dim_k * 4), gk = extent(dk_weight, d.dim_k * 4);
+  if (gq.meets(gk)) return MARL_E_CONFIG;
   const bool weights = dq_weight != nullptr || ((two || !used) && dk_weight != nullptr);
   const marl_view in[2] = {q, k}, grad[2] = {dq_out, dk_out}, out[2] = {dq, dk};
   if (used) {
@@ -479,9 +486,17 @@ int32_t marl_norm_rotary_backward(const marl_attention_dims* dims, marl_view dq_
       MARL_CHECK(check_places(dq, {k, dk_out, dk}, true));
       MARL_CHECK(check_places(dk, {q, dq_out}, true));
     }
+    const Extent angles = extent(table, (int64_t)n_positions * rotary_dim * 4), ps = places_of(d, positions), ws = extent(workspace, weights ? 2 * share_bytes(d) : 0);
+    for (int u = 0; u < (two ? 2 : 1); ++u) {
+      const int heads = u == 0 ? d.n_heads : d.n_kv_heads;
+      if (touches(out[u], d, heads, d.dim_k, {angles, ps, wq, wk, gq, gk, ws}) || touches(in[u], d, heads, d.dim_k, {gq, gk, ws}) ||
+          touches(grad[u], d, heads, d.dim_k, {gq, gk, ws}))
+        return MARL_E_CONFIG;
+    }
+    for (const Extent& x : {angles, ps, wq, wk, gq, gk})
+      if (ws.meets(x)) return MARL_E_CONFIG;
   }
   hipStream_t s = (hipStream_t)stream;
-  const int64_t half = (kMaxBlocks * d.dim_k * 4 + 255) / 256 * 256;
   WeightArgs w{};
   w.dim = d.dim_k;
   if (used) {
@@ -489,7 +504,7 @@ int32_t marl_norm_rotary_backward(const marl_attention_dims* dims, marl_view dq_
     a.a[0] = array_of(d, q, &dq_out, dq, d.n_heads, q_weight);
     if (two) a.a[1] = array_of(d, k, &dk_out, dk, d.n_kv_heads, k_weight);
     if (dq_weight != nullptr) a.a[0].part = static_cast<float*>(workspace);
-    if (two && dk_weight != nullptr) a.a[1].part = reinterpret_cast<float*>(static_cast<char*>(workspace) + half);
+    if (two && dk_weight != nullptr) a.a[1].part = reinterpret_cast<float*>(static_cast<char*>(workspace) + share_bytes(d));
     MARL_CHECK(run(a, d, true, two, s));
     const int L = lanes_of(d.precision, d.dim_k);
     w.part[0] = a.a[0].part;

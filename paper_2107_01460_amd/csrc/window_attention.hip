@@ -458,14 +458,10 @@ int32_t check_positions(const marl_attention_dims& d, const int32_t* positions, 
   if (positions == nullptr && (int64_t)first + d.n_steps > 0x7fffffff) return MARL_E_SIZE;
   return MARL_OK;
 }
-struct Extent {
-  uintptr_t from, bytes;
-  bool holds(const void* p) const { return bytes > 0 && reinterpret_cast<uintptr_t>(p) - from < bytes; }
-  bool meets(const Extent& o) const { return bytes > 0 && o.bytes > 0 && (from < o.from ? o.from - from < bytes : from - o.from < o.bytes); }
-};
 Extent cached(const marl_attention_dims& d, const void* p, int64_t slots, int dim) {
-  return {reinterpret_cast<uintptr_t>(p), p == nullptr ? 0 : (uintptr_t)((int64_t)d.n_seqs * d.n_kv_heads * slots * dim * (d.precision == 0 ? 4 : 2))};
+  return extent(p, (int64_t)d.n_seqs * d.n_kv_heads * slots * dim * (d.precision == 0 ? 4 : 2));
 }
+Extent statistics(const marl_attention_dims& d, const float* lse) { return extent(lse, (int64_t)d.n_seqs * d.n_heads * d.n_steps * 4); }
 // Both arrays or neither, aligned
 int32_t check_cache(const marl_window_cache& c, bool needed) {
   if ((c.keys == nullptr) != (c.values == nullptr) || (needed && c.keys == nullptr)) return MARL_E_NULL;
@@ -563,12 +559,13 @@ int32_t marl_window_attention(const marl_attention_dims* dims, int32_t window, i
   const bool in_place = next_cache.keys != nullptr && next_cache.keys == cache.keys && next_cache.values == cache.values;
   if (nk.meets(nv) || nk.meets(cv) || nv.meets(ck) || (!in_place && (nk.meets(ck) || nv.meets(cv)))) return MARL_E_CONFIG;
   if (used) {
-    if (ck.holds(out.data) || cv.holds(out.data) || ck.holds(lse) || cv.holds(lse)) return MARL_E_CONFIG;
-    for (const void* x : {q.data, k.data, v.data, out.data, (void*)lse, (void*)positions})
-      if (nk.holds(x) || nv.holds(x)) return MARL_E_CONFIG;
-    if (out.data == positions) return MARL_E_CONFIG;
-    for (const void* x : {q.data, k.data, v.data, out.data, (void*)positions})
-      if (lse != nullptr && x == lse) return MARL_E_CONFIG;
+    const Extent ps = places_of(d, positions), ls = statistics(d, lse);
+    if (touches(out, d, d.n_heads, d.dim_v, {ck, cv, nk, nv, ps, ls}) || touches(q, d, d.n_heads, d.dim_k, {nk, nv, ls}) ||
+        touches(k, d, d.n_kv_heads, d.dim_k, {nk, nv, ls}) || touches(v, d, d.n_kv_heads, d.dim_v, {nk, nv, ls}))
+      return MARL_E_CONFIG;
+    for (const Extent& x : {ck, cv, nk, nv, ps})
+      if (ls.meets(x)) return MARL_E_CONFIG;
+    if (ps.meets(nk) || ps.meets(nv)) return MARL_E_CONFIG;
   }
   if (d.n_seqs == 0) return MARL_OK;
   hipStream_t s = (hipStream_t)stream;
@@ -631,12 +628,17 @@ int32_t marl_window_attention_backward(const marl_attention_dims* dims, int32_t 
   if (!used) return MARL_OK;
   const int64_t slots = (int64_t)window + sinks;
   const Extent ck = cached(d, cache.keys, slots, d.dim_k), cv = cached(d, cache.values, slots, d.dim_v);
-  for (const void* x : {dq.data, dk.data, dv.data})
-    if (ck.holds(x) || cv.holds(x) || x == lse || x == positions) return MARL_E_CONFIG;
-  hipStream_t s = (hipStream_t)stream;
   const int elem = d.precision == 0 ? 4 : 2;
   const bool fast = fast_rows(d, q, d.dim_k) && fast_rows(d, k, d.dim_k) && fast_rows(d, v, d.dim_v) && fast_rows(d, out, d.dim_v) && fast_rows(d, dout, d.dim_v);
   const Plan p = plan_of(d, window, sinks, fast, true);
+  const Extent ps = places_of(d, positions), ls = statistics(d, lse), ws = extent(workspace, p.bytes);
+  if (touches(dq, d, d.n_heads, d.dim_k, {ck, cv, ps, ls, ws}) || touches(dk, d, d.n_kv_heads, d.dim_k, {ck, cv, ps, ls, ws}) ||
+      touches(dv, d, d.n_kv_heads, d.dim_v, {ck, cv, ps, ls, ws}) || touches(q, d, d.n_heads, d.dim_k, ws) || touches(k, d, d.n_kv_heads, d.dim_k, ws) ||
+      touches(v, d, d.n_kv_heads, d.dim_v, ws) || touches(out, d, d.n_heads, d.dim_v, ws) || touches(dout, d, d.n_heads, d.dim_v, ws))
+    return MARL_E_CONFIG;
+  for (const Extent& x : {ck, cv, ps, ls})
+    if (ws.meets(x)) return MARL_E_CONFIG;
+  hipStream_t s = (hipStream_t)stream;
   WindowArgs a = args_of(d, window, sinks, positions, first_position, cache);
   a.fast = fast;
   a.q = array_of(q, elem);
@@ -676,12 +678,12 @@ int32_t marl_window_attention_step(const marl_attention_dims* dims, int32_t wind
   const StepPlan p = step_plan(d, window, sinks);
   if (p.bytes > 0) MARL_REQUIRE_PTR(workspace);
   MARL_CHECK(check_places(out, {q, k, v}, true));
-  if (out.data == positions) return MARL_E_CONFIG;
   const int64_t slots = (int64_t)window + sinks;
-  const Extent ck = cached(d, cache.keys, slots, d.dim_k), cv = cached(d, cache.values, slots, d.dim_v);
-  if (ck.meets(cv)) return MARL_E_CONFIG;
-  for (const void* x : {(const void*)q.data, (const void*)k.data, (const void*)v.data, (const void*)out.data, (const void*)positions})
-    if (ck.holds(x) || cv.holds(x)) return MARL_E_CONFIG;
+  const Extent ck = cached(d, cache.keys, slots, d.dim_k), cv = cached(d, cache.values, slots, d.dim_v), ps = places_of(d, positions), ws = extent(workspace, p.bytes);
+  if (touches(out, d, d.n_heads, d.dim_v, {ck, cv, ps, ws}) || touches(q, d, d.n_heads, d.dim_k, {ck, cv, ws}) || touches(k, d, d.n_kv_heads, d.dim_k, {ck, cv, ws}) ||
+      touches(v, d, d.n_kv_heads, d.dim_v, {ck, cv, ws}))
+    return MARL_E_CONFIG;
+  if (ck.meets(cv) || ps.meets(ck) || ps.meets(cv) || ws.meets(ck) || ws.meets(cv) || ws.meets(ps)) return MARL_E_CONFIG;
   const int elem = d.precision == 0 ? 4 : 2;
   StepArgs a{};
   a.q = static_cast<const char*>(q.data);
