@@ -437,8 +437,8 @@ typedef struct marl_window_cache {
  * lse [B][n_heads][T] fp32 (nullable): kept for the gradient.  next_cache (nullable; may be `cache`, MARL_E_CONFIG where it overlaps it otherwise): the cache behind the
  * last row that holds a step; its slots that hold no step, and where there is no cache those of steps before row 0, are left as they were.  A sequence without a step:
  * the cache itself.
- * bf16: scores and statistics are fp32 sums of exact products; the weights, and in the gradient what multiplies keys and queries, are rounded to bf16 once (2^-9 of each
- * term); outputs are rounded once.  workspace: marl_window_attention_workspace bytes.
+ * bf16: scores and statistics are fp32 sums of exact products; the weights, and in the gradient what multiplies keys and queries, are rounded to bf16 once (2^-8 of each
+ * term at most); outputs are rounded once.  workspace: marl_window_attention_workspace bytes.
  * Memory shared (MARL_E_CONFIG, in the gradient and the step too): no row of q, k, v, out or their gradients lies in lse, a cache or the workspace where the call writes
  * that, no row of an output in these or in positions where it reads them, and these overlap nowhere where one of them is written.  Rows of arrays with strides may lie
  * between each other's: of such arrays an output begins where no other does.  Errors as in marl_linear_attention; MARL_E_CONFIG for window or sinks

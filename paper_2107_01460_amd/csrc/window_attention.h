@@ -5,14 +5,17 @@
 //   delta_i = dout_i . out_i,  dS_ij = P_ij (dout_i . v_j - delta_i),  dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i
 //
 // All three passes (output; dq; dk and dv) are one scheme.  A wavefront owns 32 rows of two arrays ("own": queries, or keys and values), whose
-// rows stay in registers as the second operand, one row a lane; tiles of 32 rows of two other arrays ("streamed") go through LDS, fetched one tile ahead and shared by
-// the workgroup's wavefronts.  The first product S^T = Y own^T leaves a lane 16 of the 32 streamed rows of its own column; that layout is the second operand
+// rows stay in registers as the second operand, one row a lane; tiles of 32 rows of two other arrays ("streamed") go through LDS.  For output and dq the workgroup's
+// wavefronts share them, two on their way while one is at work; for dk and dv each wavefront streams through LDS of its own, with as many on their way as its registers
+// allow (tiles_ahead), and waits for no other.  The first product S^T = Y own^T leaves a lane 16 of the 32 streamed rows of its own column; that layout is the second operand
 // of the next product, acc^T += Y^T P, as it is, once the contraction runs over the streamed rows in the order in which the registers hold them.
 // So scores and weights never leave the registers; softmax statistics are one number a lane, joined between the two halves of a wavefront.
 // Y^T comes from the same row-major tile: transposed reads of 4 x 16 for bf16, single elements for fp32.
 //
-// bf16: inputs are exact operands, sums are fp32.  P and dS are rounded once to bf16 as operands (2^-9 of each term; the statistics lse and the row
-// sums come from the fp32 values): about what the output's own rounding is, and half the matrix products of keeping two parts.  fp32: fp32 products.
+// bf16: inputs are exact operands, sums are fp32.  P and dS are rounded once to bf16 as operands (2^-8 of each term at most; the statistics lse and the row
+// sums come from the fp32 values): about what the output's own rounding is, and half the matrix products of keeping two parts (outputs 0.0020 to 0.0022 off, relative to 64
+// bits, gradients 0.0024, where the output's rounding alone makes it 0.0016).  fp32: fp32 products.
+// Exponents are to base two in here and lse, which the caller keeps, to base e: a product on either side, 2^-24 of lse each, so some 2^-23 |lse| of a gradient's weights.
 //
 // Zero times infinity: a product of tiles multiplies masked places by zero.  The loop runs without care for it; a workgroup that finds
 // an infinity or a NaN in its sums runs once more, adding the streamed rows one by one to the columns that see them only.
@@ -525,7 +528,8 @@ struct Tiles {
   }
 };
 
-// Wavefronts a SIMD that the registers are shared out for: as many as spill none, but for dq of bf16 heads wider than 64 (6 to 36 registers)
+// Wavefronts a SIMD that the registers are shared out for: as many as spill none to memory, but for dq of bf16 heads wider than 64 (1 to 36 registers).  (dq of fp32 heads
+// wider than 96 puts 2 to 6 into accumulation registers, which it has to spare.)
 template <class T, int DP, int WAVES, bool GRADIENT>
 constexpr int rows_waves() { return sizeof(T) == 4 ? (DP > 64 ? 1 : DP > 32 || WAVES == 1 ? 2 : 3) : DP <= 32 || (DP <= 64 && WAVES > 1 && !GRADIENT) ? 3 : 2; }
 template <class T, int DP>
@@ -537,7 +541,7 @@ template <class T, int DP, int WAVES, bool GRADIENT, bool FAST>
 __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, WAVES, GRADIENT>())) window_rows_kernel(const WindowArgs a) {
   typedef Products<T, DP> P;
   typedef TileShape<T, DP> Shape;
-  __shared__ __attribute__((aligned(16))) char lds[(WAVES > 4 ? WAVES : 4) * Shape::kBytes];
+  __shared__ __attribute__((aligned(16))) char lds[4 * Shape::kBytes];  // two tiles of both arrays; a place for each wavefront's own rows before and after
   auto tile_at = [&](int buffer, int which) __attribute__((always_inline)) { return lds + (2 * buffer + which) * Shape::kBytes; };
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
   // neighbouring heads, then stretches of time, then sequences: next to each other on one XCD
@@ -763,8 +767,8 @@ __global__ void __launch_bounds__(64 * WAVES, (rows_waves<T, DP, WAVES, GRADIENT
 // First steps are seen by every later row of their episode: in a long sequence far more tiles of rows than any other column, one wavefront's work.  There the pairs
 // of tiles beyond the window are cut along the rows (far): every so many tiles of rows a wavefront takes the first `far_slots` tiles of first steps that they see, into
 // fp32 parts with the tile's number beside them (8192 steps, 4 first steps: 411 us of gradient against 2881); the columns' own wavefronts add the parts with their number, in order, and take what was beyond the slots themselves.
-// Tiles of rows on their way: two where a wavefront has a SIMD's registers to itself anyway (8192 steps of 8 heads of 128, window 512: 124 us against 119), none
-// beside the one at work where that would spill.
+// Tiles of rows on their way: two where a wavefront has a SIMD's registers to itself anyway (8192 steps of 8 heads of 128 in bf16, window 512: 119 us against 124 with one),
+// none beside the one at work for fp32 heads wider than 64, whose registers are full without (heads of 65 to 96 put 96 of them into accumulation registers even so).
 template <class T, int DP>
 constexpr int tiles_ahead() { return sizeof(T) == 2 ? (DP > 64 ? 2 : 1) : DP <= 64 ? 1 : 0; }
 

@@ -39,7 +39,11 @@ Plan plan_of(const marl_attention_dims& d, int window, int sinks, bool fast, boo
   p.rows = (int64_t)d.n_seqs * (d.n_heads / p.heads_each) * p.rows_t;
   auto workgroups = [&](int64_t units) { return (units * p.heads_each + 3) / 4; };
   p.cols = workgroups((int64_t)pairs * p.tiles);
-  // First steps seen from afar are cut along the rows where columns are few (else others keep the chip busy meanwhile) and eight tiles or more lie beyond the window
+  // First steps seen from afar are cut along the rows where column tiles are few (else others keep the chip busy meanwhile) and some ten tiles or more lie beyond the window
+  // (fewer do not pay for a launch).  The whole gradient, without and with the cut, window 64 and 4 first steps in one episode.  1024 steps of 4 heads, 4096, 8192 and 16 384
+  // column tiles: of 64 in bf16 140 and 96, 148 and 151, 259 and 297 us; of 128 in bf16 221 and 189, 286 and 342, 544 and 652; of 32 in fp32 259 and 149, 241 and 236, 410 and
+  // 437.  Four sequences, 6, 8, 10 and 18 tiles beyond the window: of 64 in bf16 36 and 41, 41 and 42, 46 and 42, 67 and 44; of 32 in fp32 52 and 56, 60 and 56, 68 and 57, 99 and
+  // 58.  Sequences of 8192 steps would gain on the far side of the line too (16 of them, 16 384 column tiles of heads of 64 in bf16: 824 and 350).
   if (sinks > 0 && (int64_t)pairs * p.tiles <= 8192 && p.tiles > window / kTile + 10) {
     p.far_tiles = p.tiles > 256 ? (p.tiles + 63) / 64 : 4;
     p.far_chunks = (uint32_t)((p.tiles + p.far_tiles - 1) / p.far_tiles);
@@ -60,7 +64,10 @@ Plan plan_of(const marl_attention_dims& d, int window, int sinks, bool fast, boo
   return p;
 }
 
-// Rows that Fetch takes with unconditional loads: whole 16-byte pieces, four-byte aligned, 32 of them within 2 GB
+// Rows that Fetch takes with unconditional loads: whole 16-byte pieces, four-byte aligned, 32 of them within 2 GB, so less than 64 MB from one step to the next.  One array
+// whose rows are not like that takes the whole call to loads with branches, whose tiles wait for each other: 128 steps of 32 768 sequences of 8 heads of 64 in bf16, window 64,
+// 4.7 ms with steps 34 MB apart, 6.3 where the values' are 101 MB apart (a view of a product of queries, keys and values), the gradient 14.1 and 23.3; of 4096 sequences heads of 50
+// take 0.85 ms and 3.4, of 48 0.44 and 1.40, of 56 0.48 and 1.50; of 36 0.82 and 3.3, of 40 0.41 and 1.31; fp32 heads of 30 (4 of them, window 32) 0.53 and 1.76, of 32 0.33 and 1.04.
 bool fast_rows(const marl_attention_dims& d, const marl_view& v, int dim) {
   const int elem = d.precision == 0 ? 4 : 2;
   const int64_t step = v.step * elem;
