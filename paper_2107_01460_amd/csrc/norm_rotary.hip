@@ -4,28 +4,13 @@
 // Bound by memory: every element in and out once; table rows, weights and the partners of a rotation come from caches.  128 x 4096 steps of 8 + 8 heads of 64 in bf16: 427 us
 // for 2.1 GB; gradient of 4 + 2 heads of 32 in fp32: 228 us for 1.2 GB, and 7 for the sums of the weights' gradients: what a copy reaches.
 #include "attention_checks.h"
+#include "divisor.h"
 #include "lane_sums.h"
 
 namespace marl {
 namespace {
 
 constexpr int kMaxNormDim = 256;
-
-// Division of n < 2^31 by a number fixed at launch: a product and a shift.
-struct Divisor {
-  uint32_t d = 1, magic = 0;
-  int shift = 0;
-  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return __umulhi(2 * n, magic) >> (shift - 31); }
-};
-Divisor divisor(uint32_t d) {
-  Divisor r;
-  r.d = d;
-  int lg = 0;
-  while ((1u << lg) < d) ++lg;
-  r.shift = 31 + lg;
-  r.magic = (uint32_t)(((uint64_t)1 << r.shift) / d + 1);
-  return r;
-}
 
 struct NormArray {
   const char *x, *dy;

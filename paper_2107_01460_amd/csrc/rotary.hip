@@ -3,6 +3,7 @@
 // 389 us, 5.5 TB/s (one item a thread, division by division, table rows element by element: 616).  Rows that are no whole vectors go pair by pair: in bf16, as many
 // steps with heads of 40, all of each rotated: 758 us in halves (floor 272), 266 interleaved, where a row is whole vectors; of 32 with 8 rotated 948 and 207 (218).
 #include "common.h"
+#include "divisor.h"
 
 namespace marl {
 namespace {
@@ -30,23 +31,6 @@ __global__ void __launch_bounds__(256) rotary_table_kernel(marl_rotary_dims d, f
   sincos((double)position * f, &sine, &cosine);
   table[position * d.rotary_dim + i] = (float)(cosine * d.amplitude);
   table[position * d.rotary_dim + half + i] = (float)(sine * d.amplitude);
-}
-
-// Division of n < 2^31 by a number fixed at launch: a product and a shift.  (magic d = 2^shift + e with 0 < e <= 2^(shift - 31), so n magic / 2^shift
-// is less than n / d + 1 / d.)
-struct Divisor {
-  uint32_t d = 1, magic = 0;
-  int shift = 0;
-  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return __umulhi(2 * n, magic) >> (shift - 31); }
-};
-Divisor divisor(uint32_t d) {
-  Divisor r;
-  r.d = d;
-  int lg = 0;
-  while ((1u << lg) < d) ++lg;
-  r.shift = 31 + lg;
-  r.magic = (uint32_t)(((uint64_t)1 << r.shift) / d + 1);
-  return r;
 }
 
 // ---- rotation ----------------------------------------------------------------------------------------------------------------------
