@@ -405,7 +405,9 @@ int32_t marl_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, c
  * one pass: u = x * rstd * weight, rstd = 1 / sqrt(mean(x^2) + eps) over a head's dim (1..256) elements, weight [dim] for all heads of q, of k (fp32; NULL: 1); the
  * first rotary_dim elements of u are rotated, the others copied.  positions and first_position as in marl_rotary, but a row whose position is negative holds no
  * step: zeros.  A position behind the table gives NaNs in the rotated elements.  An output may be its input, with the same strides; otherwise it begins where no other
- * array does, and no row of it lies in the table, the weights or the positions (MARL_E_CONFIG).  The values between norm and rotation are not rounded.  dims: precision, n_steps, n_seqs, n_heads, n_kv_heads, dim_k, seqs_per_flag are read. */
+ * array does, and no row of it lies in the table, the weights or the positions (MARL_E_CONFIG).  The values between norm and rotation are not rounded.
+ * Squares are summed in fp32: a head whose sum of them passes 3.4e38 (elements of 1e18 and more) comes out as zeros.
+ * dims: precision, n_steps, n_seqs, n_heads, n_kv_heads, dim_k, seqs_per_flag are read. */
 int32_t marl_norm_rotary(const marl_attention_dims* dims, marl_view q, marl_view k, const float* q_weight, const float* k_weight, float eps,
                          const float* table, int32_t n_positions, int32_t rotary_dim, const int32_t* positions, int32_t first_position,
                          int32_t interleaved, marl_view q_out, marl_view k_out, void* stream);
@@ -448,7 +450,8 @@ int32_t marl_window_attention(const marl_attention_dims* dims, int32_t window, i
                               marl_window_cache next_cache, void* workspace, void* stream);
 
 /* Its gradient: dq, dk, dv from dout, and the call's own out and lse.  Steps of the cache are constants.  dk and dv of a head that query heads share are sums over
- * these, in a fixed order.  Rows that hold no step: zeros.  The outputs begin nowhere where another array does. */
+ * these, in a fixed order.  Rows that hold no step: zeros.  The outputs begin nowhere where another array does.  cache: as the call found it, so a copy where its
+ * next_cache was the cache itself. */
 int32_t marl_window_attention_backward(const marl_attention_dims* dims, int32_t window, int32_t sinks, marl_view q, marl_view k, marl_view v,
                                        const int32_t* positions, int32_t first_position, marl_window_cache cache, marl_view out,
                                        const float* lse, marl_view dout, marl_view dq, marl_view dk, marl_view dv, void* workspace,

@@ -705,7 +705,7 @@ def window_attention(q, k, v, out, window, sinks=0, lse=None, positions=None, fi
 
 def window_attention_backward(q, k, v, out, lse, dout, dq, dk, dv, window, sinks=0, positions=None, first_position=0, cache=None, scale=1.0, workspace=None,
                               stream=None):
-    """Gradients dq, dk, dv of window_attention from dout and what it kept; the cache's steps are constants."""
+    """Gradients dq, dk, dv of window_attention from dout and what it kept; the cache, as that call found it, holds constants."""
     _here(q, k, v, out, lse, dout, dq, dk, dv, positions, workspace, *(cache or ()))
     _int32(window, sinks, first_position)
     dims, T, B, H, Hk, Dk, Dv, at = _window_dims(q, k, v, positions, scale)

@@ -2,7 +2,7 @@
 //   u = x r w,  r = 1 / sqrt(mean(x^2) + eps),  y = turn(u);   with du = turn back(dy) and g = du w:  dx = r g - x r^3 mean(g x),  dw = sum over rows of du x r
 // dw is summed in fp32 (a lane's rows, then a workgroup's lanes, then the workgroups): 2.7e-7 off, relative to 64 bits, over 128 x 4096 steps of 4 heads in fp32.
 // Bound by memory: every element in and out once; table rows, weights and the partners of a rotation come from caches.  128 x 4096 steps of 8 + 8 heads of 64 in bf16: 427 us
-// for 2.1 GB; gradient of 4 + 2 heads of 32 in fp32: 228 us for 1.2 GB, and 7 for the sums of the weights' gradients: what a copy reaches.
+// for 2.1 GB; gradient of 4 + 2 heads of 32 in fp32: 237 us for 1.2 GB, and 8 for the sums of the weights' gradients: what a copy reaches.
 #include "attention_checks.h"
 #include "divisor.h"
 #include "lane_sums.h"
